@@ -45,7 +45,8 @@ typedef enum daf_status {
     DAF_ERR_WORKSPACE = -4,   /* workspace missing or smaller than daf_workspace_bytes                */
     DAF_ERR_CUDA = -5,        /* a CUDA runtime/driver call failed; see daf_last_cuda_error           */
     DAF_ERR_TIMEOUT = -6,     /* device: a bounded barrier wait ran out (from daf_poll_status)        */
-    DAF_ERR_BOUNDS = -7       /* device: an index outside its tensor was skipped (from daf_poll_status) */
+    DAF_ERR_BOUNDS = -7,      /* device: an index outside its tensor was skipped (from daf_poll_status) */
+    DAF_ERR_PAGES = -8        /* device: fewer free pages than a daf_page_fork asked for, nothing was changed (from daf_poll_status) */
 } daf_status;
 
 /* Problem statement of one layer (paper, "Methods", notation paragraph: L_d, L_q, r). */
@@ -355,6 +356,95 @@ int daf_last_cuda_error(void);
 
 /* Number of kernels this library has launched in this process (for accounting). */
 int64_t daf_launch_count(void);
+
+/* ---- Paged 8-bit cache: where the K/V rows of many sequences live once their context is repaired.
+ *
+ * A pool of pages of 16 to 128 tokens, shared by all layers of a model (the same page numbers in every layer):
+ *   k8, v8            bytes [n_layers, n_pages, n_kv_heads, page_tokens, 128], the 8-bit format of daf_expand_fp8_cache
+ *                     (1 sign, 4 exponent, 3 mantissa bits, no infinities, 0x7f and 0xff are NaN)
+ *   k_scale, v_scale  fp32 [n_layers, n_pages, n_kv_heads]: an element is worth scale * value.  daf_page_write leaves powers of
+ *                     two of at least 2^-60 here; the calls that read take any positive normal number.
+ *   table             int32 [n_seqs, max_pages]: page j of a sequence holds its tokens j * page_tokens and on.  Behind a
+ *                     sequence's last page: -1.
+ *   refs              int32 [n_pages]: how many entries of `table` name the page; 0: the page is free
+ * All of it is the caller's memory; refs starts as zeros and table as -1.  The calls take the sequences' lengths, positions and
+ * pages from device memory, so that a captured graph can be replayed while they change.
+ * Where a call takes `seqs` (int32 [n]), entry b of the call is row seqs[b] of `table`; NULL: row b.  Rows and sequences outside
+ * their tensors, and pages outside the pool where a sequence needs one, are skipped and recorded in the workspace's status word
+ * (DAF_ERR_BOUNDS from daf_poll_status): nothing faults.  Calls that change the same table, refs or pages must not overlap. */
+typedef struct daf_page_params {
+    int32_t n_pages;          /* pages of the pool (of each layer)                               */
+    int32_t page_tokens;      /* tokens of a page: 16, 32, 64 or 128                             */
+    int32_t n_kv_heads;       /* key/value heads, at most 256                                    */
+    int32_t head_dim;         /* must be 128                                                     */
+    int32_t n_layers;         /* layers of the pool                                              */
+    int32_t n_seqs;           /* rows of table                                                   */
+    int32_t max_pages;        /* columns of table; max_pages * page_tokens is at most 4M tokens  */
+} daf_page_params;
+
+/* Bytes of device scratch the daf_page_* calls need for up to n entries, and daf_page_attn for up to n sequences of L_q query
+ * tokens and n_q_heads query heads (0 where it is not called).  0: invalid parameters. */
+size_t daf_page_workspace_bytes(const daf_page_params* p, int32_t n, int32_t L_q, int32_t n_q_heads);
+
+/* Rows of fresh K/V into the pages of one layer.  Rows row_off[b] .. row_off[b + 1] - 1 of k and v belong to entry b.
+ *   lens     int32 [n] the sequences' lengths once this call is done
+ *   row_off  int32 [n + 1] ascending, from 0
+ *   idx      NULL: the rows are the newest tokens, positions lens[b] - rows .. lens[b] - 1.  Otherwise int32 [row_off[n]]: the row's
+ *            position, ascending within an entry and below lens[b] (the important tokens of daf_select, to be replaced in
+ *            place).  Of equal positions the last row counts.
+ *   max_rows no entry has more rows than this
+ *   k, v     bf16 [row_off[n], n_kv_heads, 128]
+ *   refs     may be NULL; else a page that is not named exactly once is left alone and recorded (DAF_ERR_BOUNDS): copy it first
+ * A page's scale for a head is the least power of two (2^-60 at least) that brings the finite new rows into the format's range
+ * and, where the page keeps other tokens below the sequence's length, at least the page's old one; kept bytes are then rounded
+ * again.  Rounding is to nearest even; infinities become the largest value, NaN stays NaN. */
+int daf_page_write(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* lens,
+                   const int32_t* row_off, const int32_t* idx, int32_t max_rows, const void* k, const void* v,
+                   const int32_t* table, const int32_t* refs, void* k8, void* v8, float* k_scale, float* v_scale,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Tokens of sequences as bf16 rows (bf16(scale * value), as daf_expand_fp8_cache gives them and daf_layer takes a cache):
+ * positions first[b] .. of entry b become rows row_off[b] .. row_off[b + 1] - 1 of k_rows and v_rows (first NULL: from 0). */
+int daf_page_read(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* first,
+                  const int32_t* row_off, int32_t max_rows, const int32_t* table, const void* k8, const void* v8,
+                  const float* k_scale, const float* v_scale, void* k_rows, void* v_rows,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of the newest L_q tokens of n sequences over their pages: query token t of entry b sees the keys at positions up to
+ * lens[b] - L_q + t (the tokens of this call are in the pages already).  L_q = 1 is a decoding step.
+ *   q     bf16 [n, L_q, n_q_heads, 128];  out  the same shape;  lse  fp32 [n, n_q_heads, L_q] or NULL
+ *   softmax_scale  <= 0 selects 1/sqrt(128)
+ * A row that sees no key is zeros with an lse of -inf.  At most 4096 sequences a call. */
+int daf_page_attn(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* lens, int32_t L_q,
+                  int32_t n_q_heads, float softmax_scale, const void* q, const int32_t* table, const void* k8, const void* v8,
+                  const float* k_scale, const float* v_scale, void* out, float* lse,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gives sequences pages.  Item i (int32 device arrays of n):
+ *   src[i] >= 0, another row   row dst[i], which must hold no pages, becomes a copy of the first keep[i] tokens of row src[i], with
+ *                              pages for want[i] tokens.  Pages held whole are shared (share != 0: same page, refs + 1) or copied
+ *                              in every layer; a page of which only a part is kept is always copied.
+ *   src[i] < 0                 row dst[i], which must hold no pages, gets pages for want[i] tokens (keep is not read)
+ *   src[i] == dst[i]           the row grows to pages for want[i] tokens.  keep[i] is its length now: the page its next token
+ *                              goes into is replaced by a copy if others share it.
+ * New pages are the free ones of lowest number, in the items' order, and start with whatever they held.  A row named as dst must
+ * not be named by any other item.  If an item is not as described, or the free pages are too few, nothing is changed and
+ * DAF_ERR_BOUNDS or DAF_ERR_PAGES recorded. */
+int daf_page_fork(const daf_page_params* p, int32_t n, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                  const int32_t* want, int32_t share, int32_t* table, int32_t* refs, void* k8, void* v8, float* k_scale,
+                  float* v_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Takes pages back: rows seqs[i] keep the pages that hold their first keep[i] tokens (NULL: none); the other entries become -1
+ * and their pages' refs one less. */
+int daf_page_free(const daf_page_params* p, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t* table, int32_t* refs,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Moves the pages in use to the front of the pool: of `live` pages in use those numbered `live` and up go, in ascending order, to
+ * the free ones below, in ascending order, in every layer.  table_out and refs_out (which may be table and refs themselves) get
+ * the new numbers and counts, live_out (int32 [1], may be NULL) the number of pages in use. */
+int daf_page_compact(const daf_page_params* p, const int32_t* table, const int32_t* refs, int32_t* table_out, int32_t* refs_out,
+                     int32_t* live_out, void* k8, void* v8, float* k_scale, float* v_scale,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

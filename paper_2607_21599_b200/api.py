@@ -25,6 +25,7 @@ DAF_ERR_WORKSPACE = -4
 DAF_ERR_CUDA = -5
 DAF_ERR_TIMEOUT = -6
 DAF_ERR_BOUNDS = -7
+DAF_ERR_PAGES = -8
 
 EXPORTS = [
     "daf_num_important", "daf_workspace_bytes", "daf_workspace_init", "daf_select", "daf_important_attn",
@@ -33,6 +34,8 @@ EXPORTS = [
     "daf_qd_attn_static", "daf_qd_attn_static_max_bytes", "daf_deviation_scores", "daf_blend_attn",
     "daf_imp_qd_attn", "daf_selftest_bounded_wait", "daf_qd_attn_static_poll_status",
     "daf_imp_qd_attn_launches", "daf_select_from_kv", "daf_expand_fp8_cache", "daf_layer_fp8", "daf_check_indices", "daf_select_topk",
+    "daf_page_workspace_bytes", "daf_page_write", "daf_page_read", "daf_page_attn", "daf_page_fork", "daf_page_free",
+    "daf_page_compact",
 ]
 
 
@@ -53,6 +56,23 @@ class daf_params(ctypes.Structure):
 def make_params(L_d: int, L_q: int, r: float, n_q_heads: int, n_kv_heads: int, head_dim: int = 128,
                 softmax_scale: float = 0.0, fuse_mode: int = 0, overwrite_doc_kv: int = 1) -> daf_params:
     return daf_params(L_d, L_q, r, n_q_heads, n_kv_heads, head_dim, softmax_scale, fuse_mode, overwrite_doc_kv)
+
+
+class daf_page_params(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("n_layers", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+    ]
+
+
+def make_page_params(n_pages: int, page_tokens: int, n_kv_heads: int, n_seqs: int, max_pages: int, n_layers: int = 1,
+                     head_dim: int = 128) -> daf_page_params:
+    return daf_page_params(n_pages, page_tokens, n_kv_heads, head_dim, n_layers, n_seqs, max_pages)
 
 
 class DafError(RuntimeError):
@@ -125,6 +145,21 @@ def lib() -> ctypes.CDLL:
         L.daf_select_topk.argtypes = [pp, vp, i32, vp, vp, sz, vp]
         L.daf_check_indices.restype = ctypes.c_int
         L.daf_check_indices.argtypes = [pp, i32, vp, vp, sz, vp]
+        pg = ctypes.POINTER(daf_page_params)
+        L.daf_page_workspace_bytes.restype = sz
+        L.daf_page_workspace_bytes.argtypes = [pg, i32, i32, i32]
+        L.daf_page_write.restype = ctypes.c_int
+        L.daf_page_write.argtypes = [pg, i32, i32] + [vp] * 4 + [i32] + [vp] * 4 + [vp] * 4 + [vp, sz, vp]
+        L.daf_page_read.restype = ctypes.c_int
+        L.daf_page_read.argtypes = [pg, i32, i32] + [vp] * 3 + [i32, vp] + [vp] * 4 + [vp, vp] + [vp, sz, vp]
+        L.daf_page_attn.restype = ctypes.c_int
+        L.daf_page_attn.argtypes = [pg, i32, i32, vp, vp, i32, i32, ctypes.c_float, vp, vp] + [vp] * 4 + [vp, vp] + [vp, sz, vp]
+        L.daf_page_fork.restype = ctypes.c_int
+        L.daf_page_fork.argtypes = [pg, i32] + [vp] * 4 + [i32, vp, vp] + [vp] * 4 + [vp, sz, vp]
+        L.daf_page_free.restype = ctypes.c_int
+        L.daf_page_free.argtypes = [pg, i32] + [vp] * 4 + [vp, sz, vp]
+        L.daf_page_compact.restype = ctypes.c_int
+        L.daf_page_compact.argtypes = [pg] + [vp] * 5 + [vp] * 4 + [vp, sz, vp]
         L.daf_poll_status.restype = ctypes.c_int
         L.daf_poll_status.argtypes = [vp, vp]
         L.daf_selftest_bounded_wait.restype = ctypes.c_int
@@ -349,6 +384,56 @@ def daf_select_topk(p, scores, n_sig, idx_out, workspace, stream=None) -> int:
 
 def daf_check_indices(p, k, idx, workspace, stream=None) -> int:
     return lib().daf_check_indices(ctypes.byref(p), int(k), _ptr(idx), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def daf_page_workspace_bytes(p: daf_page_params, n: int, L_q: int = 0, n_q_heads: int = 0) -> int:
+    return int(lib().daf_page_workspace_bytes(ctypes.byref(p), int(n), int(L_q), int(n_q_heads)))
+
+
+def alloc_page_workspace(p: daf_page_params, n: int, L_q: int = 0, n_q_heads: int = 0, device="cuda") -> torch.Tensor:
+    """A zeroed device buffer of daf_page_workspace_bytes(p, n, L_q, n_q_heads) bytes (torch owns the memory)."""
+    size = daf_page_workspace_bytes(p, n, L_q, n_q_heads)
+    if size == 0:
+        raise DafError(DAF_ERR_INVALID_ARG, "daf_page_workspace_bytes")
+    return torch.zeros(size, dtype=torch.uint8, device=device)
+
+
+def daf_page_write(p, layer, n, seqs, lens, row_off, idx, max_rows, k, v, table, refs, k8, v8, k_scale, v_scale, workspace,
+                   stream=None) -> int:
+    return lib().daf_page_write(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(lens), _ptr(row_off), _ptr(idx),
+                                int(max_rows), _ptr(k), _ptr(v), _ptr(table), _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale),
+                                _ptr(v_scale), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def daf_page_read(p, layer, n, seqs, first, row_off, max_rows, table, k8, v8, k_scale, v_scale, k_rows, v_rows, workspace,
+                  stream=None) -> int:
+    return lib().daf_page_read(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(first), _ptr(row_off), int(max_rows),
+                               _ptr(table), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(k_rows), _ptr(v_rows),
+                               _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def daf_page_attn(p, layer, n, seqs, lens, L_q, n_q_heads, softmax_scale, q, table, k8, v8, k_scale, v_scale, out, lse,
+                  workspace, stream=None) -> int:
+    return lib().daf_page_attn(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(lens), int(L_q), int(n_q_heads),
+                               float(softmax_scale), _ptr(q), _ptr(table), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale),
+                               _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def daf_page_fork(p, n, src, dst, keep, want, share, table, refs, k8, v8, k_scale, v_scale, workspace, stream=None) -> int:
+    return lib().daf_page_fork(ctypes.byref(p), int(n), _ptr(src), _ptr(dst), _ptr(keep), _ptr(want), int(bool(share)), _ptr(table),
+                               _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(workspace),
+                               _nbytes(workspace), _stream(stream))
+
+
+def daf_page_free(p, n, seqs, keep, table, refs, workspace, stream=None) -> int:
+    return lib().daf_page_free(ctypes.byref(p), int(n), _ptr(seqs), _ptr(keep), _ptr(table), _ptr(refs), _ptr(workspace),
+                               _nbytes(workspace), _stream(stream))
+
+
+def daf_page_compact(p, table, refs, table_out, refs_out, live_out, k8, v8, k_scale, v_scale, workspace, stream=None) -> int:
+    return lib().daf_page_compact(ctypes.byref(p), _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(live_out),
+                                  _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(workspace), _nbytes(workspace),
+                                  _stream(stream))
 
 
 def daf_poll_status(workspace, stream=None) -> int:

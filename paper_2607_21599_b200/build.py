@@ -8,7 +8,7 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libdaf_b200.so")
-SOURCES = ["daf_api.cu", "daf_select.cu", "daf_attn.cu"]
+SOURCES = ["daf_api.cu", "daf_select.cu", "daf_attn.cu", "daf_pages.cu", "daf_page_attn.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--use_fast_math", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -724,6 +724,7 @@ const char* daf_strerror(int status) {
         case DAF_ERR_CUDA: return "CUDA call failed (see daf_last_cuda_error)";
         case DAF_ERR_TIMEOUT: return "device-side bounded wait ran out";
         case DAF_ERR_BOUNDS: return "device-side index out of range";
+        case DAF_ERR_PAGES: return "not enough free pages";
         default: return "unknown status";
     }
 }

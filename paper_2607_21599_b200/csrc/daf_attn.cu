@@ -1059,7 +1059,7 @@ static int set_kernel_attributes() {
 
 // SMs of the current device (asked once per device; 148 on B200).  Planning runs on the host and also
 // without a device (workspace sizing in CPU-only processes): then the B200 figure is used.
-static int num_sms() {
+int num_sms() {
     static std::atomic<int> cached[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { (void)cudaGetLastError(); return kNumSMsDefault; }

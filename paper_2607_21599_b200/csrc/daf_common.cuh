@@ -88,6 +88,18 @@ int launch_attention_joint(const void* q_imp, const void* q_fresh, bool q_in_pla
                            float scale, DeviceStatus* status, void* scratch, size_t scratch_bytes, cudaStream_t stream,
                            int launches = 3);   // launches: bit 0 the attention launch, bit 1 the merge
 
+// The paged 8-bit cache (daf_pages.cu: the C ABI of the daf_page_* calls and the kernels that write, read and manage pages;
+// daf_page_attn.cu: the attention over it).
+constexpr int kPageMaxSeqs = 4096;      // sequences of one attention call: their running sums of work lie in shared memory
+struct Pool {                           // one layer of it
+    int n_pages, T, Hkv, n_seqs, max_pages;
+    uint8_t* k8; uint8_t* v8; float* k_scale; float* v_scale;
+};
+size_t page_attn_scratch_bytes(int n, int L_q, int Hq, int Hkv);
+int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t* lens, int L_q, int Hq, float scale, const void* q,
+                     const int32_t* table, void* out, float* lse, DeviceStatus* status, void* scratch, cudaStream_t stream);
+int num_sms();                          // SMs of the current device
+
 // ---------------------------------------------------------------- device side
 #ifdef __CUDACC__
 

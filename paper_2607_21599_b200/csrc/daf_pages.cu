@@ -1,0 +1,806 @@
+// The paged 8-bit cache: argument checks of all daf_page_* calls, and the kernels that write rows into pages, read them back,
+// and hand out, copy, take back and compact pages.  All of these move bytes: what bounds them is HBM where there are many and
+// the length of the chain of dependent accesses (positions -> page -> scale -> bytes) where there are few.
+#include <cuda_fp16.h>
+
+#include "daf_common.cuh"
+
+namespace daf {
+
+constexpr int kMinScaleExp = -60;      // scales that the writer leaves are at least 2^-60
+
+// ------------------------------------------------------------------------------------------------------------- 8-bit values
+__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+__device__ __forceinline__ float4 unpack_e4m3x4(uint32_t w) {
+    uint32_t lo, hi;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)(w & 0xFFFFu)));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(w >> 16)));
+    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&lo)), b = __half22float2(*reinterpret_cast<__half2*>(&hi));
+    return make_float4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }      // -126 <= e <= 127
+
+// Largest magnitude (bf16 bits, which ascend with it) among the finite ones of four bf16 values.
+__device__ __forceinline__ uint32_t finite_max4(uint2 w) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t b = ((i & 2 ? w.y : w.x) >> (16 * (i & 1))) & 0x7FFFu;
+        m = max(m, b < 0x7F80u ? b : 0u);
+    }
+    return m;
+}
+// Exponent of the least power of two s with magnitude <= 448 s (448 = 1.75 * 2^8), at least kMinScaleExp.
+__device__ __forceinline__ int scale_exp(uint32_t bf16_bits) {
+    const int e = (int)(bf16_bits >> 7) - 127 - 8 + ((bf16_bits & 0x7Fu) > 0x60u ? 1 : 0);
+    return max(e, kMinScaleExp);
+}
+
+// ---------------------------------------------------------------------------------------------------------- rows into pages
+struct WriteArgs {
+    Pool p;
+    int n, slots;               // `slots` CTAs share an entry's pages (for each head, K and V apart)
+    const int32_t* seqs; const int32_t* lens; const int32_t* row_off; const int32_t* idx;
+    const __nv_bfloat16* k; const __nv_bfloat16* v;
+    const int32_t* table; const int32_t* refs;
+    DeviceStatus* status;
+};
+
+// First of positions [a, b) of an ascending list whose value is at least `key`, found by all 128 threads of a CTA: 128 probes a
+// round, so that 16k positions take two round trips to L2 instead of the fourteen of a bisection.
+__device__ __forceinline__ int first_at_least(const int32_t* idx, int a, int b, int key) {
+    while (a < b) {
+        const int step = (b - a + 127) / 128, at = a + (int)threadIdx.x * step;
+        const int below = __syncthreads_count(at < b && __ldg(idx + at) < key);
+        if (step == 1) return a + below;
+        if (below == 0) return a;
+        b = min(b, a + below * step);
+        a = a + (below - 1) * step + 1;
+    }
+    return a;
+}
+
+// One CTA of four warps takes one page, one head, K or V at a time.  Every new row of it is read once and held in registers
+// (kRows rows a warp, four elements a lane) while the CTA finds their largest magnitude; the rows then leave scaled.  Kept bytes are
+// touched only where the scale grows.
+template <int kRows>
+__global__ void __launch_bounds__(128) page_write_kernel(const WriteArgs a) {
+    __shared__ int row_of[4 * kRows];          // new row of each token of the page, -1: none
+    __shared__ uint32_t warp_max[4];
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int T = 4 * kRows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.x / a.slots, h = blockIdx.y, Hkv = a.p.Hkv;
+    const bool reports = h == 0 && blockIdx.z == 0;       // (one of the CTAs that see the same fault)
+    const int seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b, len = __ldg(a.lens + b);
+    const int r_lo = __ldg(a.row_off + b), r_hi = __ldg(a.row_off + b + 1);
+    if (r_hi <= r_lo) return;
+    if ((unsigned)seq >= (unsigned)a.p.n_seqs || len < 0 || (long long)len > (long long)a.p.max_pages * T || r_lo < 0 ||
+        (a.idx == nullptr && r_hi - r_lo > len)) {
+        if (reports) report_status(a.status, DAF_ERR_BOUNDS, 200, b);
+        return;
+    }
+    const int start = a.idx == nullptr ? len - (r_hi - r_lo) : 0;       // first token that may be written
+    const int kept_to = a.idx == nullptr ? start : len;                 // tokens below this were there before
+    const __nv_bfloat16* const src = blockIdx.z ? a.v : a.k;
+    uint8_t* const pool = blockIdx.z ? a.p.v8 : a.p.k8;
+    float* const scales = blockIdx.z ? a.p.v_scale : a.p.k_scale;
+    for (int j = start / T + (int)(blockIdx.x % a.slots); j * T < len; j += a.slots) {
+        const int base = j * T;
+        int ra, rb;
+        if (a.idx == nullptr) {
+            ra = r_lo + max(base, start) - start;
+            rb = r_lo + min(base + T, len) - start;
+        } else {
+            ra = first_at_least(a.idx, r_lo, r_hi, base);
+            rb = first_at_least(a.idx, ra, r_hi, base + T);
+        }
+        if (ra >= rb) continue;
+        const int page = __ldg(a.table + (size_t)seq * a.p.max_pages + j);
+        const bool in_pool = (unsigned)page < (unsigned)a.p.n_pages;
+        if (!in_pool || (a.refs != nullptr && __ldg(a.refs + page) != 1)) {
+            if (reports) report_status(a.status, DAF_ERR_BOUNDS, in_pool ? 202 : 201, page);
+            continue;
+        }
+        for (int t = threadIdx.x; t < T; t += 128) row_of[t] = -1;
+        __syncthreads();
+        for (int r = ra + threadIdx.x; r < rb; r += 128) {
+            const int at = a.idx == nullptr ? r - r_lo + start : __ldg(a.idx + r);
+            if (at >= base && at < min(base + T, len)) atomicMax(&row_of[at - base], r);
+            else if (reports) report_status(a.status, DAF_ERR_BOUNDS, 203, at);       // the list does not ascend
+        }
+        __syncthreads();
+        uint2 w[kRows];
+        uint32_t m = 0;
+        bool keeps = false;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int r = row_of[warp + 4 * i];
+            w[i] = make_uint2(0u, 0u);
+            if (r >= 0) w[i] = __ldg(reinterpret_cast<const uint2*>(src + ((size_t)r * Hkv + h) * 128) + lane);
+            else keeps |= base + warp + 4 * i < kept_to;
+        }
+        float* const scale_at = scales + (size_t)page * Hkv + h;
+        const float s_old = __ldcg(scale_at);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) m = max(m, finite_max4(w[i]));
+        m = __reduce_max_sync(0xFFFFFFFFu, m);
+        if (lane == 0) warp_max[warp] = m;
+        keeps = __syncthreads_or(keeps);
+        m = max(max(warp_max[0], warp_max[1]), max(warp_max[2], warp_max[3]));
+        int e = scale_exp(m);
+        if (keeps) {       // at least the old scale, rounded up to a power of two if it is none
+            const int bits = __float_as_int(s_old);
+            e = max(e, min((bits >> 23) - 127 + ((bits & 0x7FFFFF) != 0 ? 1 : 0), 120));
+        }
+        uint32_t* const dst = reinterpret_cast<uint32_t*>(pool + ((size_t)page * Hkv + h) * (T * 128)) + lane;
+        const float inv = pow2f(-e), s_new = pow2f(e);
+        const bool again = keeps && s_new != s_old;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int t = warp + 4 * i;
+            if (row_of[t] >= 0) {
+                const float x0 = __uint_as_float(w[i].x << 16), x1 = __uint_as_float(w[i].x & 0xFFFF0000u);
+                const float x2 = __uint_as_float(w[i].y << 16), x3 = __uint_as_float(w[i].y & 0xFFFF0000u);
+                dst[t * 32] = pack_e4m3x4(x0 * inv, x1 * inv, x2 * inv, x3 * inv);
+            } else if (again && base + t < kept_to) {
+                const float f = s_old * inv;
+                const float4 x = unpack_e4m3x4(dst[t * 32]);
+                dst[t * 32] = pack_e4m3x4(x.x * f, x.y * f, x.z * f, x.w * f);
+            }
+        }
+        if (threadIdx.x == 0) *scale_at = s_new;
+        __syncthreads();       // row_of and warp_max are used again
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------- pages into rows
+struct ReadArgs {
+    Pool p;
+    int n, slots;
+    const int32_t* seqs; const int32_t* first; const int32_t* row_off; const int32_t* table;
+    __nv_bfloat16* k; __nv_bfloat16* v;
+    DeviceStatus* status;
+};
+
+__device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi, float s) {
+    const float4 x = unpack_e4m3x4(lo), y = unpack_e4m3x4(hi);
+    return make_uint4(pack_bf16(x.x * s, x.y * s), pack_bf16(x.z * s, x.w * s), pack_bf16(y.x * s, y.y * s), pack_bf16(y.z * s, y.w * s));
+}
+
+// One CTA takes one page, one head, K or V at a time: T * 8 chunks of 16 bytes, all of a thread's requested ahead of the first
+// use; a chunk becomes 32 bytes of its row.
+template <int kChunks>      // page_tokens * 8 / 128
+__global__ void __launch_bounds__(128) page_read_kernel(const ReadArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int T = kChunks * 16;
+    const int b = blockIdx.x / a.slots, h = blockIdx.y, Hkv = a.p.Hkv;
+    const bool reports = h == 0 && blockIdx.z == 0 && threadIdx.x == 0;
+    const int seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b, first = a.first != nullptr ? __ldg(a.first + b) : 0;
+    const int r_lo = __ldg(a.row_off + b), r_hi = __ldg(a.row_off + b + 1);
+    if (r_hi <= r_lo) return;
+    if ((unsigned)seq >= (unsigned)a.p.n_seqs || first < 0 || r_lo < 0 ||
+        (long long)first + (r_hi - r_lo) > (long long)a.p.max_pages * T) {
+        if (reports) report_status(a.status, DAF_ERR_BOUNDS, 210, b);
+        return;
+    }
+    const int end = first + (r_hi - r_lo);
+    const uint8_t* const pool = blockIdx.z ? a.p.v8 : a.p.k8;
+    const float* const scales = blockIdx.z ? a.p.v_scale : a.p.k_scale;
+    __nv_bfloat16* const out = blockIdx.z ? a.v : a.k;
+    for (int j = first / T + (int)(blockIdx.x % a.slots); j * T < end; j += a.slots) {
+        const int page = __ldg(a.table + (size_t)seq * a.p.max_pages + j);
+        if ((unsigned)page >= (unsigned)a.p.n_pages) {
+            if (reports) report_status(a.status, DAF_ERR_BOUNDS, 211, page);
+            continue;
+        }
+        const float s = __ldg(scales + (size_t)page * Hkv + h);
+        const uint4* const src = reinterpret_cast<const uint4*>(pool + ((size_t)page * Hkv + h) * (T * 128)) + threadIdx.x;
+        uint4 w[kChunks];
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int at = j * T + i * 16 + (int)(threadIdx.x >> 3);
+            if (at >= first && at < end) w[i] = __ldcs(src + i * 128);
+        }
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int at = j * T + i * 16 + (int)(threadIdx.x >> 3);
+            if (at >= first && at < end) {
+                uint4* const dst = reinterpret_cast<uint4*>(out + ((size_t)(r_lo + at - first) * Hkv + h) * 128) + 2 * (threadIdx.x & 7);
+                dst[0] = widen8(w[i].x, w[i].y, s);
+                dst[1] = widen8(w[i].z, w[i].w, s);
+            }
+        }
+    }
+}
+
+// ----------------------------------------------------------------------------------------------------- which pages go where
+// Both fork and compact run as two kernels: one CTA decides (who gets which page, which page is copied to which) from counts and
+// prefix sums over items and over refs, then a grid does what was decided: table, refs and the bytes.
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanRefs = 16;            // refs a thread looks at per round: 16k pages a round
+
+struct PlanHead { int ok, n_new, n_copies, live; };
+struct PlanArrays {       // in the workspace behind the status word
+    PlanHead* head;
+    int2* copies;         // [n_pages] (from, to)
+    int32_t* fresh;       // [n_pages] pages handed out, ascending (compact: where a moved page goes, by its old number)
+    int32_t* marks;       // [n_seqs]
+    int2* items;          // [n + 1] running counts: new pages, copies
+};
+
+// Exclusive prefix sums of two counts packed in 64 bits over the 1024 threads of a CTA; *total gets the sums.
+__device__ __forceinline__ unsigned long long block_scan(unsigned long long v, unsigned long long* total) {
+    __shared__ unsigned long long sums[33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned long long x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        unsigned long long s = sums[lane], t = s;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, t, o);
+            if (lane >= o) t += y;
+        }
+        sums[lane] = t - s;
+        if (lane == 31) sums[32] = t;
+    }
+    __syncthreads();
+    const unsigned long long before = sums[warp] + x - v;
+    *total = sums[32];
+    __syncthreads();
+    return before;
+}
+__device__ __forceinline__ unsigned long long pack2(int a, int b) { return ((unsigned long long)(unsigned)a << 32) | (unsigned)b; }
+
+struct ForkArgs {
+    int n_pages, T, n_seqs, max_pages, n, share;
+    const int32_t* src; const int32_t* dst; const int32_t* keep; const int32_t* want;
+    int32_t* table; int32_t* refs;
+    PlanArrays w;
+    DeviceStatus* status;
+};
+
+// What one item asks for.  Its new pages, in order: `cow` or the copies of kept pages first, then empty ones.
+struct ForkItem {
+    int src, dst, first_new, n_new, n_copies;     // columns first_new .. first_new + n_new - 1 get new pages (a replaced one included)
+};
+__device__ __forceinline__ ForkItem fork_item(const ForkArgs& a, int i, bool* bad) {
+    ForkItem f;
+    f.src = __ldg(a.src + i); f.dst = __ldg(a.dst + i);
+    f.first_new = f.n_new = f.n_copies = 0;
+    const int want = __ldg(a.want + i), keep = f.src >= 0 ? __ldg(a.keep + i) : 0;
+    const long long room = (long long)a.max_pages * a.T;
+    if ((unsigned)f.dst >= (unsigned)a.n_seqs || f.src >= a.n_seqs || want < 0 || want > room || keep < 0 || keep > room) {
+        *bad = true;
+        return f;
+    }
+    const int32_t* const row = a.table + (size_t)f.dst * a.max_pages;
+    const int pages = (want + a.T - 1) / a.T, held = (keep + a.T - 1) / a.T, whole = keep / a.T;
+    if (f.src == f.dst) {
+        int lo = 0, hi = a.max_pages;             // entries in use come first
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (row[mid] >= 0) lo = mid + 1; else hi = mid;
+        }
+        if (held > lo) { *bad = true; return f; }
+        f.first_new = lo;
+        f.n_new = max(pages - lo, 0);
+        // a page of which a part is kept, shared with others: replaced (fork_column says where its copy comes from)
+        if (whole < held && (unsigned)row[whole] < (unsigned)a.n_pages && a.refs[row[whole]] > 1) { f.n_copies = 1; f.n_new += 1; }
+    } else {
+        if (row[0] >= 0) { *bad = true; return f; }
+        if (f.src >= 0 && held > 0 && a.table[(size_t)f.src * a.max_pages + held - 1] < 0) { *bad = true; return f; }
+        f.first_new = a.share ? whole : 0;
+        f.n_copies = held - f.first_new;
+        f.n_new = max(pages, held) - f.first_new;
+    }
+    return f;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const ForkArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tid = threadIdx.x;
+    __shared__ int any_bad;
+    if (tid == 0) any_bad = 0;
+    for (int i = tid; i < a.n_seqs; i += kPlanThreads) a.w.marks[i] = 0;
+    __syncthreads();
+    // every row at most once as a target, and no target as another item's source
+    for (int i = tid; i < a.n; i += kPlanThreads) {
+        const int d = __ldg(a.dst + i);
+        if ((unsigned)d < (unsigned)a.n_seqs && atomicAdd(&a.w.marks[d], 1) != 0) any_bad = 1;
+    }
+    __syncthreads();
+    unsigned long long run = 0;
+    for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
+        const int i = i0 + tid;
+        bool bad = false;
+        ForkItem f = {};
+        if (i < a.n) {
+            f = fork_item(a, i, &bad);
+            if (f.src >= 0 && f.src < a.n_seqs && f.src != f.dst && __ldcg(&a.w.marks[f.src]) != 0) bad = true;
+            if (bad) any_bad = 1;
+        }
+        unsigned long long sum;
+        const unsigned long long at = run + block_scan(pack2(f.n_new, f.n_copies), &sum);
+        if (i < a.n) a.w.items[i] = make_int2((int)(at >> 32), (int)(at & 0xFFFFFFFFu));
+        run += sum;
+        if ((run >> 32) > (unsigned long long)a.n_pages) break;      // more than there are: the counts need not fit 32 bits
+    }
+    const long long n_new = (long long)(run >> 32);
+    const int n_copies = (int)(run & 0xFFFFFFFFu);
+    __syncthreads();
+    if (any_bad || n_new > a.n_pages) {
+        if (tid == 0) {
+            report_status(a.status, any_bad ? DAF_ERR_BOUNDS : DAF_ERR_PAGES, 220, (int)n_new);
+            *a.w.head = PlanHead{0, 0, 0, 0};
+        }
+        return;
+    }
+    // the n_new free pages of lowest number
+    int found = 0;
+    for (int p0 = 0; p0 < a.n_pages && found < n_new; p0 += kPlanThreads * kPlanRefs) {
+        const int p = p0 + tid * kPlanRefs;
+        unsigned free_bits = 0;
+#pragma unroll
+        for (int u = 0; u < kPlanRefs; ++u)
+            if (p + u < a.n_pages && a.refs[p + u] == 0) free_bits |= 1u << u;
+        unsigned long long sum;
+        int at = found + (int)block_scan((unsigned long long)__popc(free_bits), &sum);
+        for (unsigned m = free_bits; m != 0 && at < n_new; m &= m - 1) a.w.fresh[at++] = p + __ffs(m) - 1;
+        found += (int)sum;
+    }
+    const bool ok = found >= n_new;
+    if (tid == 0) {
+        if (!ok) report_status(a.status, DAF_ERR_PAGES, 221, (int)n_new);
+        *a.w.head = PlanHead{ok ? 1 : 0, (int)n_new, ok ? n_copies : 0, 0};
+        a.w.items[a.n] = make_int2((int)n_new, n_copies);
+    }
+    __syncthreads();
+    if (!ok) return;
+    // the copies: a warp per item
+    for (int i = tid >> 5; i < a.n; i += kPlanThreads / 32) {
+        const int2 at = a.w.items[i];
+        const int n_c = a.w.items[i + 1].y - at.y;
+        const int src = __ldg(a.src + i), dst = __ldg(a.dst + i);
+        const int first = (src == dst || a.share) ? __ldg(a.keep + i) / a.T : 0;      // (n_c > 0 only where src >= 0)
+        for (int c = tid & 31; c < n_c; c += 32) {
+            int from = a.table[(size_t)src * a.max_pages + first + c];
+            if ((unsigned)from >= (unsigned)a.n_pages) {
+                report_status(a.status, DAF_ERR_BOUNDS, 222, from);
+                from = -1;
+            }
+            a.w.copies[at.y + c] = make_int2(from, a.w.fresh[at.x + c]);
+        }
+    }
+}
+
+struct MoveArgs {          // the bytes of pages, K and V with their scales, in all layers
+    uint4* k8; uint4* v8; float* k_scale; float* v_scale;
+    long long n_pages;
+    int Hkv, n_layers, page_chunks;      // chunks of 16 bytes of one page of one layer, K or V
+};
+constexpr int kMoveThreads = 256, kMoveUnroll = 4;
+
+// The pages of copies[0 .. n) by the whole grid: pieces of 16 KB, every thread's four chunks requested before the first is stored.
+__device__ __forceinline__ void move_pages(const MoveArgs& m, const int2* copies, int n) {
+    constexpr int kPiece = kMoveThreads * kMoveUnroll;
+    const int pieces = (m.page_chunks + kPiece - 1) / kPiece;
+    const long long units = (long long)n * m.n_layers * 2 * pieces;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const int piece = (int)(u % pieces);
+        const long long rest = u / pieces;
+        const bool is_v = (rest & 1) != 0;
+        const int layer = (int)((rest >> 1) % m.n_layers);
+        const int2 c = __ldg(copies + (rest >> 1) / m.n_layers);
+        if (c.x < 0) continue;
+        const long long from = (long long)layer * m.n_pages + c.x, to = (long long)layer * m.n_pages + c.y;
+        uint4* const pool = is_v ? m.v8 : m.k8;
+        const uint4* const s = pool + from * m.page_chunks;
+        uint4* const d = pool + to * m.page_chunks;
+        const int i0 = piece * kPiece + (int)threadIdx.x;
+        uint4 w[kMoveUnroll];
+#pragma unroll
+        for (int i = 0; i < kMoveUnroll; ++i)
+            if (i0 + i * kMoveThreads < m.page_chunks) w[i] = __ldcs(s + i0 + i * kMoveThreads);
+        float* const sc = is_v ? m.v_scale : m.k_scale;
+        float x = 0.f;
+        const bool scaled = piece == 0 && (int)threadIdx.x < m.Hkv;        // (256 heads at most)
+        if (scaled) x = sc[from * m.Hkv + threadIdx.x];
+#pragma unroll
+        for (int i = 0; i < kMoveUnroll; ++i)
+            if (i0 + i * kMoveThreads < m.page_chunks) __stcs(d + i0 + i * kMoveThreads, w[i]);
+        if (scaled) sc[to * m.Hkv + threadIdx.x] = x;
+    }
+}
+
+__global__ void __launch_bounds__(kMoveThreads) fork_apply_kernel(const ForkArgs a, const MoveArgs m) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const PlanHead head = *a.w.head;
+    if (!head.ok) return;
+    // table rows and counts: CTAs take columns of items
+    const int parts = (a.max_pages + kMoveThreads - 1) / kMoveThreads;
+    for (long long u = blockIdx.x; u < (long long)a.n * parts; u += gridDim.x) {
+        const int i = (int)(u / parts), col = (int)(u % parts) * kMoveThreads + (int)threadIdx.x;
+        if (col >= a.max_pages) continue;
+        const int src = __ldg(a.src + i), dst = __ldg(a.dst + i);
+        const int2 at = a.w.items[i], next = a.w.items[i + 1];
+        const int n_new = next.x - at.x, n_copies = next.y - at.y;
+        int32_t* const entry = a.table + (size_t)dst * a.max_pages + col;
+        int first_new;          // first column of the new pages behind those held
+        int fresh_at = at.x;
+        if (src == dst) {
+            const int held = (__ldg(a.want + i) + a.T - 1) / a.T - (n_new - n_copies);      // columns in use before, if it grows
+            if (n_copies > 0) {
+                fresh_at += 1;
+                if (col == __ldg(a.keep + i) / a.T) {
+                    const int old = *entry, page = a.w.fresh[at.x];
+                    atomicSub(a.refs + old, 1);
+                    a.refs[page] = 1;
+                    *entry = page;
+                    continue;
+                }
+            }
+            if (n_new - n_copies <= 0) continue;
+            first_new = held;
+            const int j = col - first_new;
+            if (j >= 0 && j < n_new - n_copies) {
+                const int page = a.w.fresh[fresh_at + j];
+                a.refs[page] = 1;
+                *entry = page;
+            }
+            continue;
+        }
+        first_new = src >= 0 && a.share ? __ldg(a.keep + i) / a.T : 0;
+        int page = -1;
+        if (col < first_new) {
+            page = a.table[(size_t)src * a.max_pages + col];
+            if ((unsigned)page < (unsigned)a.n_pages) atomicAdd(a.refs + page, 1);
+            else { report_status(a.status, DAF_ERR_BOUNDS, 223, page); page = -1; }
+        } else if (col - first_new < n_new) {
+            page = a.w.fresh[fresh_at + col - first_new];
+            a.refs[page] = 1;
+        }
+        *entry = page;
+    }
+    move_pages(m, a.w.copies, head.n_copies);
+}
+
+struct FreeArgs {
+    int n_pages, T, n_seqs, max_pages, n;
+    const int32_t* seqs; const int32_t* keep; int32_t* table; int32_t* refs;
+    DeviceStatus* status;
+};
+__global__ void __launch_bounds__(256) page_free_kernel(const FreeArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int i = blockIdx.x;
+    const int seq = __ldg(a.seqs + i), keep = a.keep != nullptr ? __ldg(a.keep + i) : 0;
+    if ((unsigned)seq >= (unsigned)a.n_seqs || keep < 0) {
+        if (threadIdx.x == 0 && blockIdx.y == 0) report_status(a.status, DAF_ERR_BOUNDS, 230, seq);
+        return;
+    }
+    const int held = (int)(((long long)keep + a.T - 1) / a.T);
+    for (int col = held + (int)(blockIdx.y * 256 + threadIdx.x); col < a.max_pages; col += gridDim.y * 256) {
+        int32_t* const entry = a.table + (size_t)seq * a.max_pages + col;
+        if (*entry < 0) continue;
+        const int page = atomicExch(entry, -1);          // a row named twice gives each page back once
+        if (page < 0) continue;
+        if (page >= a.n_pages) { report_status(a.status, DAF_ERR_BOUNDS, 231, page); continue; }
+        if (atomicSub(a.refs + page, 1) <= 0) {          // the count did not cover this entry
+            atomicAdd(a.refs + page, 1);
+            report_status(a.status, DAF_ERR_BOUNDS, 232, page);
+        }
+    }
+}
+
+struct CompactArgs {
+    int n_pages; long long entries;
+    const int32_t* table; const int32_t* refs; int32_t* table_out; int32_t* refs_out; int32_t* live_out;
+    PlanArrays w;
+    DeviceStatus* status;
+};
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CompactArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tid = threadIdx.x;
+    auto used_bits = [&](int p) {
+        unsigned m = 0;
+#pragma unroll
+        for (int u = 0; u < kPlanRefs; ++u)
+            if (p + u < a.n_pages && a.refs[p + u] > 0) m |= 1u << u;
+        return m;
+    };
+    unsigned long long sum;
+    int live = 0;
+    for (int p0 = 0; p0 < a.n_pages; p0 += kPlanThreads * kPlanRefs) {
+        block_scan((unsigned long long)__popc(used_bits(p0 + tid * kPlanRefs)), &sum);
+        live += (int)sum;
+    }
+    // the r-th page in use at or above `live` goes to the r-th free one below it
+    int holes = 0, movers = 0;
+    for (int p0 = 0; p0 < a.n_pages; p0 += kPlanThreads * kPlanRefs) {
+        const int p = p0 + tid * kPlanRefs;
+        const unsigned used = used_bits(p);
+        const unsigned below = p >= live ? 0u : (live - p >= kPlanRefs ? (1u << kPlanRefs) - 1u : (1u << (live - p)) - 1u);
+        unsigned hole = ~used & below, mover = used & ~below;
+        const unsigned long long at = block_scan(pack2(__popc(hole), __popc(mover)), &sum);
+        int h = holes + (int)(at >> 32), v = movers + (int)(at & 0xFFFFFFFFu);
+        for (; hole != 0; hole &= hole - 1) a.w.copies[h++].y = p + __ffs(hole) - 1;
+        for (; mover != 0; mover &= mover - 1) a.w.copies[v++].x = p + __ffs(mover) - 1;
+        holes += (int)(sum >> 32);
+        movers += (int)(sum & 0xFFFFFFFFu);
+    }
+    __syncthreads();
+    for (int r = tid; r < movers; r += kPlanThreads) {
+        const int2 c = a.w.copies[r];
+        a.w.fresh[c.x] = c.y;
+    }
+    // the counts, here because refs_out may be refs: a moved page's goes to its new place before its old one is cleared
+    __syncthreads();
+    for (int p = tid; p < live; p += kPlanThreads) {
+        const int r = a.refs[p];
+        if (r > 0) a.refs_out[p] = r;
+    }
+    __syncthreads();
+    for (int r = tid; r < movers; r += kPlanThreads) {
+        const int2 c = a.w.copies[r];
+        a.refs_out[c.y] = a.refs[c.x];
+    }
+    __syncthreads();
+    for (int p = live + tid; p < a.n_pages; p += kPlanThreads) a.refs_out[p] = 0;
+    if (tid == 0) {
+        *a.w.head = PlanHead{1, 0, movers, live};
+        if (a.live_out != nullptr) *a.live_out = live;
+    }
+}
+__global__ void __launch_bounds__(kMoveThreads) compact_apply_kernel(const CompactArgs a, const MoveArgs m) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const PlanHead head = *a.w.head;
+    for (long long i = (long long)blockIdx.x * kMoveThreads + threadIdx.x; i < a.entries; i += (long long)gridDim.x * kMoveThreads) {
+        int page = a.table[i];
+        if (page >= a.n_pages) { report_status(a.status, DAF_ERR_BOUNDS, 240, page); page = -1; }
+        else if (page >= head.live) page = a.w.fresh[page];
+        a.table_out[i] = page < 0 ? -1 : page;
+    }
+    move_pages(m, a.w.copies, head.n_copies);
+}
+
+// ------------------------------------------------------------------------------------------------------------------ host side
+constexpr int kPageMaxTokens = 1 << 22;
+
+static int resolve_pages(const daf_page_params* p) {
+    if (p == nullptr) return DAF_ERR_INVALID_ARG;
+    if (p->n_pages <= 0 || p->n_kv_heads <= 0 || p->n_layers <= 0 || p->n_seqs <= 0 || p->max_pages <= 0) return DAF_ERR_INVALID_ARG;
+    if (p->head_dim != 128 || p->n_kv_heads > 256) return DAF_ERR_UNSUPPORTED;
+    if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128) return DAF_ERR_UNSUPPORTED;
+    if ((long long)p->max_pages * p->page_tokens > kPageMaxTokens) return DAF_ERR_UNSUPPORTED;
+    // rows of one layer are numbered in 32 bits; tables, sequences and layers stay in the range of the kernels' products
+    if ((long long)p->n_pages * p->n_kv_heads * p->page_tokens > 0x7FFFFFFFll) return DAF_ERR_UNSUPPORTED;
+    if (p->n_seqs > (1 << 20) || p->n_layers > 4096) return DAF_ERR_UNSUPPORTED;
+    return DAF_OK;
+}
+static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+static size_t plan_bytes(const daf_page_params* p, int n) {
+    return 256 + round256((size_t)p->n_pages * 8) + round256((size_t)p->n_pages * 4) + round256((size_t)p->n_seqs * 4) +
+           round256(((size_t)n + 1) * 8);
+}
+static PlanArrays plan_arrays(const daf_page_params* p, void* workspace) {
+    char* at = reinterpret_cast<char*>(workspace) + kStatusBytes;
+    PlanArrays w;
+    w.head = reinterpret_cast<PlanHead*>(at); at += 256;
+    w.copies = reinterpret_cast<int2*>(at); at += round256((size_t)p->n_pages * 8);
+    w.fresh = reinterpret_cast<int32_t*>(at); at += round256((size_t)p->n_pages * 4);
+    w.marks = reinterpret_cast<int32_t*>(at); at += round256((size_t)p->n_seqs * 4);
+    w.items = reinterpret_cast<int2*>(at);
+    return w;
+}
+static Pool layer_of(const daf_page_params* p, int layer, const void* k8, const void* v8, const float* k_scale, const float* v_scale) {
+    const size_t rows = (size_t)layer * p->n_pages * p->n_kv_heads;
+    Pool q;
+    q.n_pages = p->n_pages; q.T = p->page_tokens; q.Hkv = p->n_kv_heads; q.n_seqs = p->n_seqs; q.max_pages = p->max_pages;
+    q.k8 = reinterpret_cast<uint8_t*>(const_cast<void*>(k8)) + rows * p->page_tokens * 128;
+    q.v8 = reinterpret_cast<uint8_t*>(const_cast<void*>(v8)) + rows * p->page_tokens * 128;
+    q.k_scale = const_cast<float*>(k_scale) + rows;
+    q.v_scale = const_cast<float*>(v_scale) + rows;
+    return q;
+}
+static MoveArgs move_args(const daf_page_params* p, void* k8, void* v8, float* k_scale, float* v_scale) {
+    MoveArgs m;
+    m.k8 = reinterpret_cast<uint4*>(k8); m.v8 = reinterpret_cast<uint4*>(v8); m.k_scale = k_scale; m.v_scale = v_scale;
+    m.n_pages = p->n_pages; m.Hkv = p->n_kv_heads; m.n_layers = p->n_layers; m.page_chunks = p->n_kv_heads * p->page_tokens * 8;
+    return m;
+}
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// The pool's four tensors, all needed; the bytes 16-byte, the scales 4-byte aligned.
+static int check_pool(const void* k8, const void* v8, const float* k_scale, const float* v_scale) {
+    if (!k8 || !v8 || !k_scale || !v_scale) return DAF_ERR_INVALID_ARG;
+    if (!aligned16(k8) || !aligned16(v8) || !aligned4(k_scale) || !aligned4(v_scale)) return DAF_ERR_ALIGNMENT;
+    return DAF_OK;
+}
+static int check_ints(const void* const* ptrs, int count) {
+    for (int i = 0; i < count; ++i)
+        if (!aligned4(ptrs[i])) return DAF_ERR_ALIGNMENT;
+    return DAF_OK;
+}
+static int check_workspace(void* workspace, size_t have, size_t need) {
+    if (workspace == nullptr || have < need) return DAF_ERR_WORKSPACE;
+    return aligned16(workspace) ? DAF_OK : DAF_ERR_ALIGNMENT;
+}
+static int launched(cudaError_t e) {
+    count_launch();
+    if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
+    return check_launch();
+}
+// Pages that `rows` newest (or any consecutive) tokens can touch.
+static int touched_pages(const daf_page_params* p, int rows) {
+    const int t = (rows + p->page_tokens - 2) / p->page_tokens + 1;
+    return t < p->max_pages ? t : p->max_pages;
+}
+// CTAs for an entry's pages: at least one, all of `pages` unless the grid's first dimension would overflow.
+static int page_slots(int n, int pages) {
+    const long long most = 0x7FFFFFFFll / n;
+    return (int)(pages < most ? pages : most);
+}
+
+}  // namespace daf
+
+using namespace daf;
+
+extern "C" {
+
+size_t daf_page_workspace_bytes(const daf_page_params* p, int32_t n, int32_t L_q, int32_t n_q_heads) {
+    if (resolve_pages(p) != DAF_OK || n < 0 || L_q < 0 || n_q_heads < 0) return 0;
+    size_t need = plan_bytes(p, n);
+    if (L_q > 0 && n_q_heads > 0) {
+        if (n_q_heads % p->n_kv_heads != 0 || n_q_heads > 256 || L_q > kPageMaxTokens || n > kPageMaxSeqs) return 0;
+        const size_t attn = page_attn_scratch_bytes(n, L_q, n_q_heads, p->n_kv_heads);
+        if (attn > need) need = attn;
+    }
+    return kStatusBytes + need;
+}
+
+int daf_page_write(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* lens,
+                   const int32_t* row_off, const int32_t* idx, int32_t max_rows, const void* k, const void* v,
+                   const int32_t* table, const int32_t* refs, void* k8, void* v8, float* k_scale, float* v_scale,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = resolve_pages(p)) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes)) return rc;
+    if (layer < 0 || layer >= p->n_layers || n < 0 || max_rows < 0) return DAF_ERR_INVALID_ARG;
+    if (n == 0 || max_rows == 0) return DAF_OK;
+    if (!lens || !row_off || !k || !v || !table) return DAF_ERR_INVALID_ARG;
+    if (int rc = check_pool(k8, v8, k_scale, v_scale)) return rc;
+    if (!aligned16(k) || !aligned16(v)) return DAF_ERR_ALIGNMENT;
+    const void* ints[] = {seqs, lens, row_off, idx, table, refs};
+    if (int rc = check_ints(ints, 6)) return rc;
+    WriteArgs a;
+    a.p = layer_of(p, layer, k8, v8, k_scale, v_scale);
+    a.n = n; a.slots = page_slots(n, idx == nullptr ? touched_pages(p, max_rows) : p->max_pages);
+    a.seqs = seqs; a.lens = lens; a.row_off = row_off; a.idx = idx;
+    a.k = reinterpret_cast<const __nv_bfloat16*>(k); a.v = reinterpret_cast<const __nv_bfloat16*>(v);
+    a.table = table; a.refs = refs; a.status = reinterpret_cast<DeviceStatus*>(workspace);
+    auto* kernel = p->page_tokens == 16 ? page_write_kernel<4> : p->page_tokens == 32 ? page_write_kernel<8>
+                 : p->page_tokens == 64 ? page_write_kernel<16> : page_write_kernel<32>;
+    return launched(launch_kernel(kernel, dim3((unsigned)n * a.slots, p->n_kv_heads, 2), dim3(128), 0, (cudaStream_t)stream, a));
+}
+
+int daf_page_read(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* first,
+                  const int32_t* row_off, int32_t max_rows, const int32_t* table, const void* k8, const void* v8,
+                  const float* k_scale, const float* v_scale, void* k_rows, void* v_rows,
+                  void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = resolve_pages(p)) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes)) return rc;
+    if (layer < 0 || layer >= p->n_layers || n < 0 || max_rows < 0) return DAF_ERR_INVALID_ARG;
+    if (n == 0 || max_rows == 0) return DAF_OK;
+    if (!row_off || !table || !k_rows || !v_rows) return DAF_ERR_INVALID_ARG;
+    if (int rc = check_pool(k8, v8, k_scale, v_scale)) return rc;
+    if (!aligned16(k_rows) || !aligned16(v_rows)) return DAF_ERR_ALIGNMENT;
+    const void* ints[] = {seqs, first, row_off, table};
+    if (int rc = check_ints(ints, 4)) return rc;
+    ReadArgs a;
+    a.p = layer_of(p, layer, k8, v8, k_scale, v_scale);
+    a.n = n; a.slots = page_slots(n, touched_pages(p, max_rows));
+    a.seqs = seqs; a.first = first; a.row_off = row_off; a.table = table;
+    a.k = reinterpret_cast<__nv_bfloat16*>(k_rows); a.v = reinterpret_cast<__nv_bfloat16*>(v_rows);
+    a.status = reinterpret_cast<DeviceStatus*>(workspace);
+    auto* kernel = p->page_tokens == 16 ? page_read_kernel<1> : p->page_tokens == 32 ? page_read_kernel<2>
+                 : p->page_tokens == 64 ? page_read_kernel<4> : page_read_kernel<8>;
+    return launched(launch_kernel(kernel, dim3((unsigned)n * a.slots, p->n_kv_heads, 2), dim3(128), 0, (cudaStream_t)stream, a));
+}
+
+int daf_page_attn(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* lens, int32_t L_q,
+                  int32_t n_q_heads, float softmax_scale, const void* q, const int32_t* table, const void* k8, const void* v8,
+                  const float* k_scale, const float* v_scale, void* out, float* lse,
+                  void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = resolve_pages(p)) return rc;
+    if (layer < 0 || layer >= p->n_layers || n < 0 || L_q < 0 || n_q_heads <= 0) return DAF_ERR_INVALID_ARG;
+    if (n_q_heads % p->n_kv_heads != 0 || n_q_heads > 256 || n > kPageMaxSeqs) return DAF_ERR_UNSUPPORTED;
+    if ((long long)n * L_q > kPageMaxTokens) return DAF_ERR_UNSUPPORTED;
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes)) return rc;
+    if (n == 0 || L_q == 0) return DAF_OK;
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes + page_attn_scratch_bytes(n, L_q, n_q_heads, p->n_kv_heads))) return rc;
+    if (!lens || !q || !table || !out) return DAF_ERR_INVALID_ARG;
+    if (int rc = check_pool(k8, v8, k_scale, v_scale)) return rc;
+    if (!aligned16(q) || !aligned16(out)) return DAF_ERR_ALIGNMENT;
+    const void* ints[] = {seqs, lens, table, lse};
+    if (int rc = check_ints(ints, 4)) return rc;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 0.08838834764831845f;      // 1 / sqrt(128)
+    return launch_page_attn(layer_of(p, layer, k8, v8, k_scale, v_scale), n, seqs, lens, L_q, n_q_heads, scale, q, table, out, lse,
+                            reinterpret_cast<DeviceStatus*>(workspace), reinterpret_cast<char*>(workspace) + kStatusBytes,
+                            (cudaStream_t)stream);
+}
+
+int daf_page_fork(const daf_page_params* p, int32_t n, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                  const int32_t* want, int32_t share, int32_t* table, int32_t* refs, void* k8, void* v8, float* k_scale,
+                  float* v_scale, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = resolve_pages(p)) return rc;
+    if (n < 0) return DAF_ERR_INVALID_ARG;
+    if (n > p->n_seqs) return DAF_ERR_INVALID_ARG;         // some row would be named twice
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes + plan_bytes(p, n))) return rc;
+    if (n == 0) return DAF_OK;
+    if (!src || !dst || !keep || !want || !table || !refs) return DAF_ERR_INVALID_ARG;
+    if (int rc = check_pool(k8, v8, k_scale, v_scale)) return rc;
+    const void* ints[] = {src, dst, keep, want, table, refs};
+    if (int rc = check_ints(ints, 6)) return rc;
+    ForkArgs a;
+    a.n_pages = p->n_pages; a.T = p->page_tokens; a.n_seqs = p->n_seqs; a.max_pages = p->max_pages; a.n = n; a.share = share != 0;
+    a.src = src; a.dst = dst; a.keep = keep; a.want = want; a.table = table; a.refs = refs;
+    a.w = plan_arrays(p, workspace); a.status = reinterpret_cast<DeviceStatus*>(workspace);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (int rc = launched(launch_kernel(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a))) return rc;
+    return launched(launch_kernel(fork_apply_kernel, dim3((unsigned)num_sms() * 8), dim3(kMoveThreads), 0, st, a,
+                                  move_args(p, k8, v8, k_scale, v_scale)));
+}
+
+int daf_page_free(const daf_page_params* p, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t* table, int32_t* refs,
+                  void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = resolve_pages(p)) return rc;
+    if (n < 0) return DAF_ERR_INVALID_ARG;
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes)) return rc;
+    if (n == 0) return DAF_OK;
+    if (!seqs || !table || !refs) return DAF_ERR_INVALID_ARG;
+    const void* ints[] = {seqs, keep, table, refs};
+    if (int rc = check_ints(ints, 4)) return rc;
+    FreeArgs a;
+    a.n_pages = p->n_pages; a.T = p->page_tokens; a.n_seqs = p->n_seqs; a.max_pages = p->max_pages; a.n = n;
+    a.seqs = seqs; a.keep = keep; a.table = table; a.refs = refs; a.status = reinterpret_cast<DeviceStatus*>(workspace);
+    const unsigned parts = (unsigned)((p->max_pages + 255) / 256);
+    return launched(launch_kernel(page_free_kernel, dim3(n, parts < 64 ? parts : 64), dim3(256), 0, (cudaStream_t)stream, a));
+}
+
+int daf_page_compact(const daf_page_params* p, const int32_t* table, const int32_t* refs, int32_t* table_out, int32_t* refs_out,
+                     int32_t* live_out, void* k8, void* v8, float* k_scale, float* v_scale,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = resolve_pages(p)) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes + plan_bytes(p, 0))) return rc;
+    if (!table || !refs || !table_out || !refs_out) return DAF_ERR_INVALID_ARG;
+    if (int rc = check_pool(k8, v8, k_scale, v_scale)) return rc;
+    const void* ints[] = {table, refs, table_out, refs_out, live_out};
+    if (int rc = check_ints(ints, 5)) return rc;
+    CompactArgs a;
+    a.n_pages = p->n_pages; a.entries = (long long)p->n_seqs * p->max_pages;
+    a.table = table; a.refs = refs; a.table_out = table_out; a.refs_out = refs_out; a.live_out = live_out;
+    a.w = plan_arrays(p, workspace); a.status = reinterpret_cast<DeviceStatus*>(workspace);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (int rc = launched(launch_kernel(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a))) return rc;
+    return launched(launch_kernel(compact_apply_kernel, dim3((unsigned)num_sms() * 8), dim3(kMoveThreads), 0, st, a,
+                                  move_args(p, k8, v8, k_scale, v_scale)));
+}
+
+}  // extern "C"
