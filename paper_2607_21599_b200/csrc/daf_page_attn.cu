@@ -8,6 +8,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 #include <vector>
 
 #include "daf_common.cuh"
@@ -20,7 +21,7 @@ struct PageAttnArgs {
     Pool p;
     int n, L_q, Hq, G;
     int rows;              // query rows of a KV head: L_q * G, row r is token r / G, head r % G of the group
-    int row_blocks;        // blocks of them
+    int units;             // tiles of them: what a step of keys of one (sequence, KV head) costs
     float scale_log2;      // softmax scale * log2(e)
     const int32_t* seqs; const int32_t* lens; const int32_t* table;
     const __nv_bfloat16* q; __nv_bfloat16* out; float* lse;
@@ -68,6 +69,9 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uin
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
         : "memory");
 }
+__device__ __forceinline__ void mbar_inval(uint64_t* bar) {
+    asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -94,10 +98,12 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {            // 0xFF w
     return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
 }
 
-// A place on the work axis: segment (b, h, block) and the step in it.
-struct Place { int b, h, block, step, n_steps, seq, len; };
+// A place on the work axis: a segment is (b, h, block), a block `width` tiles (kW, or one less in the last), and each of its steps
+// takes `width` places.
+struct Place { int b, h, block, width, step, n_steps, seq, len; };
 
-// Running sums of the sequences' steps (per head and block) in shared memory: pre[b] = steps of sequences 0 .. b - 1.
+// Running sums of the sequences' steps (of one tile) in shared memory: pre[b] = steps of sequences 0 .. b - 1.  (4096 sequences of 4M
+// tokens: 2^29 steps of 32 keys.)
 __device__ __forceinline__ int seq_len(const PageAttnArgs& a, int b) {
     int len = __ldg(a.lens + b);
     const int seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b;
@@ -107,24 +113,24 @@ __device__ __forceinline__ int seq_len(const PageAttnArgs& a, int b) {
 __device__ __forceinline__ int steps_of(int len, int step) { return max(1, (len + step - 1) / step); }   // (an empty one writes its zeros)
 
 template <int kThreads>
-__device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, long long* pre, long long* warp_sums) {
+__device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, int* pre, int* warp_sums) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    long long run = 0;
+    int run = 0;
     for (int b0 = 0; b0 < a.n; b0 += kThreads) {
         const int b = b0 + tid;
-        long long x = b < a.n ? steps_of(seq_len(a, b), step) : 0;
+        int x = b < a.n ? steps_of(seq_len(a, b), step) : 0;
         if (blockIdx.x == 0 && b < a.n) {
             const int len = __ldg(a.lens + b), seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b;
             if ((unsigned)seq >= (unsigned)a.p.n_seqs || len != seq_len(a, b)) report_status(a.status, DAF_ERR_BOUNDS, 252, b);
         }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+            const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
             if (lane >= o) x += y;
         }
         if (lane == 31) warp_sums[warp] = x;
         __syncthreads();
-        long long before = run, all = 0;
+        int before = run, all = 0;
         for (int w = 0; w < kThreads / 32; ++w) {
             if (w < warp) before += warp_sums[w];
             all += warp_sums[w];
@@ -137,8 +143,25 @@ __device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, long 
     __syncthreads();
 }
 
-__device__ __forceinline__ Place place_at(const PageAttnArgs& a, int step, const long long* pre, long long at) {
-    const long long per = (long long)a.p.Hkv * a.row_blocks;
+template <int kW>
+__device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* pre, Place& x) {
+    x.step = 0;
+    x.width = min(kW, a.units - kW * ++x.block);
+    if (x.width > 0) return;
+    x.block = 0;
+    x.width = min(kW, a.units);
+    if (++x.h < a.p.Hkv) return;
+    x.h = 0;
+    ++x.b;
+    if (x.b >= a.n) return;
+    x.len = seq_len(a, x.b);
+    x.n_steps = pre[x.b + 1] - pre[x.b];
+    x.seq = a.seqs != nullptr ? __ldg(a.seqs + x.b) : x.b;
+}
+// The first step that begins at or behind `at` (which is less than the total).
+template <int kW>
+__device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre, long long at) {
+    const long long per = (long long)a.p.Hkv * a.units;
     int lo = 0, hi = a.n - 1;                    // last b with pre[b] * per <= at
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
@@ -147,26 +170,31 @@ __device__ __forceinline__ Place place_at(const PageAttnArgs& a, int step, const
     Place x;
     x.b = lo;
     x.len = seq_len(a, lo);
-    x.n_steps = (int)(pre[lo + 1] - pre[lo]);
-    const long long rest = at - pre[lo] * per;
-    const int sub = (int)(rest / x.n_steps);
-    x.step = (int)(rest - (long long)sub * x.n_steps);
-    x.h = sub / a.row_blocks;
-    x.block = sub - x.h * a.row_blocks;
     x.seq = a.seqs != nullptr ? __ldg(a.seqs + lo) : lo;
+    x.n_steps = pre[lo + 1] - pre[lo];
+    long long rest = at - pre[lo] * per;
+    const long long head = (long long)x.n_steps * a.units;
+    x.h = (int)(rest / head);
+    rest -= x.h * head;
+    x.block = (int)(rest / ((long long)kW * x.n_steps));
+    x.width = min(kW, a.units - kW * x.block);
+    rest -= (long long)x.block * kW * x.n_steps;
+    x.step = (int)((rest + x.width - 1) / x.width);
+    if (x.step == x.n_steps) next_segment<kW>(a, pre, x);
     return x;
 }
-__device__ __forceinline__ void next_segment(const PageAttnArgs& a, const long long* pre, Place& x) {
-    x.step = 0;
-    if (++x.block < a.row_blocks) return;
-    x.block = 0;
-    if (++x.h < a.p.Hkv) return;
-    x.h = 0;
-    ++x.b;
-    if (x.b >= a.n) return;
-    x.len = seq_len(a, x.b);
-    x.n_steps = (int)(pre[x.b + 1] - pre[x.b]);
-    x.seq = a.seqs != nullptr ? __ldg(a.seqs + x.b) : x.b;
+// Where a place lies on the axis.
+template <int kW>
+__device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* pre, const Place& x) {
+    if (x.b >= a.n) return (long long)pre[a.n] * a.p.Hkv * a.units;
+    return (long long)pre[x.b] * a.p.Hkv * a.units + (long long)x.n_steps * (x.h * a.units + kW * x.block) + (long long)x.step * x.width;
+}
+// The CTA whose stretch holds axis position `at` when `ctas` of them share `total`.
+__device__ __forceinline__ int cta_of(long long at, long long total, long long ctas) {
+    long long c = min(at * ctas / total, ctas - 1);
+    while (c + 1 < ctas && (c + 1) * total / ctas <= at) ++c;
+    while (c > 0 && c * total / ctas > at) --c;
+    return (int)c;
 }
 
 // A row's factor 1 / sum (a row that saw nothing: 0), its log-sum-exp, and the weight of a partial with (maximum, sum) in a merge
@@ -184,8 +212,8 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     extern __shared__ unsigned char decode_smem_raw[];
     unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(decode_smem_raw) + 1023) & ~(uintptr_t)1023);
     DecodeWarp* const warps = reinterpret_cast<DecodeWarp*>(smem + kRingBytes);
-    long long* const pre = reinterpret_cast<long long*>(warps + kDecodeWarps);
-    __shared__ long long warp_sums[kDecodeWarps];
+    int* const pre = reinterpret_cast<int*>(warps + kDecodeWarps);
+    __shared__ int warp_sums[kDecodeWarps];
     __shared__ int abort_flag;
     __shared__ int piece_kind[2 * kDecodeWarps];         // see below
     __shared__ int4 piece_seg[2 * kDecodeWarps];
@@ -206,7 +234,7 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     pdl_wait();
     pdl_launch_dependents();
     sum_steps<kDecodeWarps * 32>(a, kStep, pre, warp_sums);
-    const long long total = pre[a.n] * a.p.Hkv * a.row_blocks;
+    const long long total = (long long)pre[a.n] * a.p.Hkv * a.units;
     // CTAs that take part: no more than give each of its warps a step
     const long long ctas = min((long long)gridDim.x, (total + kDecodeWarps - 1) / kDecodeWarps);
     const long long cta_lo = min((long long)blockIdx.x, ctas) * total / ctas, cta_hi = min((long long)blockIdx.x + 1, ctas) * total / ctas;
@@ -266,13 +294,13 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         __syncwarp();
         ++ahead_at;
         if (++ahead.step == ahead.n_steps) {
-            next_segment(a, pre, ahead);
+            next_segment<1>(a, pre, ahead);
             ids_first = -1;
         }
     };
     Place at = {};
     if (lo < hi) {
-        at = place_at(a, kStep, pre, lo);
+        at = place_at<1>(a, pre, lo);
         ahead = at;
         for (int s = 0; s < kDepth && ahead_at < hi; ++s) issue(s);
     }
@@ -503,7 +531,7 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
             break;
         }
-        if (x < hi) next_segment(a, pre, at);
+        if (x < hi) next_segment<1>(a, pre, at);
     }
     if (!ok) {      // loads in flight get a bounded chance to land before the CTA retires
         for (int s = 0; s < kDepth; ++s)
@@ -581,65 +609,665 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (threadIdx.x == 0) {
         ChainEntry e = {-1, 0, 0, 0};
         if (chain_kind != 0) {
-            const long long seg_end = (pre[chain_seg.x] * Hkv + 0) * a.row_blocks + ((long long)chain_seg.y * a.row_blocks + chain_seg.z + 1) * chain_seg.w;
-            // the CTA whose stretch holds step seg_end - 1
-            long long c = min(((seg_end - 1) * ctas) / total, ctas - 1);
-            while (c + 1 < ctas && (c + 1) * total / ctas <= seg_end - 1) ++c;
-            while (c > 0 && c * total / ctas > seg_end - 1) --c;
-            e = ChainEntry{(int)c, chain_seg.x, chain_seg.y, chain_seg.z};
+            const long long seg_end = (long long)pre[chain_seg.x] * Hkv * a.units + ((long long)chain_seg.y * a.units + chain_seg.z + 1) * chain_seg.w;
+            e = ChainEntry{cta_of(seg_end - 1, total, ctas), chain_seg.x, chain_seg.y, chain_seg.z};
         }
         a.chains[blockIdx.x] = e;
     }
 }
 
-// Merge of the segments that lie in several CTAs: one CTA of four warps per (CTA that begins such a segment, row).
-__global__ void __launch_bounds__(128) page_merge_kernel(const PageAttnArgs a, int block_rows) {
-    __shared__ float4 acc_s[4][32];
-    __shared__ float sum_s[4], mx_s[4];
+// ---------------------------------------------------------------------------------------------- many rows: tensor memory
+// More than 16 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
+// of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 15 warps:
+//   14     asks for the bytes of K and V (TMA, kStages steps ahead) and their scales;
+//   10-13  widen them to fp16, exactly, into the two-slot rings that the products read (128-byte swizzle);
+//   8, 9   issue a tile group's products: S = Q K^T into one of two halves, O += P V with P from tensor memory;
+//   0-3, 4-7  a tile group's softmax, a row per thread, and its epilogue.
+// A block of two tiles shares every widened K and V (the bytes pass through shared memory once for both, and shared memory is what
+// bounds this loop: per step 64 KB of operand reads for each tile, 32 KB written and 32 KB of bytes in and out).  A block of one tile
+// gives its even steps to one group and its odd ones to the other, and the two halves of the result are merged in shared memory.
+// Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
+constexpr int kQStep = 64;
+constexpr int kQStages = 4;
+constexpr int kQRows = 256;
+constexpr int kQThreads = 480;
+constexpr int kQTile = 128 * kD * 2;                  // 32 KB: 128 rows of Q, two 64-column halves
+constexpr int kQHalf = kQTile / 2;
+constexpr int kQSlot = kQStep * kD * 2;               // 16 KB: K or V of a step, widened, two 64-column halves
+constexpr int kQSlotHalf = kQSlot / 2;
+constexpr int kQStage = 2 * kQStep * kD;              // 16 KB: the bytes of K and V of a step
+constexpr float kLazy = 2.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
+
+struct QuestionSmem {
+    uint64_t st_full[kQStages], st_empty[kQStages];
+    uint64_t k_full[2], v_full[2];
+    uint64_t q_full[2];
+    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];      // [group][half]
+    uint64_t c_full[8];
+    float4 chunk[8][4];             // of eight steps and each 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, any page missing
+    float scales[kQStages][8];      // K's, then V's, of the step's chunks of 16 keys, as they arrive
+    float2 ml[128];                 // the second group's row maxima and sums (blocks of one tile)
+    uint32_t tmem_base;
+    int abort_flag;
+    int used;                       // the barriers have been initialised
+    int poison;                     // a NaN was taken out of a value that some rows must not see
+    // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
+    Place at;
+    int step1, n_t, first_limit, last_limit;      // steps at.step .. step1 - 1, of which the first n_t have keys that some row sees
+    long long x, hi, total, ctas;
+    ChainEntry chain;
+};
+constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQTile + 4 * (size_t)kQSlot + (size_t)kQStages * kQStage + sizeof(QuestionSmem);
+
+__host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
+    return (1u << 4) | (b_mn_major << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);      // fp16 x fp16 -> fp32
+}
+
+// 32 lanes x 16 consecutive 32-bit columns
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+
+// One softmax step of one row over 64 keys: P over the first half of the logits' columns, running maximum and sum; returns the factor
+// for the row of O (1 unless the maximum grew by more than kLazy).  c: the row's factor for its logits.
+__device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4* chunk, int key0, int limit, float c, float& m, float& l) {
+    uint32_t sr[2][32];
+    tmem_ld32(s_addr, sr[0]);
+    tc_wait_ld();
+    tmem_ld32(s_addr + 32u, sr[1]);
+    const bool masked = key0 + kQStep - 1 > limit || chunk[0].w != 0.f;
+    float top = -INFINITY;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (half == 1) tc_wait_ld();
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (key0 + 32 * half + j > limit || chunk[2 * half + j / 16].x < 0.f) sr[half][j] = 0xFF800000u;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float2 k2 = *reinterpret_cast<const float2*>(chunk + 2 * half + i);
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                mx[0] = fmax3(mx[0], __uint_as_float(sr[half][16 * i + j]), __uint_as_float(sr[half][16 * i + j + 1]));
+                mx[1] = fmax3(mx[1], __uint_as_float(sr[half][16 * i + j + 2]), __uint_as_float(sr[half][16 * i + j + 3]));
+            }
+            top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), c * fabsf(k2.x), k2.y));
+        }
+    }
+    float now = fmaxf(m, top);
+    if (m != -INFINITY && now - m <= kLazy) now = m;
+    const float used = now == -INFINITY ? 0.f : now - kPExp;
+    const float alpha = m == -INFINITY ? 1.f : fast_exp2(m - now);
+    float sum = 0.f;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t pr[16];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 k4 = chunk[2 * half + i];
+            const float f = c * fabsf(k4.x), d = k4.y - used;
+            const uint64_t f2 = pack_f32x2(f, f), d2 = pack_f32x2(d, d);
+            uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const uint64_t x = ffma2(pack_f32x2(__uint_as_float(sr[half][16 * i + j]), __uint_as_float(sr[half][16 * i + j + 1])), f2, d2);
+                const float p0 = fast_exp2(f32x2_lo(x)), p1 = fast_exp2(f32x2_hi(x));
+                acc[(j >> 1) & 1] = fadd2(acc[(j >> 1) & 1], pack_f32x2(p0, p1));
+                pr[8 * i + (j >> 1)] = pack_f16(p0, p1);
+            }
+            const uint64_t both = fadd2(acc[0], acc[1]);
+            sum = fmaf(f32x2_lo(both) + f32x2_hi(both), k4.z, sum);
+        }
+        tmem_st16(s_addr + (uint32_t)(16 * half), pr);
+    }
+    l = l * alpha + sum;
+    m = now;
+    return alpha;
+}
+
+__global__ void __launch_bounds__(kQThreads, 1)
+page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
+    extern __shared__ unsigned char question_smem_raw[];
+    unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(question_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* const q_smem = smem;                          // two tiles
+    unsigned char* const k_smem = q_smem + 2 * kQTile;           // two slots
+    unsigned char* const v_smem = k_smem + 2 * kQSlot;
+    unsigned char* const stage_smem = v_smem + 2 * kQSlot;
+    QuestionSmem* const sm = reinterpret_cast<QuestionSmem*>(stage_smem + kQStages * kQStage);
+    int* const pre = reinterpret_cast<int*>(sm + 1);
+    __shared__ int warp_sums[kQThreads / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* const abort = &sm->abort_flag;
+
+    if (warp == 8) {
+        tmem_alloc(&sm->tmem_base, 512);
+        tmem_relinquish();
+    }
+    if (threadIdx.x == 0) {
+        sm->abort_flag = 0;
+        tma_prefetch_desc(&tmap_k);
+        tma_prefetch_desc(&tmap_v);
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+    sum_steps<kQThreads>(a, kQStep, pre, warp_sums);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm->tmem_base;
+    const int T = a.p.T, Hkv = a.p.Hkv;
+    if (threadIdx.x == 0) {
+        const long long total = (long long)pre[a.n] * Hkv * a.units;
+        const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than four steps of a tile each
+        const long long c_lo = min((long long)blockIdx.x, ctas) * total / ctas, c_hi = min((long long)blockIdx.x + 1, ctas) * total / ctas;
+        // both ends move up to the next step's begin
+        Place at = {};
+        sm->x = sm->hi = total;
+        if (c_hi < total) { at = place_at<2>(a, pre, c_hi); sm->hi = axis_at<2>(a, pre, at); }
+        if (c_lo < total) { at = place_at<2>(a, pre, c_lo); sm->x = axis_at<2>(a, pre, at); }
+        sm->at = at;
+        sm->step1 = 0;
+        sm->used = 0;
+        sm->total = total;
+        sm->ctas = ctas;
+        sm->chain = ChainEntry{-1, 0, 0, 0};
+    }
+    for (;;) {
+        // ---- one segment, or this CTA's stretch of it
+        if (threadIdx.x == 0) {
+            if (sm->step1 > 0) {            // behind the piece before
+                sm->x += (long long)(sm->step1 - sm->at.step) * sm->at.width;
+                sm->at.step = sm->step1;
+                if (sm->at.step == sm->at.n_steps) next_segment<2>(a, pre, sm->at);
+            }
+            const Place at = sm->at;
+            sm->step1 = 0;
+            if (sm->x < sm->hi) {
+                const int step1 = (int)min((long long)at.n_steps, at.step + (sm->hi - sm->x) / at.width);
+                const int row0 = at.block * kQRows, last_row = min(a.rows, row0 + kQRows) - 1;
+                sm->step1 = step1;
+                sm->first_limit = at.len - a.L_q + row0 / a.G;
+                sm->last_limit = at.len - a.L_q + last_row / a.G;
+                sm->n_t = max(0, min(step1, (sm->last_limit + kQStep) / kQStep) - at.step);       // (a negative limit: none)
+                if (at.step == 0 && step1 < at.n_steps) {
+                    Place end = at;
+                    end.step = at.n_steps - 1;
+                    sm->chain = ChainEntry{cta_of(axis_at<2>(a, pre, end), sm->total, sm->ctas), at.b, at.h, at.block};
+                }
+            }
+            if (sm->used)                   // the barriers start anew with every piece: nothing is under way on them
+                for (uint64_t* bar = sm->st_full; bar != sm->c_full + 8; ++bar) mbar_inval(bar);
+            sm->used = 1;
+            for (int i = 0; i < kQStages; ++i) { mbar_init(&sm->st_full[i], 1 + 8); mbar_init(&sm->st_empty[i], 4); }
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(&sm->k_full[i], 4); mbar_init(&sm->v_full[i], 4); mbar_init(&sm->q_full[i], 4);
+                for (int j = 0; j < 2; ++j) { mbar_init(&sm->s_full[i][j], 1); mbar_init(&sm->p_full[i][j], 4); mbar_init(&sm->pv_done[i][j], 1); }
+            }
+            for (int i = 0; i < 8; ++i) mbar_init(&sm->c_full[i], 1);
+            sm->poison = 0;
+            mbar_fence_init();
+        }
+        __syncthreads();
+        if (sm->step1 == 0) break;
+        bool ok = true;
+        const int n_t = sm->n_t, step0 = sm->at.step;
+        const bool pair = sm->at.width == 2;
+        if (warp == 14) {
+            // -------------------------------------------------------------------------------------------- bytes and scales
+            const Place at = sm->at;
+            int ids = -1, ids_first = -1;
+            const int box = min(T, kQStep), pages = kQStep / box;      // copies of a step
+            for (int t = 0; t < n_t && ok; ++t) {
+                const int slot = t % kQStages;
+                if (t >= kQStages) {
+                    ok = mbar_wait(&sm->st_empty[slot], (uint32_t)((t / kQStages - 1) & 1), abort, a.status, 260);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                }
+                const int key0 = (step0 + t) * kQStep, page0 = key0 / T;
+                if (ids_first < 0 || page0 + pages > ids_first + 32) {
+                    ids_first = page0;
+                    const int j = page0 + lane;
+                    const bool needed = j < a.p.max_pages && (long long)j * T < at.len;
+                    ids = needed ? __ldg(a.table + (size_t)at.seq * a.p.max_pages + j) : -1;
+                    if ((unsigned)ids >= (unsigned)a.p.n_pages) {
+                        if (needed && at.h == 0 && at.block == 0) report_status(a.status, DAF_ERR_BOUNDS, 261, ids);
+                        ids = -1;
+                    }
+                }
+                // lanes 0-3: K's scales of the chunks of 16 keys, 4-7: V's
+                const int id = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + ((lane & 3) * 16) / box * (box < kQStep ? 1 : 0));
+                if (lane < 8) {
+                    float* const dst = &sm->scales[slot][lane];
+                    if (id >= 0) {
+                        const float* const src = (lane < 4 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + at.h;
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sm->st_full[slot])) : "memory");
+                    } else {
+                        *dst = -1.f;
+                        mbar_arrive(&sm->st_full[slot]);
+                    }
+                }
+                const int mine = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (lane < pages ? lane : 0));
+                const unsigned there = __ballot_sync(0xFFFFFFFFu, lane < pages && mine >= 0);
+                if (lane == 0) mbar_arrive_expect_tx(&sm->st_full[slot], (uint32_t)(__popc(there) * 2 * box * kD));
+                __syncwarp();
+                if ((there >> lane) & 1u) {
+                    unsigned char* const dst = stage_smem + slot * kQStage + lane * box * kD;
+                    const int row = (mine * Hkv + at.h) * T + key0 % T;       // (key0 % T is 0 unless a page holds several steps)
+                    tma_load_2d(dst, &tmap_k, &sm->st_full[slot], 0, row);
+                    tma_load_2d(dst + kQStep * kD, &tmap_v, &sm->st_full[slot], 0, row);
+                }
+                __syncwarp();
+            }
+            if (!ok)       // loads in flight get a bounded chance to land before the CTA retires
+                for (int i = 0; i < kQStages && lane == 0; ++i)
+                    for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[i], 0) && !mbar_try_wait(&sm->st_full[i], 1); ++k) {}
+        } else if (warp >= 10) {
+            // --------------------------------------------------------------------------------------------------- widening
+            // A lane takes 16 bytes of a row at a time.  Eight lanes take four neighbouring pieces of each of two rows r and r ^ 5:
+            // with the swizzle of either side their reads and their writes all fall into different banks.
+            const int cw = warp - 10;
+            const int first_limit = sm->first_limit, len = sm->at.len;
+            const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
+            for (int t = 0; t < n_t && ok; ++t) {
+                const int slot = t % kQStages, b = t & 1;
+                ok = mbar_wait(&sm->st_full[slot], (uint32_t)((t / kQStages) & 1), abort, a.status, 262);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                const int key0 = (step0 + t) * kQStep;
+                const float* const sc = sm->scales[slot];
+                const bool missing = sc[0] < 0.f || sc[1] < 0.f || sc[2] < 0.f || sc[3] < 0.f;
+                const bool odd = key0 + kQStep - 1 > first_limit || missing;
+                // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
+                const int u = pair ? t - 2 : (t >> 1) - 1;
+                for (int kv = 0; kv < 2 && ok; ++kv) {
+                    const unsigned char* const src = stage_smem + slot * kQStage + kv * kQStep * kD;
+                    unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot;
+                    uint4 w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
+                        const int r = 16 * cw + 8 * (i >> 1) + r8, c = 4 * (i & 1) + piece;
+                        w[i] = *reinterpret_cast<const uint4*>(src + r * kD + ((c ^ r8) << 4));
+                    }
+                    if (kv == 1 && odd) {
+                        // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in a key that
+                        // only some rows see is taken out, and put into the rows that see it at the end.
+                        bool found = false;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key0 + 16 * cw + 8 * (i >> 1) + r8;
+                            if (key >= len || sc[cw] < 0.f) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                            else if (key > first_limit) {
+                                const uint4 nan = make_uint4(nan_bytes(w[i].x), nan_bytes(w[i].y), nan_bytes(w[i].z), nan_bytes(w[i].w));
+                                found |= (nan.x | nan.y | nan.z | nan.w) != 0u;
+                                w[i].x &= ~nan.x; w[i].y &= ~nan.y; w[i].z &= ~nan.z; w[i].w &= ~nan.w;
+                            }
+                        }
+                        if (found) sm->poison = 1;
+                    }
+                    uint32_t h[4][8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        h[i][0] = widen2(w[i].x); h[i][1] = widen2(w[i].x >> 16); h[i][2] = widen2(w[i].y); h[i][3] = widen2(w[i].y >> 16);
+                        h[i][4] = widen2(w[i].z); h[i][5] = widen2(w[i].z >> 16); h[i][6] = widen2(w[i].w); h[i][7] = widen2(w[i].w >> 16);
+                    }
+                    if (kv == 1) {       // what is left of V's scale beside a power of two (nothing, as daf_page_write leaves them)
+                        const float vs = sc[4 + cw];
+                        const float vm = vs > 0.f ? __int_as_float((__float_as_int(vs) & 0x7FFFFF) | 0x3F800000) : 1.f;
+                        if (vm != 1.f) {
+                            const __half2 f = __float2half2_rn(vm);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const __half2 y = __hmul2(*reinterpret_cast<__half2*>(&h[i][j]), f);
+                                    h[i][j] = *reinterpret_cast<const uint32_t*>(&y);
+                                }
+                        }
+                    }
+                    if (t >= 2) {
+                        uint64_t (*const freed)[2] = kv == 0 ? sm->s_full : sm->pv_done;
+                        if (pair) {
+                            ok = mbar_wait(&freed[0][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 263);
+                            if (ok) ok = mbar_wait(&freed[1][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 264);
+                        } else {
+                            ok = mbar_wait(&freed[b][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 265);
+                        }
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 16 * cw + 8 * (i >> 1) + r8;
+                        unsigned char* const row = dst + (i & 1) * kQSlotHalf + r * 128;
+                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(h[i][0], h[i][1], h[i][2], h[i][3]);
+                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(h[i][4], h[i][5], h[i][6], h[i][7]);
+                    }
+                    if (kv == 0 && cw == 0 && lane < 4) {
+                        const float vs = sc[4 + lane];
+                        const int e = vs > 0.f ? max((__float_as_int(vs) >> 23) - 127, -126) : 0;
+                        sm->chunk[t & 7][lane] = make_float4(sc[lane], (float)e, __int_as_float((127 - e) << 23), missing ? 1.f : 0.f);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (kv == 0 && cw == 0) mbar_arrive(&sm->c_full[t & 7]);
+                        mbar_arrive(kv == 0 ? &sm->k_full[b] : &sm->v_full[b]);
+                        if (kv == 1) mbar_arrive(&sm->st_empty[slot]);
+                    }
+                }
+            }
+        } else if (warp >= 8) {
+            // --------------------------------------------------------------------------------------------------- products
+            const int g = warp - 8;
+            const int n_u = pair ? n_t : (n_t - g + 1) / 2;          // steps of this group
+            if (n_u > 0) {
+                constexpr uint32_t idesc_qk = make_idesc_f16(128, kQStep, 0), idesc_pv = make_idesc_f16(128, kD, 1);
+                const uint32_t qa = smem_u32(q_smem + (pair ? g : 0) * kQTile);
+                const uint32_t s_col = tmem + (uint32_t)(g * 256), o_col = s_col + 128u;
+                uint64_t qd[8], kd[2][8], vd[2][4];
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) {
+                    qd[kk] = make_smem_desc(qa + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQHalf), 16, 1024);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        kd[b][kk] = make_smem_desc(smem_u32(k_smem + (pair ? b : g) * kQSlot) + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQSlotHalf), 16, 1024);
+                }
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        vd[b][kk] = make_smem_desc(smem_u32(v_smem + (pair ? b : g) * kQSlot) + (uint32_t)kk * 2048u, kQSlotHalf, 1024);
+                auto slot_of = [&](int u) { return pair ? u & 1 : g; };
+                auto use_of = [&](int u) { return pair ? u >> 1 : u; };       // how often the slot was filled before
+                auto issue_qk = [&](int b) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        tc_mma_ss(s_col + (uint32_t)(b * kQStep), qd[kk], b ? kd[1][kk] : kd[0][kk], idesc_qk, kk > 0 ? 1u : 0u);
+                    tc_commit(&sm->s_full[g][b]);
+                };
+                ok = mbar_wait(&sm->q_full[pair ? g : 0], 0, abort, a.status, 266);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                for (int u = 0; u < 2 && u < n_u && ok; ++u) {
+                    ok = mbar_wait(&sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 267);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) issue_qk(u);
+                    __syncwarp();
+                }
+                auto step = [&](auto half, int u) -> bool {
+                    constexpr int b = decltype(half)::value;
+                    bool there = mbar_wait(&sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 268);
+                    if (there) there = mbar_wait(&sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, a.status, 269);
+                    if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            tc_mma_ts(o_col, s_col + (uint32_t)(b * kQStep + kk * 8), vd[b][kk], idesc_pv, (u == 0 && kk == 0) ? 0u : 1u);
+                        tc_commit(&sm->pv_done[g][b]);
+                    }
+                    __syncwarp();
+                    if (u + 2 < n_u) {
+                        there = mbar_wait(&sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, a.status, 270);
+                        if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                        tc_fence_after();
+                        if (elect_one()) issue_qk(b);
+                        __syncwarp();
+                    }
+                    return true;
+                };
+                for (int u = 0; u < n_u && ok; u += 2) {
+                    ok = step(std::integral_constant<int, 0>{}, u);
+                    if (ok && u + 1 < n_u) ok = step(std::integral_constant<int, 1>{}, u + 1);
+                }
+            }
+        } else {
+            // ------------------------------------------------------------------------------------- softmax, a row per thread
+            const int g = warp >> 2, rt = threadIdx.x & 127;
+            const int row = sm->at.block * kQRows + (pair ? g * 128 : 0) + rt;
+            const bool valid = row < a.rows;
+            const int limit = valid ? sm->at.len - a.L_q + row / a.G : sm->last_limit;
+            const int n_u = pair ? n_t : (n_t - g + 1) / 2;
+            float c;
+            {
+                // this thread's row of Q, scaled to a largest magnitude of 2^14 .. 2^15, as fp16 in the layout of a tiled copy
+                uint32_t big = 0;
+                const uint4* const src = reinterpret_cast<const uint4*>(a.q + (((size_t)sm->at.b * a.L_q + row / a.G) * a.Hq + sm->at.h * a.G + row % a.G) * kD);
+#pragma unroll
+                for (int i = 0; i < 16; i += 8) {
+                    uint4 w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = valid ? __ldg(src + i + j) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const uint32_t v = (j & 3) == 0 ? w[j >> 2].x : (j & 3) == 1 ? w[j >> 2].y : (j & 3) == 2 ? w[j >> 2].z : w[j >> 2].w;
+                        const uint32_t b0 = v & 0x7FFFu, b1 = (v >> 16) & 0x7FFFu;
+                        big = max(big, max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u));
+                    }
+                }
+                const int e = max((int)(big >> 7) - 127, -100);
+                const float up = __int_as_float((14 - e + 127) << 23);
+                c = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
+                if (pair || g == 0) {
+                    unsigned char* const dst = q_smem + g * kQTile + rt * 128;
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {       // (read again: it is in L1, and the registers are needed elsewhere)
+                        const uint4 w = valid ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+                        uint4 y;
+                        y.x = pack_f16(__uint_as_float(w.x << 16) * up, __uint_as_float(w.x & 0xFFFF0000u) * up);
+                        y.y = pack_f16(__uint_as_float(w.y << 16) * up, __uint_as_float(w.y & 0xFFFF0000u) * up);
+                        y.z = pack_f16(__uint_as_float(w.z << 16) * up, __uint_as_float(w.z & 0xFFFF0000u) * up);
+                        y.w = pack_f16(__uint_as_float(w.w << 16) * up, __uint_as_float(w.w & 0xFFFF0000u) * up);
+                        *reinterpret_cast<uint4*>(dst + (i >> 3) * kQHalf + (((i & 7) ^ (rt & 7)) << 4)) = y;
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm->q_full[g]);
+                }
+            }
+            const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+            const uint32_t s_addr = tmem + (uint32_t)(g * 256) + lane_addr, o_addr = s_addr + 128u;
+            float m = -INFINITY, l = 0.f;
+            for (int u = 0; u < n_u; ++u) {
+                const int t = pair ? u : 2 * u + g, b = u & 1;
+                ok = mbar_wait(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, a.status, 271);
+                if (ok) ok = mbar_wait(&sm->s_full[g][b], (uint32_t)((u >> 1) & 1), abort, a.status, 272);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t & 7], (step0 + t) * kQStep, limit, c, m, l);
+                if (u > 0 && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
+                    // the product before must have completed before O is touched
+                    ok = mbar_wait(&sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, a.status, 273);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t r[32];
+                        tmem_ld32(o_addr + (uint32_t)(32 * i), r);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
+                        tmem_st32(o_addr + (uint32_t)(32 * i), r);
+                    }
+                }
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm->p_full[g][b]);
+            }
+            // both last products (each on a barrier of its own)
+            for (int u = max(0, n_u - 2); u < n_u && ok; ++u) {
+                ok = mbar_wait(&sm->pv_done[g][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 274);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+            }
+            tc_fence_after();
+            // ---- epilogue.  A block of one tile: the second group hands its rows to the first through the rings, which are idle now.
+            float w0 = 1.f, w1 = 0.f;
+            float* const other = reinterpret_cast<float*>(k_smem) + rt * kD;
+            static_assert(4 * kQSlot >= 128 * kD * (int)sizeof(float), "the rings hold a tile of fp32 rows");
+            if (!pair) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (g == 1 && ok) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t r[32];
+                        if (n_u > 0) {
+                            tmem_ld32(o_addr + (uint32_t)(32 * i), r);
+                            tc_wait_ld();
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4)
+                            *reinterpret_cast<float4*>(other + (((8 * i + j / 4) ^ lane) << 2)) =
+                                n_u > 0 ? make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]))
+                                        : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                    sm->ml[rt] = make_float2(m, l);
+                }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (g == 0) {
+                    const float2 ml = sm->ml[rt];
+                    const float mx = fmaxf(m, ml.x);
+                    w0 = partial_weight(make_float2(m, l), mx);
+                    w1 = partial_weight(ml, mx);
+                    m = mx;
+                    l = w0 * l + w1 * ml.y;
+                }
+            }
+            if (ok && (pair || g == 0)) {      // (whole warps: the reads of tensor memory are theirs)
+                const Place at = sm->at;
+                const int tok = row / a.G, head = at.h * a.G + row % a.G;
+                const bool begins = step0 == 0, ends = sm->step1 == at.n_steps;
+                const float inv = row_inverse(l);
+                const size_t set = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t r[16];
+                    float o[16];
+                    if (n_u > 0) {
+                        tmem_ld16(o_addr + (uint32_t)(16 * i), r);
+                        tc_wait_ld();
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = n_u > 0 ? __uint_as_float(r[j]) : 0.f;
+                    if (!pair) {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 y = *reinterpret_cast<const float4*>(other + (((4 * i + j / 4) ^ lane) << 2));
+                            o[j] = w0 * o[j] + w1 * y.x; o[j + 1] = w0 * o[j + 1] + w1 * y.y;
+                            o[j + 2] = w0 * o[j + 2] + w1 * y.z; o[j + 3] = w0 * o[j + 3] + w1 * y.w;
+                        }
+                    }
+                    if (!valid) continue;
+                    if (sm->poison != 0) {
+                        // values that were NaN, in keys that this row sees and the block's first does not
+                        const int from = max(sm->first_limit + 1, step0 * kQStep), to = min(min(limit, at.len - 1), (step0 + n_t) * kQStep - 1);
+                        for (int key = from; key <= to; ++key) {
+                            const int id = __ldg(a.table + (size_t)at.seq * a.p.max_pages + key / T);
+                            if ((unsigned)id >= (unsigned)a.p.n_pages) continue;
+                            const uint8_t* const v = a.p.v8 + (((size_t)id * Hkv + at.h) * T + key % T) * kD + 16 * i;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                if ((__ldg(v + j) & 0x7F) == 0x7F) o[j] = __int_as_float(0x7FC00000);
+                        }
+                    }
+                    if (begins && ends) {
+                        uint4* const dst = reinterpret_cast<uint4*>(a.out + (((size_t)at.b * a.L_q + tok) * a.Hq + head) * kD) + 2 * i;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            dst[j] = make_uint4(pack_bf16(o[8 * j] * inv, o[8 * j + 1] * inv), pack_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
+                                                pack_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv), pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
+                    } else {
+                        float4* const dst = reinterpret_cast<float4*>(a.part_o + set * kD) + 4 * i;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                    }
+                }
+                if (!valid) {
+                } else if (begins && ends) {
+                    if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + head) * a.L_q + tok] = row_lse(m, l);
+                } else {
+                    a.part_ml[set] = make_float2(m, l);
+                }
+            }
+        }
+        tc_fence_before();
+        __syncthreads();       // the barriers, rings and tensor memory are free
+        tc_fence_after();
+        if (sm->abort_flag != 0) break;
+    }
+    if (threadIdx.x == 0) a.chains[blockIdx.x] = sm->abort_flag == 0 ? sm->chain : ChainEntry{-1, 0, 0, 0};
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Merge of the segments that lie in several CTAs: kWarps warps per row of a segment that CTA blockIdx.x begins.  Few rows with many
+// partials (one answer over a long context: 37) are bound by the trips to L2, so that several warps share a row's partials; of many
+// rows with few each takes one warp.
+template <int kWarps>
+__global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, int block_rows) {
+    constexpr int kRows = 8 / kWarps;
+    __shared__ float4 acc_s[8][32];
+    __shared__ float sum_s[8];
     pdl_wait();
     pdl_launch_dependents();
     const ChainEntry e = a.chains[blockIdx.x];
-    const int first = blockIdx.x, last = e.last_cta, r = blockIdx.y;
-    if (last < 0) return;
+    if (e.last_cta < 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
+    const int first = blockIdx.x, r = blockIdx.y * kRows + warp / kWarps;
     const int row = e.block * block_rows + r;
-    if (row >= a.rows) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool there = r < block_rows && row < a.rows;
     // partial i of the row: the first CTA's second set, then the following CTAs' first sets
     auto set_of = [&](int i) { return i == 0 ? (size_t)first * 2 + 1 : (size_t)(first + i) * 2; };
-    const int n = last - first + 1;
+    const int n = there ? e.last_cta - first + 1 : 0;
     float mx = -INFINITY;
-    for (int i = threadIdx.x; i < n; i += 128) mx = fmaxf(mx, __ldcg(&a.part_ml[set_of(i) * block_rows + r].x));
+    for (int i = lane; i < n; i += 32) mx = fmaxf(mx, __ldcg(&a.part_ml[set_of(i) * block_rows + r].x));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
-    if (lane == 0) mx_s[warp] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(mx_s[0], mx_s[1]), fmaxf(mx_s[2], mx_s[3]));
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
-    for (int i = warp; i < n; i += 4) {
+    for (int i = part; i < n; i += kWarps) {
         const float2 ml = __ldcg(&a.part_ml[set_of(i) * block_rows + r]);
         const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + (set_of(i) * block_rows + r) * kD) + lane);
         const float w = partial_weight(ml, mx);
         sum += w * ml.y;
         acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
     }
-    acc_s[warp][lane] = acc;
-    if (lane == 0) sum_s[warp] = sum;
-    __syncthreads();
-    if (warp != 0) return;
-    sum = (sum_s[0] + sum_s[1]) + (sum_s[2] + sum_s[3]);
+    if (kWarps > 1) {
+        acc_s[warp][lane] = acc;
+        if (lane == 0) sum_s[warp] = sum;
+        __syncthreads();
+        if (part != 0) return;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) {
-        const float4 v = acc_s[w][lane];
-        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        for (int w = 1; w < kWarps; ++w) {
+            const float4 v = acc_s[warp + w][lane];
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+            sum += sum_s[warp + w];
+        }
     }
+    if (!there) return;
     const int tok = row / a.G, head = e.h * a.G + row % a.G;
     const float inv = row_inverse(sum);
     reinterpret_cast<uint2*>(a.out + (((size_t)e.b * a.L_q + tok) * a.Hq + head) * kD)[lane] =
         make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    if (a.lse != nullptr && lane == 0)
-        a.lse[((size_t)e.b * a.Hq + head) * a.L_q + tok] = row_lse(mx, sum);
+    if (a.lse != nullptr && lane == 0) a.lse[((size_t)e.b * a.Hq + head) * a.L_q + tok] = row_lse(mx, sum);
 }
 
 // ------------------------------------------------------------------------------------------------------------------ host side
@@ -681,15 +1309,18 @@ static int make_pool_map(CUtensorMap* m, const void* base, long long rows, int b
 }
 
 static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
-// Partial rows: two sets a CTA, and one a warp for the pieces parked on the way.
-static size_t decode_sets(int ctas) { return (size_t)ctas * (2 + kDecodeWarps); }
-static size_t decode_smem(int n) { return kDecodeSmem + ((size_t)n + 1) * sizeof(long long); }
+// Partial rows: two sets a CTA, and for the kernel of few rows one a warp for the pieces parked on the way.
+static bool few_rows(int rows) { return rows <= kBlockRows; }
+static size_t partial_rows(int ctas, bool few) {
+    return few ? (size_t)ctas * (2 + kDecodeWarps) * kBlockRows : (size_t)ctas * 2 * kQRows;
+}
+static size_t prefix_bytes(int n) { return ((size_t)n + 1) * sizeof(int); }
 
 size_t page_attn_scratch_bytes(int n, int L_q, int Hq, int Hkv) {
-    (void)n; (void)L_q; (void)Hq; (void)Hkv;
+    (void)n;
     const int ctas = num_sms();
-    return round256((size_t)ctas * sizeof(ChainEntry)) + round256(decode_sets(ctas) * kBlockRows * sizeof(float2)) +
-           decode_sets(ctas) * kBlockRows * kD * sizeof(float);
+    const size_t rows = partial_rows(ctas, few_rows(L_q * (Hq / Hkv)));
+    return round256((size_t)ctas * sizeof(ChainEntry)) + round256(rows * sizeof(float2)) + rows * kD * sizeof(float);
 }
 
 int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t* lens, int L_q, int Hq, float scale, const void* q,
@@ -698,32 +1329,37 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     PageAttnArgs a;
     a.p = pool; a.n = n; a.L_q = L_q; a.Hq = Hq; a.G = Hq / pool.Hkv;
     a.rows = L_q * a.G;
-    a.row_blocks = (a.rows + kBlockRows - 1) / kBlockRows;
+    const bool few = few_rows(a.rows);
+    a.units = few ? 1 : (a.rows + 127) / 128;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.seqs = seqs; a.lens = lens; a.table = table;
     a.q = reinterpret_cast<const __nv_bfloat16*>(q); a.out = reinterpret_cast<__nv_bfloat16*>(out); a.lse = lse;
     char* at = reinterpret_cast<char*>(scratch);
     a.chains = reinterpret_cast<ChainEntry*>(at); at += round256((size_t)ctas * sizeof(ChainEntry));
-    a.part_ml = reinterpret_cast<float2*>(at); at += round256(decode_sets(ctas) * kBlockRows * sizeof(float2));
+    a.part_ml = reinterpret_cast<float2*>(at); at += round256(partial_rows(ctas, few) * sizeof(float2));
     a.part_o = reinterpret_cast<float*>(at);
     a.status = status;
     const long long rows = (long long)pool.n_pages * pool.Hkv * pool.T;
     CUtensorMap mk, mv;
-    const int box = pool.T < kStep ? pool.T : kStep;
+    const int step = few ? kStep : kQStep, box = pool.T < step ? pool.T : step;
     if (int rc = make_pool_map(&mk, pool.k8, rows, box)) return rc;
     if (int rc = make_pool_map(&mv, pool.v8, rows, box)) return rc;
     static std::atomic<bool> attr_done[64];
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64 || !attr_done[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(page_decode_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)decode_smem(kPageMaxSeqs));
+        cudaError_t e = cudaFuncSetAttribute(page_decode_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kDecodeSmem + prefix_bytes(kPageMaxSeqs)));
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(page_question_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQuestionSmem + prefix_bytes(kPageMaxSeqs)));
         if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
         if (dev >= 0 && dev < 64) attr_done[dev].store(true, std::memory_order_release);
     }
-    cudaError_t e = launch_kernel(page_decode_kernel, dim3(ctas), dim3(kDecodeWarps * 32), decode_smem(n), stream, mk, mv, a);
+    cudaError_t e = few ? launch_kernel(page_decode_kernel, dim3(ctas), dim3(kDecodeWarps * 32), kDecodeSmem + prefix_bytes(n), stream, mk, mv, a)
+                        : launch_kernel(page_question_kernel, dim3(ctas), dim3(kQThreads), kQuestionSmem + prefix_bytes(n), stream, mk, mv, a);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
-    e = launch_kernel(page_merge_kernel, dim3(ctas, kBlockRows), dim3(128), 0, stream, a, (int)kBlockRows);
+    e = few ? launch_kernel(page_merge_kernel<4>, dim3(ctas, kBlockRows / 2), dim3(256), 0, stream, a, (int)kBlockRows)
+            : launch_kernel(page_merge_kernel<1>, dim3(ctas, kQRows / 8), dim3(256), 0, stream, a, (int)kQRows);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
     return check_launch();
