@@ -630,22 +630,23 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 constexpr int kQStep = 64;
 constexpr int kQStages = 4;
 constexpr int kQRows = 256;
-constexpr int kQThreads = 480;
+constexpr int kQThreads = 512;
 constexpr int kQTile = 128 * kD * 2;                  // 32 KB: 128 rows of Q, two 64-column halves
 constexpr int kQHalf = kQTile / 2;
 constexpr int kQSlot = kQStep * kD * 2;               // 16 KB: K or V of a step, widened, two 64-column halves
 constexpr int kQSlotHalf = kQSlot / 2;
-constexpr int kQStage = 2 * kQStep * kD;              // 16 KB: the bytes of K and V of a step
+constexpr int kQStage = kQStep * kD;                  // 8 KB: the bytes of K or V of a step
 constexpr float kLazy = 2.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
 
 struct QuestionSmem {
-    uint64_t st_full[kQStages], st_empty[kQStages];
+    uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V]
     uint64_t k_full[2], v_full[2];
     uint64_t q_full[2];
     uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];      // [group][half]
     uint64_t c_full[8];
-    float4 chunk[8][4];             // of eight steps and each 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, any page missing
-    float scales[kQStages][8];      // K's, then V's, of the step's chunks of 16 keys, as they arrive
+    float4 chunk[8][4];             // of eight steps and each 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
+    int missing[8];                 // some keys of the step have no page
+    float scales[kQStages][8];      // K's, then V's, of the step's chunks of 16 keys, as they arrive with the bytes of K
     float2 ml[128];                 // the second group's row maxima and sums (blocks of one tile)
     uint32_t tmem_base;
     int abort_flag;
@@ -657,7 +658,7 @@ struct QuestionSmem {
     long long x, hi, total, ctas;
     ChainEntry chain;
 };
-constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQTile + 4 * (size_t)kQSlot + (size_t)kQStages * kQStage + sizeof(QuestionSmem);
+constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQTile + 4 * (size_t)kQSlot + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
 __host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
     return (1u << 4) | (b_mn_major << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);      // fp16 x fp16 -> fp32
@@ -675,12 +676,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 
 // One softmax step of one row over 64 keys: P over the first half of the logits' columns, running maximum and sum; returns the factor
 // for the row of O (1 unless the maximum grew by more than kLazy).  c: the row's factor for its logits.
-__device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4* chunk, int key0, int limit, float c, float& m, float& l) {
+__device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4* chunk, bool missing, int key0, int limit, float c, float& m, float& l) {
     uint32_t sr[2][32];
     tmem_ld32(s_addr, sr[0]);
     tc_wait_ld();
     tmem_ld32(s_addr + 32u, sr[1]);
-    const bool masked = key0 + kQStep - 1 > limit || chunk[0].w != 0.f;
+    const bool masked = key0 + kQStep - 1 > limit || missing;
     float top = -INFINITY;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -741,7 +742,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     unsigned char* const k_smem = q_smem + 2 * kQTile;           // two slots
     unsigned char* const v_smem = k_smem + 2 * kQSlot;
     unsigned char* const stage_smem = v_smem + 2 * kQSlot;
-    QuestionSmem* const sm = reinterpret_cast<QuestionSmem*>(stage_smem + kQStages * kQStage);
+    QuestionSmem* const sm = reinterpret_cast<QuestionSmem*>(stage_smem + 2 * kQStages * kQStage);
     int* const pre = reinterpret_cast<int*>(sm + 1);
     __shared__ int warp_sums[kQThreads / 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -780,259 +781,52 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         sm->ctas = ctas;
         sm->chain = ChainEntry{-1, 0, 0, 0};
     }
-    for (;;) {
-        // ---- one segment, or this CTA's stretch of it
-        if (threadIdx.x == 0) {
-            if (sm->step1 > 0) {            // behind the piece before
-                sm->x += (long long)(sm->step1 - sm->at.step) * sm->at.width;
-                sm->at.step = sm->step1;
-                if (sm->at.step == sm->at.n_steps) next_segment<2>(a, pre, sm->at);
+    // Two of the four warpgroups need few registers: 256 x 160 + 256 x 96 = 512 x 128
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+        for (;;) {
+            // ---- one segment, or this CTA's stretch of it
+            if (threadIdx.x == 0) {
+                if (sm->step1 > 0) {            // behind the piece before
+                    sm->x += (long long)(sm->step1 - sm->at.step) * sm->at.width;
+                    sm->at.step = sm->step1;
+                    if (sm->at.step == sm->at.n_steps) next_segment<2>(a, pre, sm->at);
+                }
+                const Place at = sm->at;
+                sm->step1 = 0;
+                if (sm->x < sm->hi) {
+                    const int step1 = (int)min((long long)at.n_steps, at.step + (sm->hi - sm->x) / at.width);
+                    const int row0 = at.block * kQRows, last_row = min(a.rows, row0 + kQRows) - 1;
+                    sm->step1 = step1;
+                    sm->first_limit = at.len - a.L_q + row0 / a.G;
+                    sm->last_limit = at.len - a.L_q + last_row / a.G;
+                    sm->n_t = max(0, min(step1, (sm->last_limit + kQStep) / kQStep) - at.step);       // (a negative limit: none)
+                    if (at.step == 0 && step1 < at.n_steps) {
+                        Place end = at;
+                        end.step = at.n_steps - 1;
+                        sm->chain = ChainEntry{cta_of(axis_at<2>(a, pre, end), sm->total, sm->ctas), at.b, at.h, at.block};
+                    }
+                }
+                if (sm->used)                   // the barriers start anew with every piece: nothing is under way on them
+                    for (uint64_t* bar = sm->st_full[0]; bar != sm->c_full + 8; ++bar) mbar_inval(bar);
+                sm->used = 1;
+                for (int i = 0; i < kQStages; ++i) {
+                    mbar_init(&sm->st_full[0][i], 1 + 8); mbar_init(&sm->st_full[1][i], 1);
+                    mbar_init(&sm->st_empty[0][i], 4); mbar_init(&sm->st_empty[1][i], 4);
+                }
+                for (int i = 0; i < 2; ++i) {
+                    mbar_init(&sm->k_full[i], 4); mbar_init(&sm->v_full[i], 4); mbar_init(&sm->q_full[i], 4);
+                    for (int j = 0; j < 2; ++j) { mbar_init(&sm->s_full[i][j], 1); mbar_init(&sm->p_full[i][j], 4); mbar_init(&sm->pv_done[i][j], 1); }
+                }
+                for (int i = 0; i < 8; ++i) mbar_init(&sm->c_full[i], 1);
+                sm->poison = 0;
+                mbar_fence_init();
             }
-            const Place at = sm->at;
-            sm->step1 = 0;
-            if (sm->x < sm->hi) {
-                const int step1 = (int)min((long long)at.n_steps, at.step + (sm->hi - sm->x) / at.width);
-                const int row0 = at.block * kQRows, last_row = min(a.rows, row0 + kQRows) - 1;
-                sm->step1 = step1;
-                sm->first_limit = at.len - a.L_q + row0 / a.G;
-                sm->last_limit = at.len - a.L_q + last_row / a.G;
-                sm->n_t = max(0, min(step1, (sm->last_limit + kQStep) / kQStep) - at.step);       // (a negative limit: none)
-                if (at.step == 0 && step1 < at.n_steps) {
-                    Place end = at;
-                    end.step = at.n_steps - 1;
-                    sm->chain = ChainEntry{cta_of(axis_at<2>(a, pre, end), sm->total, sm->ctas), at.b, at.h, at.block};
-                }
-            }
-            if (sm->used)                   // the barriers start anew with every piece: nothing is under way on them
-                for (uint64_t* bar = sm->st_full; bar != sm->c_full + 8; ++bar) mbar_inval(bar);
-            sm->used = 1;
-            for (int i = 0; i < kQStages; ++i) { mbar_init(&sm->st_full[i], 1 + 8); mbar_init(&sm->st_empty[i], 4); }
-            for (int i = 0; i < 2; ++i) {
-                mbar_init(&sm->k_full[i], 4); mbar_init(&sm->v_full[i], 4); mbar_init(&sm->q_full[i], 4);
-                for (int j = 0; j < 2; ++j) { mbar_init(&sm->s_full[i][j], 1); mbar_init(&sm->p_full[i][j], 4); mbar_init(&sm->pv_done[i][j], 1); }
-            }
-            for (int i = 0; i < 8; ++i) mbar_init(&sm->c_full[i], 1);
-            sm->poison = 0;
-            mbar_fence_init();
-        }
-        __syncthreads();
-        if (sm->step1 == 0) break;
-        bool ok = true;
-        const int n_t = sm->n_t, step0 = sm->at.step;
-        const bool pair = sm->at.width == 2;
-        if (warp == 14) {
-            // -------------------------------------------------------------------------------------------- bytes and scales
-            const Place at = sm->at;
-            int ids = -1, ids_first = -1;
-            const int box = min(T, kQStep), pages = kQStep / box;      // copies of a step
-            for (int t = 0; t < n_t && ok; ++t) {
-                const int slot = t % kQStages;
-                if (t >= kQStages) {
-                    ok = mbar_wait(&sm->st_empty[slot], (uint32_t)((t / kQStages - 1) & 1), abort, a.status, 260);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                }
-                const int key0 = (step0 + t) * kQStep, page0 = key0 / T;
-                if (ids_first < 0 || page0 + pages > ids_first + 32) {
-                    ids_first = page0;
-                    const int j = page0 + lane;
-                    const bool needed = j < a.p.max_pages && (long long)j * T < at.len;
-                    ids = needed ? __ldg(a.table + (size_t)at.seq * a.p.max_pages + j) : -1;
-                    if ((unsigned)ids >= (unsigned)a.p.n_pages) {
-                        if (needed && at.h == 0 && at.block == 0) report_status(a.status, DAF_ERR_BOUNDS, 261, ids);
-                        ids = -1;
-                    }
-                }
-                // lanes 0-3: K's scales of the chunks of 16 keys, 4-7: V's
-                const int id = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + ((lane & 3) * 16) / box * (box < kQStep ? 1 : 0));
-                if (lane < 8) {
-                    float* const dst = &sm->scales[slot][lane];
-                    if (id >= 0) {
-                        const float* const src = (lane < 4 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + at.h;
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sm->st_full[slot])) : "memory");
-                    } else {
-                        *dst = -1.f;
-                        mbar_arrive(&sm->st_full[slot]);
-                    }
-                }
-                const int mine = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (lane < pages ? lane : 0));
-                const unsigned there = __ballot_sync(0xFFFFFFFFu, lane < pages && mine >= 0);
-                if (lane == 0) mbar_arrive_expect_tx(&sm->st_full[slot], (uint32_t)(__popc(there) * 2 * box * kD));
-                __syncwarp();
-                if ((there >> lane) & 1u) {
-                    unsigned char* const dst = stage_smem + slot * kQStage + lane * box * kD;
-                    const int row = (mine * Hkv + at.h) * T + key0 % T;       // (key0 % T is 0 unless a page holds several steps)
-                    tma_load_2d(dst, &tmap_k, &sm->st_full[slot], 0, row);
-                    tma_load_2d(dst + kQStep * kD, &tmap_v, &sm->st_full[slot], 0, row);
-                }
-                __syncwarp();
-            }
-            if (!ok)       // loads in flight get a bounded chance to land before the CTA retires
-                for (int i = 0; i < kQStages && lane == 0; ++i)
-                    for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[i], 0) && !mbar_try_wait(&sm->st_full[i], 1); ++k) {}
-        } else if (warp >= 10) {
-            // --------------------------------------------------------------------------------------------------- widening
-            // A lane takes 16 bytes of a row at a time.  Eight lanes take four neighbouring pieces of each of two rows r and r ^ 5:
-            // with the swizzle of either side their reads and their writes all fall into different banks.
-            const int cw = warp - 10;
-            const int first_limit = sm->first_limit, len = sm->at.len;
-            const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
-            for (int t = 0; t < n_t && ok; ++t) {
-                const int slot = t % kQStages, b = t & 1;
-                ok = mbar_wait(&sm->st_full[slot], (uint32_t)((t / kQStages) & 1), abort, a.status, 262);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
-                const int key0 = (step0 + t) * kQStep;
-                const float* const sc = sm->scales[slot];
-                const bool missing = sc[0] < 0.f || sc[1] < 0.f || sc[2] < 0.f || sc[3] < 0.f;
-                const bool odd = key0 + kQStep - 1 > first_limit || missing;
-                // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
-                const int u = pair ? t - 2 : (t >> 1) - 1;
-                for (int kv = 0; kv < 2 && ok; ++kv) {
-                    const unsigned char* const src = stage_smem + slot * kQStage + kv * kQStep * kD;
-                    unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot;
-                    uint4 w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
-                        const int r = 16 * cw + 8 * (i >> 1) + r8, c = 4 * (i & 1) + piece;
-                        w[i] = *reinterpret_cast<const uint4*>(src + r * kD + ((c ^ r8) << 4));
-                    }
-                    if (kv == 1 && odd) {
-                        // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in a key that
-                        // only some rows see is taken out, and put into the rows that see it at the end.
-                        bool found = false;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = key0 + 16 * cw + 8 * (i >> 1) + r8;
-                            if (key >= len || sc[cw] < 0.f) w[i] = make_uint4(0u, 0u, 0u, 0u);
-                            else if (key > first_limit) {
-                                const uint4 nan = make_uint4(nan_bytes(w[i].x), nan_bytes(w[i].y), nan_bytes(w[i].z), nan_bytes(w[i].w));
-                                found |= (nan.x | nan.y | nan.z | nan.w) != 0u;
-                                w[i].x &= ~nan.x; w[i].y &= ~nan.y; w[i].z &= ~nan.z; w[i].w &= ~nan.w;
-                            }
-                        }
-                        if (found) sm->poison = 1;
-                    }
-                    uint32_t h[4][8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        h[i][0] = widen2(w[i].x); h[i][1] = widen2(w[i].x >> 16); h[i][2] = widen2(w[i].y); h[i][3] = widen2(w[i].y >> 16);
-                        h[i][4] = widen2(w[i].z); h[i][5] = widen2(w[i].z >> 16); h[i][6] = widen2(w[i].w); h[i][7] = widen2(w[i].w >> 16);
-                    }
-                    if (kv == 1) {       // what is left of V's scale beside a power of two (nothing, as daf_page_write leaves them)
-                        const float vs = sc[4 + cw];
-                        const float vm = vs > 0.f ? __int_as_float((__float_as_int(vs) & 0x7FFFFF) | 0x3F800000) : 1.f;
-                        if (vm != 1.f) {
-                            const __half2 f = __float2half2_rn(vm);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    const __half2 y = __hmul2(*reinterpret_cast<__half2*>(&h[i][j]), f);
-                                    h[i][j] = *reinterpret_cast<const uint32_t*>(&y);
-                                }
-                        }
-                    }
-                    if (t >= 2) {
-                        uint64_t (*const freed)[2] = kv == 0 ? sm->s_full : sm->pv_done;
-                        if (pair) {
-                            ok = mbar_wait(&freed[0][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 263);
-                            if (ok) ok = mbar_wait(&freed[1][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 264);
-                        } else {
-                            ok = mbar_wait(&freed[b][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 265);
-                        }
-                        ok = __all_sync(0xFFFFFFFFu, ok);
-                        if (!ok) break;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 16 * cw + 8 * (i >> 1) + r8;
-                        unsigned char* const row = dst + (i & 1) * kQSlotHalf + r * 128;
-                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(h[i][0], h[i][1], h[i][2], h[i][3]);
-                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(h[i][4], h[i][5], h[i][6], h[i][7]);
-                    }
-                    if (kv == 0 && cw == 0 && lane < 4) {
-                        const float vs = sc[4 + lane];
-                        const int e = vs > 0.f ? max((__float_as_int(vs) >> 23) - 127, -126) : 0;
-                        sm->chunk[t & 7][lane] = make_float4(sc[lane], (float)e, __int_as_float((127 - e) << 23), missing ? 1.f : 0.f);
-                    }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (kv == 0 && cw == 0) mbar_arrive(&sm->c_full[t & 7]);
-                        mbar_arrive(kv == 0 ? &sm->k_full[b] : &sm->v_full[b]);
-                        if (kv == 1) mbar_arrive(&sm->st_empty[slot]);
-                    }
-                }
-            }
-        } else if (warp >= 8) {
-            // --------------------------------------------------------------------------------------------------- products
-            const int g = warp - 8;
-            const int n_u = pair ? n_t : (n_t - g + 1) / 2;          // steps of this group
-            if (n_u > 0) {
-                constexpr uint32_t idesc_qk = make_idesc_f16(128, kQStep, 0), idesc_pv = make_idesc_f16(128, kD, 1);
-                const uint32_t qa = smem_u32(q_smem + (pair ? g : 0) * kQTile);
-                const uint32_t s_col = tmem + (uint32_t)(g * 256), o_col = s_col + 128u;
-                uint64_t qd[8], kd[2][8], vd[2][4];
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    qd[kk] = make_smem_desc(qa + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQHalf), 16, 1024);
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        kd[b][kk] = make_smem_desc(smem_u32(k_smem + (pair ? b : g) * kQSlot) + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQSlotHalf), 16, 1024);
-                }
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        vd[b][kk] = make_smem_desc(smem_u32(v_smem + (pair ? b : g) * kQSlot) + (uint32_t)kk * 2048u, kQSlotHalf, 1024);
-                auto slot_of = [&](int u) { return pair ? u & 1 : g; };
-                auto use_of = [&](int u) { return pair ? u >> 1 : u; };       // how often the slot was filled before
-                auto issue_qk = [&](int b) {
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        tc_mma_ss(s_col + (uint32_t)(b * kQStep), qd[kk], b ? kd[1][kk] : kd[0][kk], idesc_qk, kk > 0 ? 1u : 0u);
-                    tc_commit(&sm->s_full[g][b]);
-                };
-                ok = mbar_wait(&sm->q_full[pair ? g : 0], 0, abort, a.status, 266);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                for (int u = 0; u < 2 && u < n_u && ok; ++u) {
-                    ok = mbar_wait(&sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 267);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) issue_qk(u);
-                    __syncwarp();
-                }
-                auto step = [&](auto half, int u) -> bool {
-                    constexpr int b = decltype(half)::value;
-                    bool there = mbar_wait(&sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 268);
-                    if (there) there = mbar_wait(&sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, a.status, 269);
-                    if (!__all_sync(0xFFFFFFFFu, there)) return false;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            tc_mma_ts(o_col, s_col + (uint32_t)(b * kQStep + kk * 8), vd[b][kk], idesc_pv, (u == 0 && kk == 0) ? 0u : 1u);
-                        tc_commit(&sm->pv_done[g][b]);
-                    }
-                    __syncwarp();
-                    if (u + 2 < n_u) {
-                        there = mbar_wait(&sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, a.status, 270);
-                        if (!__all_sync(0xFFFFFFFFu, there)) return false;
-                        tc_fence_after();
-                        if (elect_one()) issue_qk(b);
-                        __syncwarp();
-                    }
-                    return true;
-                };
-                for (int u = 0; u < n_u && ok; u += 2) {
-                    ok = step(std::integral_constant<int, 0>{}, u);
-                    if (ok && u + 1 < n_u) ok = step(std::integral_constant<int, 1>{}, u + 1);
-                }
-            }
-        } else {
+            __syncthreads();
+            if (sm->step1 == 0) break;
+            bool ok = true;
+            const int n_t = sm->n_t, step0 = sm->at.step;
+            const bool pair = sm->at.width == 2;
             // ------------------------------------------------------------------------------------- softmax, a row per thread
             const int g = warp >> 2, rt = threadIdx.x & 127;
             const int row = sm->at.block * kQRows + (pair ? g * 128 : 0) + rt;
@@ -1086,7 +880,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t & 7], (step0 + t) * kQStep, limit, c, m, l);
+                const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t & 7], sm->missing[t & 7] != 0, (step0 + t) * kQStep, limit, c, m, l);
                 if (u > 0 && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
                     // the product before must have completed before O is touched
                     ok = mbar_wait(&sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, a.status, 273);
@@ -1202,11 +996,247 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     a.part_ml[set] = make_float2(m, l);
                 }
             }
+            tc_fence_before();
+            __syncthreads();       // the barriers, rings and tensor memory are free
+            tc_fence_after();
+            if (sm->abort_flag != 0) break;
         }
-        tc_fence_before();
-        __syncthreads();       // the barriers, rings and tensor memory are free
-        tc_fence_after();
-        if (sm->abort_flag != 0) break;
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        for (;;) {
+            __syncthreads();
+            if (sm->step1 == 0) break;
+            bool ok = true;
+            const int n_t = sm->n_t, step0 = sm->at.step;
+            const bool pair = sm->at.width == 2;
+            if (warp == 14) {
+                // -------------------------------------------------------------------------------------------- bytes and scales
+                const Place at = sm->at;
+                int ids = -1, ids_first = -1;
+                const int box = min(T, kQStep), pages = kQStep / box;      // copies of a step
+                // in the order in which they are widened: K two steps ahead of V
+                for (int i = 0; i < 2 * (n_t + 2) && ok; ++i) {
+                    const int kv = i & 1, t = (i >> 1) - 2 * kv;
+                    if (t < 0 || t >= n_t) continue;
+                    const int slot = t % kQStages;
+                    if (t >= kQStages) {
+                        ok = mbar_wait(&sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, a.status, 260);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                    }
+                    uint64_t* const full = &sm->st_full[kv][slot];
+                    const int key0 = (step0 + t) * kQStep, page0 = key0 / T;
+                    if (ids_first < 0 || page0 < ids_first || page0 + pages > ids_first + 32) {
+                        ids_first = max(0, page0 - 2 * pages * (1 - kv));           // (V of two steps before is still to come)
+                        const int j = ids_first + lane;
+                        const bool needed = j < a.p.max_pages && (long long)j * T < at.len;
+                        ids = needed ? __ldg(a.table + (size_t)at.seq * a.p.max_pages + j) : -1;
+                        if ((unsigned)ids >= (unsigned)a.p.n_pages) {
+                            if (needed && at.h == 0 && at.block == 0) report_status(a.status, DAF_ERR_BOUNDS, 261, ids);
+                            ids = -1;
+                        }
+                    }
+                    // lanes 0-3: K's scales of the chunks of 16 keys, 4-7: V's
+                    const int id = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (box < kQStep ? (lane & 3) * 16 / box : 0));
+                    if (kv == 0 && lane < 8) {
+                        float* const dst = &sm->scales[slot][lane];
+                        if (id >= 0) {
+                            const float* const src = (lane < 4 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + at.h;
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+                            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
+                        } else {
+                            *dst = -1.f;
+                            mbar_arrive(full);
+                        }
+                    }
+                    const int mine = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (lane < pages ? lane : 0));
+                    const unsigned there = __ballot_sync(0xFFFFFFFFu, lane < pages && mine >= 0);
+                    if (lane == 0) mbar_arrive_expect_tx(full, (uint32_t)(__popc(there) * box * kD));
+                    __syncwarp();
+                    if ((there >> lane) & 1u) {
+                        const int row = (mine * Hkv + at.h) * T + key0 % T;       // (key0 % T is 0 unless a page holds several steps)
+                        tma_load_2d(stage_smem + (kv * kQStages + slot) * kQStage + lane * box * kD, kv == 0 ? &tmap_k : &tmap_v, full, 0, row);
+                    }
+                    __syncwarp();
+                }
+                if (!ok)       // loads in flight get a bounded chance to land before the CTA retires
+                    for (int i = 0; i < 2 * kQStages && lane == 0; ++i)
+                        for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[0][i], 0) && !mbar_try_wait(&sm->st_full[0][i], 1); ++k) {}
+            } else if (warp == 15) {
+            } else if (warp >= 10) {
+                // --------------------------------------------------------------------------------------------------- widening
+                // A lane takes 16 bytes of a row at a time.  Eight lanes take four neighbouring pieces of each of two rows r and r ^ 5:
+                // with the swizzle of either side their reads and their writes all fall into different banks.
+                // K runs two steps ahead of V: K's slot is free once the logits two steps before are there, V's once the product two
+                // steps before is, a softmax later; in step, K of the next step would wait for that too.
+                const int cw = warp - 10;
+                const int first_limit = sm->first_limit, len = sm->at.len;
+                const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
+                auto widen = [&](auto kv_c, int t) -> bool {
+                    constexpr int kv = decltype(kv_c)::value;
+                    const int slot = t % kQStages, b = t & 1;
+                    bool there = mbar_wait(&sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, a.status, 262);
+                    if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                    const int key0 = (step0 + t) * kQStep;
+                    const unsigned char* const src = stage_smem + (kv * kQStages + slot) * kQStage;
+                    uint4 w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
+                        const int r = 16 * cw + 8 * (i >> 1) + r8, c = 4 * (i & 1) + piece;
+                        w[i] = *reinterpret_cast<const uint4*>(src + r * kD + ((c ^ r8) << 4));
+                    }
+                    if (kv == 0 && cw == 0 && lane < 4) {
+                        const float* const sc = sm->scales[slot];
+                        const float vs = sc[4 + lane];
+                        const int bits = __float_as_int(vs), e = vs > 0.f ? max((bits >> 23) - 127, -126) : 0;
+                        sm->chunk[t & 7][lane] = make_float4(sc[lane], (float)e, __int_as_float((127 - e) << 23),
+                                                             vs > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f);
+                        if (lane == 0) sm->missing[t & 7] = sc[0] < 0.f || sc[1] < 0.f || sc[2] < 0.f || sc[3] < 0.f;
+                    }
+                    float4 sc = make_float4(0.f, 0.f, 0.f, 1.f);
+                    if (kv == 1) sc = sm->chunk[t & 7][cw];
+                    if (kv == 1 && (key0 + kQStep - 1 > first_limit || sc.x < 0.f)) {
+                        // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in a key that
+                        // only some rows see is taken out, and put into the rows that see it at the end.
+                        bool found = false;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key0 + 16 * cw + 8 * (i >> 1) + r8;
+                            if (key >= len || sc.x < 0.f) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                            else if (key > first_limit) {
+                                const uint4 nan = make_uint4(nan_bytes(w[i].x), nan_bytes(w[i].y), nan_bytes(w[i].z), nan_bytes(w[i].w));
+                                found |= (nan.x | nan.y | nan.z | nan.w) != 0u;
+                                w[i].x &= ~nan.x; w[i].y &= ~nan.y; w[i].z &= ~nan.z; w[i].w &= ~nan.w;
+                            }
+                        }
+                        if (found) sm->poison = 1;
+                    }
+                    uint32_t h[4][8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        h[i][0] = widen2(w[i].x); h[i][1] = widen2(w[i].x >> 16); h[i][2] = widen2(w[i].y); h[i][3] = widen2(w[i].y >> 16);
+                        h[i][4] = widen2(w[i].z); h[i][5] = widen2(w[i].z >> 16); h[i][6] = widen2(w[i].w); h[i][7] = widen2(w[i].w >> 16);
+                    }
+                    if (kv == 1 && sc.w != 1.f) {       // what V's scale is beside a power of two (nothing, as daf_page_write leaves them)
+                        const __half2 f = __float2half2_rn(sc.w);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const __half2 y = __hmul2(*reinterpret_cast<__half2*>(&h[i][j]), f);
+                                h[i][j] = *reinterpret_cast<const uint32_t*>(&y);
+                            }
+                    }
+                    if (t >= 2) {
+                        // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
+                        const int u = pair ? t - 2 : (t >> 1) - 1;
+                        uint64_t (*const freed)[2] = kv == 0 ? sm->s_full : sm->pv_done;
+                        if (pair) {
+                            there = mbar_wait(&freed[0][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 263);
+                            if (there) there = mbar_wait(&freed[1][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 264);
+                        } else {
+                            there = mbar_wait(&freed[b][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 265);
+                        }
+                        if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                    }
+                    unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 16 * cw + 8 * (i >> 1) + r8;
+                        unsigned char* const row = dst + (i & 1) * kQSlotHalf + r * 128;
+                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(h[i][0], h[i][1], h[i][2], h[i][3]);
+                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(h[i][4], h[i][5], h[i][6], h[i][7]);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (kv == 0 && cw == 0) mbar_arrive(&sm->c_full[t & 7]);
+                        mbar_arrive(kv == 0 ? &sm->k_full[b] : &sm->v_full[b]);
+                        mbar_arrive(&sm->st_empty[kv][slot]);
+                    }
+                    return true;
+                };
+                for (int t = -2; t < n_t && ok; ++t) {
+                    if (t + 2 < n_t) ok = widen(std::integral_constant<int, 0>{}, t + 2);
+                    if (ok && t >= 0) {
+                        // (the constants of the step were written by one of these warps)
+                        ok = mbar_wait(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, a.status, 275);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (ok) ok = widen(std::integral_constant<int, 1>{}, t);
+                    }
+                }
+            } else if (warp >= 8) {
+                // --------------------------------------------------------------------------------------------------- products
+                const int g = warp - 8;
+                const int n_u = pair ? n_t : (n_t - g + 1) / 2;          // steps of this group
+                if (n_u > 0) {
+                    constexpr uint32_t idesc_qk = make_idesc_f16(128, kQStep, 0), idesc_pv = make_idesc_f16(128, kD, 1);
+                    const uint32_t qa = smem_u32(q_smem + (pair ? g : 0) * kQTile);
+                    const uint32_t s_col = tmem + (uint32_t)(g * 256), o_col = s_col + 128u;
+                    uint64_t qd[8], kd[2][8], vd[2][4];
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        qd[kk] = make_smem_desc(qa + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQHalf), 16, 1024);
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+                            kd[b][kk] = make_smem_desc(smem_u32(k_smem + (pair ? b : g) * kQSlot) + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQSlotHalf), 16, 1024);
+                    }
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+                            vd[b][kk] = make_smem_desc(smem_u32(v_smem + (pair ? b : g) * kQSlot) + (uint32_t)kk * 2048u, kQSlotHalf, 1024);
+                    auto slot_of = [&](int u) { return pair ? u & 1 : g; };
+                    auto use_of = [&](int u) { return pair ? u >> 1 : u; };       // how often the slot was filled before
+                    auto issue_qk = [&](int b) {
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)
+                            tc_mma_ss(s_col + (uint32_t)(b * kQStep), qd[kk], b ? kd[1][kk] : kd[0][kk], idesc_qk, kk > 0 ? 1u : 0u);
+                        tc_commit(&sm->s_full[g][b]);
+                    };
+                    ok = mbar_wait(&sm->q_full[pair ? g : 0], 0, abort, a.status, 266);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    for (int u = 0; u < 2 && u < n_u && ok; ++u) {
+                        ok = mbar_wait(&sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 267);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) issue_qk(u);
+                        __syncwarp();
+                    }
+                    auto step = [&](auto half, int u) -> bool {
+                        constexpr int b = decltype(half)::value;
+                        bool there = mbar_wait(&sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 268);
+                        if (there) there = mbar_wait(&sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, a.status, 269);
+                        if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 0; kk < 4; ++kk)
+                                tc_mma_ts(o_col, s_col + (uint32_t)(b * kQStep + kk * 8), vd[b][kk], idesc_pv, (u == 0 && kk == 0) ? 0u : 1u);
+                            tc_commit(&sm->pv_done[g][b]);
+                        }
+                        __syncwarp();
+                        if (u + 2 < n_u) {
+                            there = mbar_wait(&sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, a.status, 270);
+                            if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                            tc_fence_after();
+                            if (elect_one()) issue_qk(b);
+                            __syncwarp();
+                        }
+                        return true;
+                    };
+                    for (int u = 0; u < n_u && ok; u += 2) {
+                        ok = step(std::integral_constant<int, 0>{}, u);
+                        if (ok && u + 1 < n_u) ok = step(std::integral_constant<int, 1>{}, u + 1);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncthreads();       // the barriers, rings and tensor memory are free
+            tc_fence_after();
+            if (sm->abort_flag != 0) break;
+        }
     }
     if (threadIdx.x == 0) a.chains[blockIdx.x] = sm->abort_flag == 0 ? sm->chain : ChainEntry{-1, 0, 0, 0};
     tc_fence_before();
@@ -1351,6 +1381,10 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
         cudaError_t e = cudaFuncSetAttribute(page_decode_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kDecodeSmem + prefix_bytes(kPageMaxSeqs)));
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(page_question_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQuestionSmem + prefix_bytes(kPageMaxSeqs)));
+        // the question kernel's warpgroups trade registers: their shares add up to what 128 a thread give the block at launch
+        cudaFuncAttributes fa = {};
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, page_question_kernel);
+        if (e == cudaSuccess && fa.numRegs < 128) e = cudaErrorLaunchOutOfResources;
         if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
         if (dev >= 0 && dev < 64) attr_done[dev].store(true, std::memory_order_release);
     }
