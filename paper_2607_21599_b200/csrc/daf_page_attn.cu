@@ -210,7 +210,7 @@ __device__ __forceinline__ float partial_weight(float2 ml, float mx) {
 __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
 page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
     extern __shared__ unsigned char decode_smem_raw[];
-    unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(decode_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* const smem = decode_smem_raw + ((1024u - (smem_u32(decode_smem_raw) & 1023u)) & 1023u);      // (stays a shared address to the compiler)
     DecodeWarp* const warps = reinterpret_cast<DecodeWarp*>(smem + kRingBytes);
     int* const pre = reinterpret_cast<int*>(warps + kDecodeWarps);
     __shared__ int warp_sums[kDecodeWarps];
@@ -618,9 +618,10 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 
 // ---------------------------------------------------------------------------------------------- many rows: tensor memory
 // More than 16 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
-// of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 15 warps:
-//   14     asks for the bytes of K and V (TMA, kStages steps ahead) and their scales;
-//   10-13  widen them to fp16, exactly, into the two-slot rings that the products read (128-byte swizzle);
+// of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 20 warps:
+//   10, 11  ask for the bytes of K and V (TMA, kQStages steps ahead) and their scales;
+//   12-15, 16-19  widen K's, and V's, to fp16, exactly, into the two-slot rings that the products read (128-byte swizzle).  Each of
+//          these is a chain of waits, reads, conversions and writes, so K and V have warps of their own;
 //   8, 9   issue a tile group's products: S = Q K^T into one of two halves, O += P V with P from tensor memory;
 //   0-3, 4-7  a tile group's softmax, a row per thread, and its epilogue.
 // A block of two tiles shares every widened K and V (the bytes pass through shared memory once for both, and shared memory is what
@@ -630,7 +631,7 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 constexpr int kQStep = 64;
 constexpr int kQStages = 4;
 constexpr int kQRows = 256;
-constexpr int kQThreads = 512;
+constexpr int kQThreads = 640;
 constexpr int kQTile = 128 * kD * 2;                  // 32 KB: 128 rows of Q, two 64-column halves
 constexpr int kQHalf = kQTile / 2;
 constexpr int kQSlot = kQStep * kD * 2;               // 16 KB: K or V of a step, widened, two 64-column halves
@@ -677,20 +678,29 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 // One softmax step of one row over 64 keys: P over the first half of the logits' columns, running maximum and sum; returns the factor
 // for the row of O (1 unless the maximum grew by more than kLazy).  c: the row's factor for its logits.
 __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4* chunk, bool missing, int key0, int limit, float c, float& m, float& l) {
+    if (__any_sync(0xFFFFFFFFu, key0 + kQStep - 1 > limit || missing)) {
+        // rare (the last steps of a sequence): logits of keys that the row does not see become -inf where they are
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            uint32_t r[16];
+            tmem_ld16(s_addr + (uint32_t)(16 * i), r);
+            tc_wait_ld();
+            const int last = chunk[i].x < 0.f ? -1 : limit - key0 - 16 * i;
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (j > last) r[j] = 0xFF800000u;
+            tmem_st16(s_addr + (uint32_t)(16 * i), r);
+        }
+        tc_wait_st();
+    }
     uint32_t sr[2][32];
     tmem_ld32(s_addr, sr[0]);
     tc_wait_ld();
     tmem_ld32(s_addr + 32u, sr[1]);
-    const bool masked = key0 + kQStep - 1 > limit || missing;
     float top = -INFINITY;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         if (half == 1) tc_wait_ld();
-        if (masked) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (key0 + 32 * half + j > limit || chunk[2 * half + j / 16].x < 0.f) sr[half][j] = 0xFF800000u;
-        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const float2 k2 = *reinterpret_cast<const float2*>(chunk + 2 * half + i);
@@ -734,10 +744,28 @@ __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4*
     return alpha;
 }
 
+// The bounded wait of this kernel (a second at most, or until another thread has given up): it only leaves the number of the wait in
+// the abort flag, which one thread reports at the end.  The warps' loops are many, and what they keep in the instruction caches
+// counts: with longer waits and every rare case unrolled, warps that had work found no instruction a sixth of the time.
+__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile int* abort, int where) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = global_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (*abort != 0) return false;
+        if (global_ns() - t0 > kWaitLimitNs) {
+            *abort = where;
+            return false;
+        }
+    }
+}
+
 __global__ void __launch_bounds__(kQThreads, 1)
 page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
     extern __shared__ unsigned char question_smem_raw[];
-    unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(question_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* const smem = question_smem_raw + ((1024u - (smem_u32(question_smem_raw) & 1023u)) & 1023u);      // (stays a shared address to the compiler)
     unsigned char* const q_smem = smem;                          // two tiles
     unsigned char* const k_smem = q_smem + 2 * kQTile;           // two slots
     unsigned char* const v_smem = k_smem + 2 * kQSlot;
@@ -781,9 +809,9 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         sm->ctas = ctas;
         sm->chain = ChainEntry{-1, 0, 0, 0};
     }
-    // Two of the four warpgroups need few registers: 256 x 160 + 256 x 96 = 512 x 128
+    // Three of the five warpgroups need few registers: 256 x 144 + 384 x 64 = 640 x 96
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
         for (;;) {
             // ---- one segment, or this CTA's stretch of it
             if (threadIdx.x == 0) {
@@ -875,15 +903,15 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             float m = -INFINITY, l = 0.f;
             for (int u = 0; u < n_u; ++u) {
                 const int t = pair ? u : 2 * u + g, b = u & 1;
-                ok = mbar_wait(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, a.status, 271);
-                if (ok) ok = mbar_wait(&sm->s_full[g][b], (uint32_t)((u >> 1) & 1), abort, a.status, 272);
+                ok = wait_phase(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, 271);
+                if (ok) ok = wait_phase(&sm->s_full[g][b], (uint32_t)((u >> 1) & 1), abort, 272);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t & 7], sm->missing[t & 7] != 0, (step0 + t) * kQStep, limit, c, m, l);
                 if (u > 0 && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
                     // the product before must have completed before O is touched
-                    ok = mbar_wait(&sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, a.status, 273);
+                    ok = wait_phase(&sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, 273);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) break;
                     tc_fence_after();
@@ -904,7 +932,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             }
             // both last products (each on a barrier of its own)
             for (int u = max(0, n_u - 2); u < n_u && ok; ++u) {
-                ok = mbar_wait(&sm->pv_done[g][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 274);
+                ok = wait_phase(&sm->pv_done[g][u & 1], (uint32_t)((u >> 1) & 1), abort, 274);
                 ok = __all_sync(0xFFFFFFFFu, ok);
             }
             tc_fence_after();
@@ -1002,150 +1030,138 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             if (sm->abort_flag != 0) break;
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         for (;;) {
             __syncthreads();
             if (sm->step1 == 0) break;
             bool ok = true;
             const int n_t = sm->n_t, step0 = sm->at.step;
             const bool pair = sm->at.width == 2;
-            if (warp == 14) {
-                // -------------------------------------------------------------------------------------------- bytes and scales
-                const Place at = sm->at;
-                int ids = -1, ids_first = -1;
-                const int box = min(T, kQStep), pages = kQStep / box;      // copies of a step
-                // in the order in which they are widened: K two steps ahead of V
-                for (int i = 0; i < 2 * (n_t + 2) && ok; ++i) {
-                    const int kv = i & 1, t = (i >> 1) - 2 * kv;
-                    if (t < 0 || t >= n_t) continue;
+            if (warp == 10 || warp == 11) {
+                // ---------------------------------------------------------------------------------------- bytes and scales
+                const int kv = warp - 10, seq = sm->at.seq, h = sm->at.h, len = sm->at.len;
+                const bool reports = kv == 0 && h == 0 && sm->at.block == 0;
+                const int page_bits = 31 - __clz(T), box = min(T, kQStep), pages = kQStep / box;      // copies of a step
+                const int chunk_page = box < kQStep ? ((lane & 3) * 16) >> page_bits : 0;             // page of a chunk of 16 keys
+                int ids = -1, ids_end = 0;          // page numbers of 32 pages that end in front of ids_end, one a lane
+                for (int t = 0; t < n_t && ok; ++t) {
                     const int slot = t % kQStages;
                     if (t >= kQStages) {
-                        ok = mbar_wait(&sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, a.status, 260);
-                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        ok = __all_sync(0xFFFFFFFFu, wait_phase(&sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, 260));
                         if (!ok) break;
                     }
                     uint64_t* const full = &sm->st_full[kv][slot];
-                    const int key0 = (step0 + t) * kQStep, page0 = key0 / T;
-                    if (ids_first < 0 || page0 < ids_first || page0 + pages > ids_first + 32) {
-                        ids_first = max(0, page0 - 2 * pages * (1 - kv));           // (V of two steps before is still to come)
-                        const int j = ids_first + lane;
-                        const bool needed = j < a.p.max_pages && (long long)j * T < at.len;
-                        ids = needed ? __ldg(a.table + (size_t)at.seq * a.p.max_pages + j) : -1;
+                    const int key0 = (step0 + t) * kQStep, page0 = key0 >> page_bits;
+                    if (page0 + pages > ids_end) {
+                        ids_end = page0 + 32;
+                        const int j = page0 + lane;
+                        const bool needed = j < a.p.max_pages && (long long)j * T < len;
+                        ids = needed ? __ldg(a.table + (size_t)seq * a.p.max_pages + j) : -1;
                         if ((unsigned)ids >= (unsigned)a.p.n_pages) {
-                            if (needed && at.h == 0 && at.block == 0) report_status(a.status, DAF_ERR_BOUNDS, 261, ids);
+                            if (needed && reports) report_status(a.status, DAF_ERR_BOUNDS, 261, ids);
                             ids = -1;
                         }
                     }
-                    // lanes 0-3: K's scales of the chunks of 16 keys, 4-7: V's
-                    const int id = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (box < kQStep ? (lane & 3) * 16 / box : 0));
-                    if (kv == 0 && lane < 8) {
-                        float* const dst = &sm->scales[slot][lane];
-                        if (id >= 0) {
-                            const float* const src = (lane < 4 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + at.h;
-                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-                            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
-                        } else {
-                            *dst = -1.f;
-                            mbar_arrive(full);
+                    const int at0 = page0 - (ids_end - 32);
+                    if (kv == 0) {
+                        // lanes 0-3: K's scales of the chunks, 4-7: V's
+                        const int id = __shfl_sync(0xFFFFFFFFu, ids, at0 + chunk_page);
+                        if (lane < 8) {
+                            float* const dst = &sm->scales[slot][lane];
+                            if (id >= 0) {
+                                const float* const src = (lane < 4 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + h;
+                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+                                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
+                            } else {
+                                *dst = -1.f;
+                                mbar_arrive(full);
+                            }
                         }
                     }
-                    const int mine = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (lane < pages ? lane : 0));
+                    const int mine = __shfl_sync(0xFFFFFFFFu, ids, (at0 + lane) & 31);
                     const unsigned there = __ballot_sync(0xFFFFFFFFu, lane < pages && mine >= 0);
                     if (lane == 0) mbar_arrive_expect_tx(full, (uint32_t)(__popc(there) * box * kD));
                     __syncwarp();
-                    if ((there >> lane) & 1u) {
-                        const int row = (mine * Hkv + at.h) * T + key0 % T;       // (key0 % T is 0 unless a page holds several steps)
-                        tma_load_2d(stage_smem + (kv * kQStages + slot) * kQStage + lane * box * kD, kv == 0 ? &tmap_k : &tmap_v, full, 0, row);
-                    }
+                    if ((there >> lane) & 1u)
+                        tma_load_2d(stage_smem + (kv * kQStages + slot) * kQStage + lane * box * kD, kv == 0 ? &tmap_k : &tmap_v, full, 0,
+                                    (mine * Hkv + h) * T + (key0 & (T - 1)));       // (not 0 only where a page holds several steps)
                     __syncwarp();
                 }
                 if (!ok)       // loads in flight get a bounded chance to land before the CTA retires
-                    for (int i = 0; i < 2 * kQStages && lane == 0; ++i)
-                        for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[0][i], 0) && !mbar_try_wait(&sm->st_full[0][i], 1); ++k) {}
-            } else if (warp == 15) {
-            } else if (warp >= 10) {
+                    for (int i = 0; i < kQStages && lane == 0; ++i)
+                        for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[kv][i], 0) && !mbar_try_wait(&sm->st_full[kv][i], 1); ++k) {}
+            } else if (warp >= 12) {
                 // --------------------------------------------------------------------------------------------------- widening
                 // A lane takes 16 bytes of a row at a time.  Eight lanes take four neighbouring pieces of each of two rows r and r ^ 5:
                 // with the swizzle of either side their reads and their writes all fall into different banks.
-                // K runs two steps ahead of V: K's slot is free once the logits two steps before are there, V's once the product two
-                // steps before is, a softmax later; in step, K of the next step would wait for that too.
-                const int cw = warp - 10;
+                const int cw = warp & 3;
                 const int first_limit = sm->first_limit, len = sm->at.len;
                 const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
-                auto widen = [&](auto kv_c, int t) -> bool {
-                    constexpr int kv = decltype(kv_c)::value;
+                const int kv = warp >= 16;
+                for (int t = 0; t < n_t; ++t) {
                     const int slot = t % kQStages, b = t & 1;
-                    bool there = mbar_wait(&sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, a.status, 262);
-                    if (!__all_sync(0xFFFFFFFFu, there)) return false;
-                    const int key0 = (step0 + t) * kQStep;
-                    const unsigned char* const src = stage_smem + (kv * kQStages + slot) * kQStage;
-                    uint4 w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
-                        const int r = 16 * cw + 8 * (i >> 1) + r8, c = 4 * (i & 1) + piece;
-                        w[i] = *reinterpret_cast<const uint4*>(src + r * kD + ((c ^ r8) << 4));
-                    }
-                    if (kv == 0 && cw == 0 && lane < 4) {
-                        const float* const sc = sm->scales[slot];
-                        const float vs = sc[4 + lane];
-                        const int bits = __float_as_int(vs), e = vs > 0.f ? max((bits >> 23) - 127, -126) : 0;
-                        sm->chunk[t & 7][lane] = make_float4(sc[lane], (float)e, __int_as_float((127 - e) << 23),
-                                                             vs > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f);
-                        if (lane == 0) sm->missing[t & 7] = sc[0] < 0.f || sc[1] < 0.f || sc[2] < 0.f || sc[3] < 0.f;
-                    }
-                    float4 sc = make_float4(0.f, 0.f, 0.f, 1.f);
-                    if (kv == 1) sc = sm->chunk[t & 7][cw];
-                    if (kv == 1 && (key0 + kQStep - 1 > first_limit || sc.x < 0.f)) {
-                        // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in a key that
-                        // only some rows see is taken out, and put into the rows that see it at the end.
-                        bool found = false;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = key0 + 16 * cw + 8 * (i >> 1) + r8;
-                            if (key >= len || sc.x < 0.f) w[i] = make_uint4(0u, 0u, 0u, 0u);
-                            else if (key > first_limit) {
-                                const uint4 nan = make_uint4(nan_bytes(w[i].x), nan_bytes(w[i].y), nan_bytes(w[i].z), nan_bytes(w[i].w));
-                                found |= (nan.x | nan.y | nan.z | nan.w) != 0u;
-                                w[i].x &= ~nan.x; w[i].y &= ~nan.y; w[i].z &= ~nan.z; w[i].w &= ~nan.w;
-                            }
-                        }
-                        if (found) sm->poison = 1;
-                    }
-                    uint32_t h[4][8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        h[i][0] = widen2(w[i].x); h[i][1] = widen2(w[i].x >> 16); h[i][2] = widen2(w[i].y); h[i][3] = widen2(w[i].y >> 16);
-                        h[i][4] = widen2(w[i].z); h[i][5] = widen2(w[i].z >> 16); h[i][6] = widen2(w[i].w); h[i][7] = widen2(w[i].w >> 16);
-                    }
-                    if (kv == 1 && sc.w != 1.f) {       // what V's scale is beside a power of two (nothing, as daf_page_write leaves them)
-                        const __half2 f = __float2half2_rn(sc.w);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const __half2 y = __hmul2(*reinterpret_cast<__half2*>(&h[i][j]), f);
-                                h[i][j] = *reinterpret_cast<const uint32_t*>(&y);
-                            }
-                    }
-                    if (t >= 2) {
+                    bool there = wait_phase(&sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, 262);
+                    // (the constants of a step, written by a warp that widens K)
+                    if (kv == 1 && there) there = wait_phase(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, 275);
+                    if (there && t >= 2) {
                         // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
                         const int u = pair ? t - 2 : (t >> 1) - 1;
-                        uint64_t (*const freed)[2] = kv == 0 ? sm->s_full : sm->pv_done;
-                        if (pair) {
-                            there = mbar_wait(&freed[0][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 263);
-                            if (there) there = mbar_wait(&freed[1][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 264);
-                        } else {
-                            there = mbar_wait(&freed[b][u & 1], (uint32_t)((u >> 1) & 1), abort, a.status, 265);
-                        }
-                        if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                        uint64_t* const freed = (kv == 0 ? sm->s_full[0] : sm->pv_done[0]) + (u & 1);
+                        there = wait_phase(freed + (pair ? 0 : 2 * b), (uint32_t)((u >> 1) & 1), abort, 263);
+                        if (there && pair) there = wait_phase(freed + 2, (uint32_t)((u >> 1) & 1), abort, 264);
                     }
-                    unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot;
+                    if (!__all_sync(0xFFFFFFFFu, there)) break;
+                    unsigned char* const src = stage_smem + (kv * kQStages + slot) * kQStage + (16 * cw + r8) * kD;
+                    float vm = 1.f;
+                    if (kv == 0) {
+                        if (cw == 0 && lane < 4) {
+                            const float* const sc = sm->scales[slot];
+                            const float vs = sc[4 + lane];
+                            const int bits = __float_as_int(vs), e = vs > 0.f ? max((bits >> 23) - 127, -126) : 0;
+                            sm->chunk[t & 7][lane] = make_float4(sc[lane], (float)e, __int_as_float((127 - e) << 23),
+                                                                 vs > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f);
+                            if (lane == 0) sm->missing[t & 7] = sc[0] < 0.f || sc[1] < 0.f || sc[2] < 0.f || sc[3] < 0.f;
+                        }
+                    } else {
+                        const float4 sc = sm->chunk[t & 7][cw];
+                        const int key0 = (step0 + t) * kQStep;
+                        vm = sc.w;
+                        if (key0 + kQStep - 1 > first_limit || sc.x < 0.f) {
+                            // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in
+                            // a key that only some rows see is taken out, and put into the rows that see it at the end.
+#pragma unroll 1
+                            for (int i = 0; i < 4; ++i) {
+                                const int key = key0 + 16 * cw + 8 * (i >> 1) + r8;
+                                uint4* const at = reinterpret_cast<uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
+                                uint4 w = *at;
+                                if (key >= len || sc.x < 0.f) w = make_uint4(0u, 0u, 0u, 0u);
+                                else if (key > first_limit) {
+                                    const uint4 nan = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
+                                    if ((nan.x | nan.y | nan.z | nan.w) != 0u) sm->poison = 1;
+                                    w.x &= ~nan.x; w.y &= ~nan.y; w.z &= ~nan.z; w.w &= ~nan.w;
+                                }
+                                *at = w;      // (each lane's own pieces)
+                            }
+                        }
+                    }
+                    unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot + (16 * cw + r8) * 128;
+#pragma unroll 2
+                    for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
+                        const uint4 w = *reinterpret_cast<const uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
+                        uint32_t h[8] = {widen2(w.x), widen2(w.x >> 16), widen2(w.y), widen2(w.y >> 16),
+                                         widen2(w.z), widen2(w.z >> 16), widen2(w.w), widen2(w.w >> 16)};
+                        unsigned char* const row = dst + (i & 1) * kQSlotHalf + 8 * (i >> 1) * 128;
+                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+                    }
+                    if (vm != 1.f) {       // what V's scale is beside a power of two (nothing, as daf_page_write leaves them): each lane its own pieces
+                        const __half2 f = __float2half2_rn(vm);
+#pragma unroll 1
+                        for (int i = 0; i < 8; ++i) {
+                            __half2* const h = reinterpret_cast<__half2*>(dst + (i & 1) * kQSlotHalf + 8 * ((i >> 1) & 1) * 128 + (((2 * piece + (i >> 2)) ^ r8) << 4));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = 16 * cw + 8 * (i >> 1) + r8;
-                        unsigned char* const row = dst + (i & 1) * kQSlotHalf + r * 128;
-                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(h[i][0], h[i][1], h[i][2], h[i][3]);
-                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(h[i][4], h[i][5], h[i][6], h[i][7]);
+                            for (int j = 0; j < 4; ++j) h[j] = __hmul2(h[j], f);
+                        }
                     }
                     fence_proxy_async();
                     __syncwarp();
@@ -1154,18 +1170,8 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         mbar_arrive(kv == 0 ? &sm->k_full[b] : &sm->v_full[b]);
                         mbar_arrive(&sm->st_empty[kv][slot]);
                     }
-                    return true;
-                };
-                for (int t = -2; t < n_t && ok; ++t) {
-                    if (t + 2 < n_t) ok = widen(std::integral_constant<int, 0>{}, t + 2);
-                    if (ok && t >= 0) {
-                        // (the constants of the step were written by one of these warps)
-                        ok = mbar_wait(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, a.status, 275);
-                        ok = __all_sync(0xFFFFFFFFu, ok);
-                        if (ok) ok = widen(std::integral_constant<int, 1>{}, t);
-                    }
                 }
-            } else if (warp >= 8) {
+            } else if (warp < 10) {
                 // --------------------------------------------------------------------------------------------------- products
                 const int g = warp - 8;
                 const int n_u = pair ? n_t : (n_t - g + 1) / 2;          // steps of this group
@@ -1173,62 +1179,54 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     constexpr uint32_t idesc_qk = make_idesc_f16(128, kQStep, 0), idesc_pv = make_idesc_f16(128, kD, 1);
                     const uint32_t qa = smem_u32(q_smem + (pair ? g : 0) * kQTile);
                     const uint32_t s_col = tmem + (uint32_t)(g * 256), o_col = s_col + 128u;
-                    uint64_t qd[8], kd[2][8], vd[2][4];
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk) {
-                        qd[kk] = make_smem_desc(qa + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQHalf), 16, 1024);
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-                            kd[b][kk] = make_smem_desc(smem_u32(k_smem + (pair ? b : g) * kQSlot) + (uint32_t)((kk & 3) * 32 + (kk >> 2) * kQSlotHalf), 16, 1024);
-                    }
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-                            vd[b][kk] = make_smem_desc(smem_u32(v_smem + (pair ? b : g) * kQSlot) + (uint32_t)kk * 2048u, kQSlotHalf, 1024);
+                    // descriptors of the first 16 channels (or keys); the others, and the other slot's, differ in the address, in 16-byte units
+                    const uint64_t qd = make_smem_desc(qa, 16, 1024);
+                    const uint64_t kd = make_smem_desc(smem_u32(k_smem + (pair ? 0 : g) * kQSlot), 16, 1024);
+                    const uint64_t vd = make_smem_desc(smem_u32(v_smem + (pair ? 0 : g) * kQSlot), kQSlotHalf, 1024);
+                    const uint64_t next_slot = pair ? kQSlot / 16 : 0;
                     auto slot_of = [&](int u) { return pair ? u & 1 : g; };
                     auto use_of = [&](int u) { return pair ? u >> 1 : u; };       // how often the slot was filled before
                     auto issue_qk = [&](int b) {
+                        const uint64_t k0 = kd + (b ? next_slot : 0);
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)
-                            tc_mma_ss(s_col + (uint32_t)(b * kQStep), qd[kk], b ? kd[1][kk] : kd[0][kk], idesc_qk, kk > 0 ? 1u : 0u);
+                            tc_mma_ss(s_col + (uint32_t)(b * kQStep), qd + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQHalf / 16)),
+                                      k0 + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQSlotHalf / 16)), idesc_qk, kk > 0 ? 1u : 0u);
                         tc_commit(&sm->s_full[g][b]);
                     };
-                    ok = mbar_wait(&sm->q_full[pair ? g : 0], 0, abort, a.status, 266);
+                    ok = wait_phase(&sm->q_full[pair ? g : 0], 0, abort, 266);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     for (int u = 0; u < 2 && u < n_u && ok; ++u) {
-                        ok = mbar_wait(&sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 267);
+                        ok = wait_phase(&sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 267);
                         ok = __all_sync(0xFFFFFFFFu, ok);
                         if (!ok) break;
                         tc_fence_after();
                         if (elect_one()) issue_qk(u);
                         __syncwarp();
                     }
-                    auto step = [&](auto half, int u) -> bool {
-                        constexpr int b = decltype(half)::value;
-                        bool there = mbar_wait(&sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, a.status, 268);
-                        if (there) there = mbar_wait(&sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, a.status, 269);
-                        if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                    for (int u = 0; u < n_u && ok; ++u) {
+                        const int b = u & 1;
+                        bool there = wait_phase(&sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 268);
+                        if (there) there = wait_phase(&sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, 269);
+                        ok = __all_sync(0xFFFFFFFFu, there);
+                        if (!ok) break;
                         tc_fence_after();
                         if (elect_one()) {
+                            const uint64_t v0 = vd + (b ? next_slot : 0);
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
-                                tc_mma_ts(o_col, s_col + (uint32_t)(b * kQStep + kk * 8), vd[b][kk], idesc_pv, (u == 0 && kk == 0) ? 0u : 1u);
+                                tc_mma_ts(o_col, s_col + (uint32_t)(b * kQStep + kk * 8), v0 + (uint64_t)(kk * 128), idesc_pv,
+                                          (u == 0 && kk == 0) ? 0u : 1u);
                             tc_commit(&sm->pv_done[g][b]);
                         }
                         __syncwarp();
                         if (u + 2 < n_u) {
-                            there = mbar_wait(&sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, a.status, 270);
-                            if (!__all_sync(0xFFFFFFFFu, there)) return false;
+                            ok = __all_sync(0xFFFFFFFFu, wait_phase(&sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, 270));
+                            if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) issue_qk(b);
                             __syncwarp();
                         }
-                        return true;
-                    };
-                    for (int u = 0; u < n_u && ok; u += 2) {
-                        ok = step(std::integral_constant<int, 0>{}, u);
-                        if (ok && u + 1 < n_u) ok = step(std::integral_constant<int, 1>{}, u + 1);
                     }
                 }
             }
@@ -1238,7 +1236,11 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             if (sm->abort_flag != 0) break;
         }
     }
-    if (threadIdx.x == 0) a.chains[blockIdx.x] = sm->abort_flag == 0 ? sm->chain : ChainEntry{-1, 0, 0, 0};
+    if (threadIdx.x == 0) {
+        const int gave_up = sm->abort_flag;
+        if (gave_up != 0) report_status(a.status, DAF_ERR_TIMEOUT, gave_up, 0);
+        a.chains[blockIdx.x] = gave_up == 0 ? sm->chain : ChainEntry{-1, 0, 0, 0};
+    }
     tc_fence_before();
     __syncthreads();
     if (warp == 8) {
@@ -1381,10 +1383,10 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
         cudaError_t e = cudaFuncSetAttribute(page_decode_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kDecodeSmem + prefix_bytes(kPageMaxSeqs)));
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(page_question_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQuestionSmem + prefix_bytes(kPageMaxSeqs)));
-        // the question kernel's warpgroups trade registers: their shares add up to what 128 a thread give the block at launch
+        // the question kernel's warpgroups trade registers: their shares add up to what 96 a thread give the block at launch
         cudaFuncAttributes fa = {};
         if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, page_question_kernel);
-        if (e == cudaSuccess && fa.numRegs < 128) e = cudaErrorLaunchOutOfResources;
+        if (e == cudaSuccess && fa.numRegs < 96) e = cudaErrorLaunchOutOfResources;
         if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
         if (dev >= 0 && dev < 64) attr_done[dev].store(true, std::memory_order_release);
     }
