@@ -45,13 +45,13 @@ struct ChainEntry {
 // Q K^T, keeps the running maximum and sum, and multiplies P V.
 //   8-bit values are exact in fp16, and so are the query rows once each is scaled by a power of two to a largest magnitude of
 //   2^14 .. 2^15 (elements 2^-31 of that and below are rounded), so the logits are products of the given numbers with fp32 sums.
-//   P goes into the product as fp16 of p * vs * 2^13 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-27 of the
-//   largest and some bits down to 2^-37 (as bf16 it would have 8), while sums of p stay in fp32.
+//   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
+//   largest and some bits down to 2^-34 (as bf16 it would have 8), while sums of p stay in fp32.
 constexpr int kStep = 32;
 constexpr int kDecodeWarps = 8, kDepth = 3;
 constexpr int kBlockRows = 16;
 constexpr int kTile = kStep * kD;                    // 4 KB: K or V of one step
-constexpr float kPExp = 13.f;
+constexpr float kPExp = 9.f;
 
 struct DecodeStage { float ks[2], vs[2]; };          // scales of the step's first and second 16 keys; negative: no such page
 struct DecodeWarp {
@@ -637,7 +637,7 @@ constexpr int kQHalf = kQTile / 2;
 constexpr int kQSlot = kQStep * kD * 2;               // 16 KB: K or V of a step, widened, two 64-column halves
 constexpr int kQSlotHalf = kQSlot / 2;
 constexpr int kQStage = kQStep * kD;                  // 8 KB: the bytes of K or V of a step
-constexpr float kLazy = 2.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
+constexpr float kLazy = 6.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
 
 struct QuestionSmem {
     uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V]
@@ -652,6 +652,7 @@ struct QuestionSmem {
     uint32_t tmem_base;
     int abort_flag;
     int used;                       // the barriers have been initialised
+    int go[2][2];                   // [K, V][step mod 2] what the polling warp found
     int poison;                     // a NaN was taken out of a value that some rows must not see
     // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
     Place at;
@@ -1100,17 +1101,23 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const int kv = warp >= 16;
                 for (int t = 0; t < n_t; ++t) {
                     const int slot = t % kQStages, b = t & 1;
-                    bool there = wait_phase(&sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, 262);
-                    // (the constants of a step, written by a warp that widens K)
-                    if (kv == 1 && there) there = wait_phase(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, 275);
-                    if (there && t >= 2) {
-                        // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
-                        const int u = pair ? t - 2 : (t >> 1) - 1;
-                        uint64_t* const freed = (kv == 0 ? sm->s_full[0] : sm->pv_done[0]) + (u & 1);
-                        there = wait_phase(freed + (pair ? 0 : 2 * b), (uint32_t)((u >> 1) & 1), abort, 263);
-                        if (there && pair) there = wait_phase(freed + 2, (uint32_t)((u >> 1) & 1), abort, 264);
+                    // one of the four warps polls, the others sleep at a barrier (twelve polling warps took half of the issue slots)
+                    if (cw == 0) {
+                        bool there = wait_phase(&sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, 262);
+                        // (the constants of a step, written by a warp that widens K)
+                        if (kv == 1 && there) there = wait_phase(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, 275);
+                        if (there && t >= 2) {
+                            // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
+                            const int u = pair ? t - 2 : (t >> 1) - 1;
+                            uint64_t* const freed = (kv == 0 ? sm->s_full[0] : sm->pv_done[0]) + (u & 1);
+                            there = wait_phase(freed + (pair ? 0 : 2 * b), (uint32_t)((u >> 1) & 1), abort, 263);
+                            if (there && pair) there = wait_phase(freed + 2, (uint32_t)((u >> 1) & 1), abort, 264);
+                        }
+                        there = __all_sync(0xFFFFFFFFu, there);
+                        if (lane == 0) sm->go[kv][b] = there;
                     }
-                    if (!__all_sync(0xFFFFFFFFu, there)) break;
+                    asm volatile("bar.sync %0, 128;" ::"r"(2 + kv) : "memory");
+                    if (!sm->go[kv][b]) break;
                     unsigned char* const src = stage_smem + (kv * kQStages + slot) * kQStage + (16 * cw + r8) * kD;
                     float vm = 1.f;
                     if (kv == 0) {
