@@ -38,18 +38,19 @@ struct ChainEntry {
 };
 
 // ---------------------------------------------------------------------------------------------------- few rows: warps on their own
-// Rows of a KV head go through the warp-wide matrix instruction in blocks of 16.  (With one token and seven heads a group there
-// are two flops per byte and row: the cache's way from HBM is what counts, not the tensor cores' rate, and a warp that needs
-// nobody else keeps its loads in flight all the time.)  A warp walks its stretch of the work axis in steps of 32 keys: it asks for
-// the tiles of K and V kDepth steps ahead (TMA into a ring of its own, rows of 128 bytes with the 128-byte swizzle), multiplies
-// Q K^T, keeps the running maximum and sum, and multiplies P V.
+// Up to 32 rows of a KV head go through the warp-wide matrix instruction, eight at a time: with keys (and then channels) as its 16
+// rows and query rows as its eight columns, S^T = K Q^T and O^T = V^T P^T, so that one token of a group of up to eight heads wastes
+// nothing, and a widened tile of K or V serves all kN column blocks.  (There are 4 flops per byte and row: the cache's way from HBM
+// is what counts, not the tensor cores' rate, and a warp that needs nobody else keeps its loads in flight all the time.)  A warp
+// walks its stretch of the work axis in steps of 32 keys: it asks for the tiles of K and V kDepth steps ahead (TMA into a ring of
+// its own, rows of 128 bytes with the 128-byte swizzle), multiplies, keeps the running maximum and sum, and multiplies again.
 //   8-bit values are exact in fp16, and so are the query rows once each is scaled by a power of two to a largest magnitude of
 //   2^14 .. 2^15 (elements 2^-31 of that and below are rounded), so the logits are products of the given numbers with fp32 sums.
 //   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
 //   largest and some bits down to 2^-34 (as bf16 it would have 8), while sums of p stay in fp32.
 constexpr int kStep = 32;
 constexpr int kDecodeWarps = 8, kDepth = 3;
-constexpr int kBlockRows = 16;
+constexpr int kMostBlocks = 4;                       // column blocks of eight rows
 constexpr int kTile = kStep * kD;                    // 4 KB: K or V of one step
 constexpr float kPExp = 9.f;
 
@@ -58,10 +59,10 @@ struct DecodeWarp {
     uint64_t full[kDepth];
     DecodeStage sc[kDepth];
 };
-constexpr int kPieceFloats = kBlockRows * kD + 2 * kBlockRows;       // an unfinished segment's rows, maxima and sums
+__host__ __device__ constexpr int piece_floats(int rows) { return rows * kD + 2 * rows; }       // an unfinished segment's rows, maxima and sums
 constexpr size_t kRingBytes = (size_t)kDecodeWarps * kDepth * 2 * kTile;
 constexpr size_t kDecodeSmem = 1024 + kRingBytes + sizeof(DecodeWarp) * kDecodeWarps;
-static_assert(kDecodeWarps * kPieceFloats * sizeof(float) <= kRingBytes, "the pieces take the ring's place at the end");
+static_assert(kDecodeWarps * piece_floats(8 * kMostBlocks) * sizeof(float) <= kRingBytes, "the pieces take the ring's place at the end");
 
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
     asm volatile(
@@ -83,6 +84,11 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {           // an 8 x 8 matrix of 16-bit elements, two neighbours a lane
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+    return d;
 }
 __device__ __forceinline__ uint32_t widen2(uint32_t two_bytes) {       // two 8-bit values -> two fp16
     uint32_t d;
@@ -143,6 +149,13 @@ __device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, int* 
     __syncthreads();
 }
 
+// Quotients on the work axis: the axis is seldom longer than 32 bits, and a division of 64 bits takes some 300 cycles.
+__device__ __forceinline__ long long axis_div(long long x, long long y) {
+    return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+}
+// Where CTA c's stretch begins when `ctas` of them share `total`: floor(c total / ctas).
+__device__ __forceinline__ long long cta_begin(long long c, long long total, long long ctas) { return axis_div(c * total, ctas); }
+
 template <int kW>
 __device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* pre, Place& x) {
     x.step = 0;
@@ -174,12 +187,12 @@ __device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre,
     x.n_steps = pre[lo + 1] - pre[lo];
     long long rest = at - pre[lo] * per;
     const long long head = (long long)x.n_steps * a.units;
-    x.h = (int)(rest / head);
+    x.h = (int)axis_div(rest, head);
     rest -= x.h * head;
-    x.block = (int)(rest / ((long long)kW * x.n_steps));
+    x.block = kW == 1 && a.units == 1 ? 0 : (int)axis_div(rest, (long long)kW * x.n_steps);
     x.width = min(kW, a.units - kW * x.block);
     rest -= (long long)x.block * kW * x.n_steps;
-    x.step = (int)((rest + x.width - 1) / x.width);
+    x.step = kW == 1 ? (int)rest : (int)((rest + x.width - 1) >> (x.width - 1));       // (a block's width is 1 or 2)
     if (x.step == x.n_steps) next_segment<kW>(a, pre, x);
     return x;
 }
@@ -191,9 +204,9 @@ __device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* p
 }
 // The CTA whose stretch holds axis position `at` when `ctas` of them share `total`.
 __device__ __forceinline__ int cta_of(long long at, long long total, long long ctas) {
-    long long c = min(at * ctas / total, ctas - 1);
-    while (c + 1 < ctas && (c + 1) * total / ctas <= at) ++c;
-    while (c > 0 && c * total / ctas > at) --c;
+    long long c = min(axis_div(at * ctas, total), ctas - 1);
+    while (c + 1 < ctas && cta_begin(c + 1, total, ctas) <= at) ++c;
+    while (c > 0 && cta_begin(c, total, ctas) > at) --c;
     return (int)c;
 }
 
@@ -207,20 +220,22 @@ __device__ __forceinline__ float partial_weight(float2 ml, float mx) {
     return ml.y == 0.f ? 0.f : (ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - mx));
 }
 
+template <int kN>
 __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
 page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
+    constexpr int kRows = 8 * kN, kPiece = piece_floats(kRows);
     extern __shared__ unsigned char decode_smem_raw[];
     unsigned char* const smem = decode_smem_raw + ((1024u - (smem_u32(decode_smem_raw) & 1023u)) & 1023u);      // (stays a shared address to the compiler)
     DecodeWarp* const warps = reinterpret_cast<DecodeWarp*>(smem + kRingBytes);
     int* const pre = reinterpret_cast<int*>(warps + kDecodeWarps);
     __shared__ int warp_sums[kDecodeWarps];
     __shared__ int abort_flag;
-    __shared__ int piece_kind[2 * kDecodeWarps];         // see below
-    __shared__ int4 piece_seg[2 * kDecodeWarps];
+    __shared__ int piece_kind[2 * kDecodeWarps];         // of each warp, parked and last: 1 there, 2 begins its segment, 4 ends it
+    __shared__ int2 piece_seg[2 * kDecodeWarps];         // (b, h)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     DecodeWarp& me = warps[warp];
-    unsigned char* const ring = smem + (size_t)warp * (kDepth * 2 * kTile);
+    unsigned char* const ring = smem + warp * (kDepth * 2 * kTile);
     if (lane == 0) {
         for (int s = 0; s < kDepth; ++s) mbar_init(&me.full[s], 5);      // one arrival with the byte count, four with the scales
         mbar_fence_init();
@@ -234,39 +249,38 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     pdl_wait();
     pdl_launch_dependents();
     sum_steps<kDecodeWarps * 32>(a, kStep, pre, warp_sums);
-    const long long total = (long long)pre[a.n] * a.p.Hkv * a.units;
+    const long long total = (long long)pre[a.n] * a.p.Hkv;
     // CTAs that take part: no more than give each of its warps a step
     const long long ctas = min((long long)gridDim.x, (total + kDecodeWarps - 1) / kDecodeWarps);
-    const long long cta_lo = min((long long)blockIdx.x, ctas) * total / ctas, cta_hi = min((long long)blockIdx.x + 1, ctas) * total / ctas;
-    const long long span = cta_hi - cta_lo;
+    const long long cta_lo = cta_begin(min((long long)blockIdx.x, ctas), total, ctas);
+    const long long span = cta_begin(min((long long)blockIdx.x + 1, ctas), total, ctas) - cta_lo;
     const long long lo = cta_lo + warp * span / kDecodeWarps, hi = cta_lo + (warp + 1) * span / kDecodeWarps;
 
-    const int T = a.p.T, Hkv = a.p.Hkv;
-    const int box = min(T, kStep);               // keys of one copy
+    const int T = a.p.T, Hkv = a.p.Hkv, page_bits = 31 - __clz(T);
+    const uint32_t box_bytes = (uint32_t)(min(T, kStep) * kD);
     volatile int* const abort = &abort_flag;
+    Place at = {};
+    if (lo < hi) at = place_at<1>(a, pre, lo);
     // ---- the loads run ahead of the products with a place of their own
-    Place ahead = {};
+    Place ahead = at;
     long long ahead_at = lo;
-    int ids = -1, ids_first = -1;                // page numbers of 32 pages of the place's sequence, one a lane
+    int ids = -1, ids_first = -64;               // page numbers of 32 pages of the place's sequence, one a lane
     auto issue = [&](int slot) {
-        const int key0 = ahead.step * kStep;
-        const int page0 = key0 / T;
-        if (ids_first < 0 || page0 < ids_first || page0 + 1 >= ids_first + 32) {
+        const int key0 = ahead.step * kStep, page0 = key0 >> page_bits;
+        if ((unsigned)(page0 - ids_first) >= 31u) {
             ids_first = page0;
             const int j = page0 + lane;
-            ids = j < a.p.max_pages && (long long)j * T < ahead.len ? __ldg(a.table + (size_t)ahead.seq * a.p.max_pages + j) : -1;
+            const bool needed = j < a.p.max_pages && (j << page_bits) < ahead.len;
+            ids = needed ? __ldg(a.table + (size_t)ahead.seq * a.p.max_pages + j) : -1;
             if ((unsigned)ids >= (unsigned)a.p.n_pages) {
-                if ((long long)j * T < ahead.len && ahead.h == 0 && ahead.block == 0) report_status(a.status, DAF_ERR_BOUNDS, 250, ids);
+                if (needed && ahead.h == 0) report_status(a.status, DAF_ERR_BOUNDS, 250, ids);
                 ids = -1;
             }
         }
-        const int id0 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first);
-        const int id1 = T >= kStep ? id0 : __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + 1);
-        unsigned char* const k_dst = ring + slot * 2 * kTile;
-        unsigned char* const v_dst = k_dst + kTile;
+        const int id0 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first), id1 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + 1);
+        const int id = (lane & 1) && T < kStep ? id1 : id0;
         if (lane < 4) {
             // lanes 0, 1: K's scale of the first and second half; 2, 3: V's
-            const int id = lane & 1 ? id1 : id0;
             float* const dst = lane < 2 ? &me.sc[slot].ks[lane] : &me.sc[slot].vs[lane - 2];
             if (id >= 0) {
                 const float* const src = (lane < 2 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + ahead.h;
@@ -277,169 +291,167 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 mbar_arrive(&me.full[slot]);
             }
         }
-        if (lane == 0) {
-            const int copies = (id0 >= 0 ? 1 : 0) + (T < kStep && id1 >= 0 ? 1 : 0);
-            mbar_arrive_expect_tx(&me.full[slot], (uint32_t)(copies * 2 * box * kD));
-            if (id0 >= 0) {
-                const int row = (id0 * Hkv + ahead.h) * T + key0 % T;
-                tma_load_2d(k_dst, &tmap_k, &me.full[slot], 0, row);
-                tma_load_2d(v_dst, &tmap_v, &me.full[slot], 0, row);
-            }
-            if (T < kStep && id1 >= 0) {
-                const int row = (id1 * Hkv + ahead.h) * T;
-                tma_load_2d(k_dst + box * kD, &tmap_k, &me.full[slot], 0, row);
-                tma_load_2d(v_dst + box * kD, &tmap_v, &me.full[slot], 0, row);
-            }
+        // lanes 0 and 1 copy a box of K and of V each (the second only where the step takes two pages)
+        const bool copies = id >= 0 && (lane == 0 || (lane == 1 && T < kStep));
+        const unsigned boxes = __popc(__ballot_sync(0xFFFFFFFFu, copies));
+        if (lane == 0) mbar_arrive_expect_tx(&me.full[slot], 2u * boxes * box_bytes);
+        __syncwarp();
+        if (copies) {
+            unsigned char* const dst = ring + slot * 2 * kTile + lane * box_bytes;
+            const int row = ((id * Hkv + ahead.h) << page_bits) + (key0 & (T - 1));      // (a second box begins its page: T is 16 then)
+            tma_load_2d(dst, &tmap_k, &me.full[slot], 0, row);
+            tma_load_2d(dst + kTile, &tmap_v, &me.full[slot], 0, row);
         }
         __syncwarp();
         ++ahead_at;
         if (++ahead.step == ahead.n_steps) {
             next_segment<1>(a, pre, ahead);
-            ids_first = -1;
+            ids_first = -64;
         }
     };
-    Place at = {};
-    if (lo < hi) {
-        at = place_at<1>(a, pre, lo);
-        ahead = at;
+    if (lo < hi)
         for (int s = 0; s < kDepth && ahead_at < hi; ++s) issue(s);
-    }
     int slot = 0;
     uint32_t phase = 0;
-    bool ok = true;
-    bool tail = false;
-    float o[16][4], m[2], l[2];
+    bool ok = true, tail = false;
+    float o[kN][8][4];       // [column block][16 channels]: channels 16 c + 2 g and + 1 of rows 2 t (elements 0, 2) and 2 t + 1 (1, 3)
+    float m[kN][2], l[kN][2];
     for (long long x = lo; x < hi && ok;) {
         // ---- a segment, or the stretch of it that is this warp's
         const int first_step = at.step;
-        const int r0 = at.block * kBlockRows, n_rows = min(kBlockRows, a.rows - r0);
-        const int rg[2] = {r0 + g, r0 + g + 8};
-        int limit[2];                      // last key each of this thread's two rows sees
-        uint32_t qf[8][4];
-        float cs[2];
-        {
-            uint32_t w[2][16];             // four consecutive channels of each k-step
+        uint32_t qf[kN][8][2];
+        float cs[kN][2];                   // factors of the logits of this thread's rows
+        int limit[kN][2];                  // last key each of them sees
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const bool there = rg[i] < a.rows;
-                const int tok = rg[i] / a.G, head = at.h * a.G + rg[i] % a.G;
-                limit[i] = there ? at.len - a.L_q + tok : -1;
-                const uint2* const src = reinterpret_cast<const uint2*>(a.q + (((size_t)at.b * a.L_q + tok) * a.Hq + head) * kD) + t;
-                uint32_t big = 0;
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    const uint2 v = there ? __ldg(src + kk * 4) : make_uint2(0u, 0u);
-                    w[i][2 * kk] = v.x; w[i][2 * kk + 1] = v.y;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const uint32_t bits = ((u & 2 ? v.y : v.x) >> (16 * (u & 1))) & 0x7FFFu;
-                        big = max(big, bits < 0x7F80u ? bits : 0u);
-                    }
-                }
-                big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
-                big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
-                const int e = max((int)(big >> 7) - 127, -100);
-                const float up = __int_as_float((14 - e + 127) << 23);
-                cs[i] = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    w[i][j] = pack_f16(__uint_as_float(w[i][j] << 16) * up, __uint_as_float(w[i][j] & 0xFFFF0000u) * up);
-            }
+        for (int n = 0; n < kN; ++n) {
+            const int row = 8 * n + g;
+            const bool there = row < a.rows;
+            const uint2* const src = reinterpret_cast<const uint2*>(a.q + (((size_t)at.b * a.L_q + row / a.G) * a.Hq + at.h * a.G + row % a.G) * kD) + t;
+            uint32_t big = 0;
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
-                qf[kk][0] = w[0][2 * kk]; qf[kk][1] = w[1][2 * kk]; qf[kk][2] = w[0][2 * kk + 1]; qf[kk][3] = w[1][2 * kk + 1];
+                const uint2 v = there ? __ldg(src + kk * 4) : make_uint2(0u, 0u);
+                qf[n][kk][0] = v.x; qf[n][kk][1] = v.y;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t bits = ((u & 2 ? v.y : v.x) >> (16 * (u & 1))) & 0x7FFFu;
+                    big = max(big, bits < 0x7F80u ? bits : 0u);
+                }
             }
+            big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
+            big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
+            const int e = max((int)(big >> 7) - 127, -100);
+            const float up = __int_as_float((14 - e + 127) << 23), back = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    qf[n][kk][j] = pack_f16(__uint_as_float(qf[n][kk][j] << 16) * up, __uint_as_float(qf[n][kk][j] & 0xFFFF0000u) * up);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int mine = 8 * n + 2 * t + j;
+                cs[n][j] = __shfl_sync(0xFFFFFFFFu, back, 4 * (2 * t + j));
+                limit[n][j] = mine < a.rows ? at.len - a.L_q + mine / a.G : -1;
+                m[n][j] = -INFINITY;
+                l[n][j] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) o[n][c][u] = 0.f;
         }
-        const int first_limit = at.len - a.L_q + r0 / a.G;       // of the block's rows
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-        m[0] = m[1] = -INFINITY;
-        l[0] = l[1] = 0.f;
+        const int first_limit = at.len - a.L_q;       // of the first row
         for (; at.step < at.n_steps && x < hi; ++at.step, ++x) {
             ok = mbar_wait(&me.full[slot], phase, abort, a.status, 251);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
-            const uint32_t k_at = smem_u32(ring + slot * 2 * kTile), v_at = k_at + kTile;
+            const uint32_t k_at = smem_u32(ring) + (uint32_t)(slot * 2 * kTile), v_at = k_at + kTile;
             const DecodeStage sc = me.sc[slot];
             const int key0 = at.step * kStep;
-            // logits: 32 keys in four tiles of eight
-            float s[4][4];
+            // S^T: 32 keys in two tiles of 16.  A lane's four bytes of a key are four neighbouring channels: two k-slots and, eight
+            // further, two more (the order of the channels within a k-step is free, and Q's fragments have it too).
+            float s[kN][2][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int n = 0; n < kN; ++n)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) s[j][u] = 0.f;
-                const uint32_t row = k_at + (uint32_t)((8 * j + (lane & 7)) * kD);
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t w[4];
-                    ldsm4(w, row + (uint32_t)((((lane >> 3) + 4 * half) ^ (lane & 7)) << 4));
+                    for (int u = 0; u < 4; ++u) s[n][i][u] = 0.f;
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) mma16816(s[j], qf[4 * half + u], widen2(w[u]), widen2(w[u] >> 16));
-                }
+            for (int c = 0; c < 8; c += 2) {
+                uint32_t w[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)      // matrices: keys 0-7 and 8-15 of channels 16 c .., then of 16 (c + 1) ..
+                    ldsm4(w[i], k_at + (uint32_t)((16 * i + (lane & 15)) * kD + (((c + (lane >> 4)) ^ (lane & 7)) << 4)));
+#pragma unroll
+                for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t f[4] = {widen2(w[i][2 * cc]), widen2(w[i][2 * cc + 1]), widen2(w[i][2 * cc] >> 16), widen2(w[i][2 * cc + 1] >> 16)};
+#pragma unroll
+                        for (int n = 0; n < kN; ++n) mma16816(s[n][i], f, qf[n][c + cc][0], qf[n][c + cc][1]);
+                    }
             }
             // a step with keys that some row does not see, or without a page
             const bool odd = key0 + kStep - 1 > first_limit || sc.ks[0] < 0.f || sc.ks[1] < 0.f;
-            float top[2] = {-INFINITY, -INFINITY};
-            int ve[2];
-            float vm[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {      // vs = vm * 2^ve, 1 <= vm < 2
-                const int bits = __float_as_int(sc.vs[j]);
-                ve[j] = sc.vs[j] > 0.f ? (bits >> 23) - 127 : 0;
-                vm[j] = sc.vs[j] > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float ks = sc.ks[j >> 1], shift = (float)ve[j >> 1];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    s[j][u] = s[j][u] * (cs[u >> 1] * ks) + shift;
-                    if (odd && (key0 + 8 * j + 2 * t + (u & 1) > limit[u >> 1] || ks < 0.f)) s[j][u] = -INFINITY;
-                    top[u >> 1] = fmaxf(top[u >> 1], s[j][u]);
-                }
-            }
-            float used[2], alpha[2];
+            float shift[2], vm[2], back[2];      // vs = vm * 2^shift, 1 <= vm < 2; back = 2^-shift: the sums are of p itself
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 1));
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 2));
-                const float now = fmaxf(m[i], top[i]);
-                alpha[i] = m[i] == now ? 1.f : fast_exp2(m[i] - now);      // (2^-inf = 0 at the first key)
-                used[i] = now == -INFINITY ? 0.f : now - kPExp;
-                m[i] = now;
+                const int bits = __float_as_int(sc.vs[i]), e = sc.vs[i] > 0.f ? max((bits >> 23) - 127, -126) : 0;
+                shift[i] = (float)e;
+                back[i] = __int_as_float((127 - e) << 23);
+                vm[i] = sc.vs[i] > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f;
             }
-            if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+            uint32_t pf[kN][2][2];               // P^T: [16 keys][their halves], two keys of row g
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    o[i][0] *= alpha[0]; o[i][1] *= alpha[0];
-                    o[i][2] *= alpha[1]; o[i][3] *= alpha[1];
+            for (int n = 0; n < kN; ++n) {
+                float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        s[n][i][u] = fmaf(s[n][i][u], cs[n][u & 1] * sc.ks[i], shift[i]);
+                        if (odd && (key0 + 16 * i + 8 * (u >> 1) + g > limit[n][u & 1] || sc.ks[i] < 0.f)) s[n][i][u] = -INFINITY;
+                        top[u & 1] = fmaxf(top[u & 1], s[n][i][u]);
+                    }
+                float used[2], alpha[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], d));
+                    const float now = fmaxf(m[n][j], top[j]);
+                    alpha[j] = m[n][j] == now ? 1.f : fast_exp2(m[n][j] - now);      // (2^-inf = 0 at the first key)
+                    used[j] = now == -INFINITY ? 0.f : now - kPExp;
+                    m[n][j] = now;
                 }
-                l[0] *= alpha[0]; l[1] *= alpha[1];
-            }
-            uint32_t pf[2][4];
+                if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float back = __int_as_float((127 - max(ve[j >> 1], -126)) << 23);     // 2^-ve: the sums are of p itself
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float e = fast_exp2(s[j][u] - used[u >> 1]);
-                    l[u >> 1] += e * back;
-                    s[j][u] = e * vm[j >> 1];
+                    for (int c = 0; c < 8; ++c) {
+                        o[n][c][0] *= alpha[0]; o[n][c][2] *= alpha[0];
+                        o[n][c][1] *= alpha[1]; o[n][c][3] *= alpha[1];
+                    }
+                    l[n][0] *= alpha[0]; l[n][1] *= alpha[1];
                 }
-                pf[j >> 1][2 * (j & 1)] = pack_f16(s[j][0], s[j][1]);
-                pf[j >> 1][2 * (j & 1) + 1] = pack_f16(s[j][2], s[j][3]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const float e = fast_exp2(s[n][i][u] - used[u & 1]);
+                        l[n][u & 1] = fmaf(e, back[i], l[n][u & 1]);
+                        s[n][i][u] = e * vm[i];
+                    }
+                    pf[n][i][0] = transpose8(pack_f16(s[n][i][0], s[n][i][1]));
+                    pf[n][i][1] = transpose8(pack_f16(s[n][i][2], s[n][i][3]));
+                }
             }
-            // O += P V: channels 16 c + 2 n and 16 c + 2 n + 1 are columns n of two products
+            // O^T += V^T P^T: channels 16 c + 2 r and 16 c + 2 r + 1 are rows r and r + 8 of the instruction
             bool poison = false;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
 #pragma unroll
                 for (int c = 0; c < 8; c += 2) {
-                    const int row = 16 * i + 8 * ((lane >> 3) & 1) + (lane & 7);
                     uint32_t w[4];
-                    ldsm4_t(w, v_at + (uint32_t)(row * kD + (((c + (lane >> 4)) ^ (lane & 7)) << 4)));
+                    ldsm4_t(w, v_at + (uint32_t)((16 * i + (lane & 15)) * kD + (((c + (lane >> 4)) ^ (lane & 7)) << 4)));
                     if (odd) {
                         // Keys that no row of the sequence sees, or of no page: whatever lies there counts as zero.  Keys that
                         // some rows see: a NaN must not reach the others, so it is taken out here and put into the rows that
@@ -460,8 +472,9 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
                     for (int cc = 0; cc < 2; ++cc) {
                         const uint32_t w0 = __byte_perm(w[2 * cc], 0u, 0x3120), w1 = __byte_perm(w[2 * cc + 1], 0u, 0x3120);
-                        mma16816(o[2 * (c + cc)], pf[i], widen2(w0), widen2(w1));
-                        mma16816(o[2 * (c + cc) + 1], pf[i], widen2(w0 >> 16), widen2(w1 >> 16));
+                        const uint32_t f[4] = {widen2(w0), widen2(w0 >> 16), widen2(w1), widen2(w1 >> 16)};
+#pragma unroll
+                        for (int n = 0; n < kN; ++n) mma16816(o[n][c + cc], f, pf[n][i][0], pf[n][i][1]);
                     }
                 }
             }
@@ -471,13 +484,12 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     if (key <= first_limit || key >= at.len) continue;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        const uint32_t w = nan_bytes(*reinterpret_cast<const uint32_t*>(ring + slot * 2 * kTile + kTile + j * kD + ((c ^ (j & 7)) << 4) + 4 * t));
+                        const uint32_t w = nan_bytes(*reinterpret_cast<const uint16_t*>(ring + slot * 2 * kTile + kTile + j * kD + ((c ^ (j & 7)) << 4) + 2 * g));
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            if ((w >> (8 * u)) & 1u) {
-                                if (key <= limit[0]) o[2 * c + (u & 1)][u >> 1] = __int_as_float(0x7FC00000);
-                                if (key <= limit[1]) o[2 * c + (u & 1)][2 + (u >> 1)] = __int_as_float(0x7FC00000);
-                            }
+                        for (int n = 0; n < kN; ++n)
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                if (((w >> (8 * (u >> 1))) & 1u) && key <= limit[n][u & 1]) o[n][c][u] = __int_as_float(0x7FC00000);
                     }
                 }
             }
@@ -487,49 +499,52 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         if (!ok) break;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 2);
-        }
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
         const bool begins = first_step == 0, ends = at.step == at.n_steps;
         if (begins && ends) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (rg[i] >= a.rows) continue;
-                const int tok = rg[i] / a.G, head = at.h * a.G + rg[i] % a.G;
-                const float inv = row_inverse(l[i]);
-                uint2* const dst = reinterpret_cast<uint2*>(a.out + (((size_t)at.b * a.L_q + tok) * a.Hq + head) * kD) + t;
+            for (int n = 0; n < kN; ++n)
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    dst[c * 4] = make_uint2(pack_bf16(o[2 * c][2 * i] * inv, o[2 * c + 1][2 * i] * inv),
-                                            pack_bf16(o[2 * c][2 * i + 1] * inv, o[2 * c + 1][2 * i + 1] * inv));
-                if (a.lse != nullptr && t == 0)
-                    a.lse[((size_t)at.b * a.Hq + head) * a.L_q + tok] = row_lse(m[i], l[i]);
-            }
-        } else if (ends) {
-            // the end of a segment that begins in front of this warp's stretch: parked in global memory, since the ring is in use
-            float* const dst = a.part_o + ((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + warp) * (kBlockRows * kD);
-            float2* const ml = a.part_ml + ((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + warp) * kBlockRows;
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 8 * n + 2 * t + j;
+                    if (row >= a.rows) continue;
+                    const int tok = row / a.G, head = at.h * a.G + row % a.G;
+                    const float inv = row_inverse(l[n][j]);
+                    uint32_t* const dst = reinterpret_cast<uint32_t*>(a.out + (((size_t)at.b * a.L_q + tok) * a.Hq + head) * kD) + g;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (g + 8 * i >= n_rows) continue;
+                    for (int c = 0; c < 8; ++c) dst[8 * c] = pack_bf16(o[n][c][j] * inv, o[n][c][2 + j] * inv);
+                    if (a.lse != nullptr && g == 0) a.lse[((size_t)at.b * a.Hq + head) * a.L_q + tok] = row_lse(m[n][j], l[n][j]);
+                }
+        } else if (x < hi) {
+            // The end of a segment that begins in front of this warp's stretch, with more behind it: parked in global memory, since the
+            // ring is in use.
+            const size_t set = (size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + warp;
+            float* const dst = a.part_o + set * (kRows * kD);
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    *reinterpret_cast<float4*>(dst + (g + 8 * i) * kD + c * 16 + 4 * t) =
-                        make_float4(o[2 * c][2 * i], o[2 * c + 1][2 * i], o[2 * c][2 * i + 1], o[2 * c + 1][2 * i + 1]);
-                if (t == 0) ml[g + 8 * i] = make_float2(m[i], l[i]);
-            }
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 8 * n + 2 * t + j;
+                    if (row >= a.rows) continue;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        *reinterpret_cast<float2*>(dst + row * kD + 16 * c + 2 * g) = make_float2(o[n][c][j], o[n][c][2 + j]);
+                    if (g == 0) a.part_ml[set * kRows + row] = make_float2(m[n][j], l[n][j]);
+                }
             if (lane == 0) {
                 piece_kind[2 * warp] = 1 | 4;
-                piece_seg[2 * warp] = make_int4(at.b, at.h, at.block, at.n_steps);
+                piece_seg[2 * warp] = make_int2(at.b, at.h);
             }
         } else {
             tail = true;           // stays in registers until the ring is free
             if (lane == 0) {
-                piece_kind[2 * warp + 1] = 1 | (begins ? 2 : 0);
-                piece_seg[2 * warp + 1] = make_int4(at.b, at.h, at.block, at.n_steps);
+                piece_kind[2 * warp + 1] = 1 | (begins ? 2 : 0) | (ends ? 4 : 0);
+                piece_seg[2 * warp + 1] = make_int2(at.b, at.h);
             }
-            break;
         }
         if (x < hi) next_segment<1>(a, pre, at);
     }
@@ -545,79 +560,77 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // ---- the warps' unfinished pieces: neighbours of one segment are merged; what is still unfinished is the CTA's
     float* const pieces = reinterpret_cast<float*>(smem);
     if (tail) {
-        float* const dst = pieces + warp * kPieceFloats;
+        float* const dst = pieces + warp * kPiece;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-                *reinterpret_cast<float4*>(dst + (g + 8 * i) * kD + c * 16 + 4 * t) =
-                    make_float4(o[2 * c][2 * i], o[2 * c + 1][2 * i], o[2 * c][2 * i + 1], o[2 * c + 1][2 * i + 1]);
-            if (t == 0) reinterpret_cast<float2*>(dst + kBlockRows * kD)[g + 8 * i] = make_float2(m[i], l[i]);
-        }
+            for (int j = 0; j < 2; ++j) {
+                const int row = 8 * n + 2 * t + j;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    *reinterpret_cast<float2*>(dst + row * kD + 16 * c + 2 * g) = make_float2(o[n][c][j], o[n][c][2 + j]);
+                if (g == 0) reinterpret_cast<float2*>(dst + kRows * kD)[row] = make_float2(m[n][j], l[n][j]);
+            }
     }
     __syncthreads();
-    int chain_kind = 0;            // 1: the CTA begins a segment that it does not end
-    int4 chain_seg = make_int4(0, 0, 0, 0);
-    for (int i0 = 0; i0 < 2 * kDecodeWarps;) {
-        if (piece_kind[i0] == 0) { ++i0; continue; }
-        // pieces i0 .. i1 - 1 are of one segment: the first begins it or lies first in the CTA, the last ends it or lies last
-        int i1 = i0, last = i0;
-        for (;;) {
-            last = i1++;
-            if (piece_kind[last] & 4) break;
-            while (i1 < 2 * kDecodeWarps && piece_kind[i1] == 0) ++i1;
-            if (i1 == 2 * kDecodeWarps) break;
-        }
-        const bool begins = (piece_kind[i0] & 2) != 0, ends = (piece_kind[last] & 4) != 0;
-        const int4 seg = piece_seg[i0];
-        const int r0 = seg.z * kBlockRows, n_rows = min(kBlockRows, a.rows - r0);
-        for (int r = warp; r < n_rows; r += kDecodeWarps) {
-            float mx = -INFINITY;
-            auto ml_of = [&](int i) {
-                return (i & 1) ? reinterpret_cast<const float2*>(pieces + (i >> 1) * kPieceFloats + kBlockRows * kD)[r]
-                               : __ldcg(a.part_ml + ((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kBlockRows + r);
-            };
-            for (int i = i0; i < i1; ++i)
-                if (piece_kind[i] != 0) mx = fmaxf(mx, ml_of(i).x);
+    const int kind = lane < 2 * kDecodeWarps ? piece_kind[lane] : 0;
+    unsigned left = __ballot_sync(0xFFFFFFFFu, kind != 0);
+    const unsigned beginning = __ballot_sync(0xFFFFFFFFu, (kind & 2) != 0), ending = __ballot_sync(0xFFFFFFFFu, (kind & 4) != 0);
+    ChainEntry chain = {-1, 0, 0, 0};
+    while (left != 0) {
+        // pieces of one segment: from the first left to the one that ends the segment, or to the last
+        const int first = __ffs(left) - 1;
+        const unsigned ends_at = left & ending;
+        const unsigned group = ends_at != 0 ? left & ((ends_at & (0u - ends_at)) * 2u - 1u) : left;
+        left &= ~group;
+        const bool begins = (beginning >> first) & 1u, ends = ends_at != 0;
+        const int2 seg = piece_seg[first];
+        for (int r = warp; r < a.rows; r += kDecodeWarps) {
+            // lane i knows piece i: odd ones lie here, even ones were parked
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if ((group >> lane) & 1u)
+                ml = (lane & 1) ? reinterpret_cast<const float2*>(pieces + (lane >> 1) * kPiece + kRows * kD)[r]
+                                : __ldcg(a.part_ml + ((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (lane >> 1)) * kRows + r);
+            float mx = ml.x;
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
+            mx = __shfl_sync(0xFFFFFFFFu, mx, 0);
+            const float mine = partial_weight(ml, mx);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             float sum = 0.f;
-            for (int i = i0; i < i1; ++i) {
-                if (piece_kind[i] == 0) continue;
-                const float2 ml = ml_of(i);
-                const float w = partial_weight(ml, mx);
-                const float4 v = (i & 1) ? reinterpret_cast<const float4*>(pieces + (i >> 1) * kPieceFloats + r * kD)[lane]
-                                         : __ldcg(reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kBlockRows + r) * kD) + lane);
-                sum += w * ml.y;
+            for (unsigned rest = group; rest != 0; rest &= rest - 1) {
+                const int i = __ffs(rest) - 1;
+                const float w = __shfl_sync(0xFFFFFFFFu, mine, i);
+                const float4 v = (i & 1) ? reinterpret_cast<const float4*>(pieces + (i >> 1) * kPiece + r * kD)[lane]
+                                         : __ldcg(reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kRows + r) * kD) + lane);
+                sum += w * __shfl_sync(0xFFFFFFFFu, ml.y, i);
                 acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
             }
             if (begins && ends) {
-                const int row = r0 + r, tok = row / a.G, head = seg.y * a.G + row % a.G;
+                const int tok = r / a.G, head = seg.y * a.G + r % a.G;
                 const float inv = row_inverse(sum);
                 reinterpret_cast<uint2*>(a.out + (((size_t)seg.x * a.L_q + tok) * a.Hq + head) * kD)[lane] =
                     make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                if (a.lse != nullptr && lane == 0)
-                    a.lse[((size_t)seg.x * a.Hq + head) * a.L_q + tok] = row_lse(mx, sum);
+                if (a.lse != nullptr && lane == 0) a.lse[((size_t)seg.x * a.Hq + head) * a.L_q + tok] = row_lse(mx, sum);
             } else {
                 const size_t set = (size_t)blockIdx.x * 2 + (begins ? 1 : 0);
-                reinterpret_cast<float4*>(a.part_o + (set * kBlockRows + r) * kD)[lane] = acc;
-                if (lane == 0) a.part_ml[set * kBlockRows + r] = make_float2(mx, sum);
+                reinterpret_cast<float4*>(a.part_o + (set * kRows + r) * kD)[lane] = acc;
+                if (lane == 0) a.part_ml[set * kRows + r] = make_float2(mx, sum);
             }
         }
-        if (begins && !ends) { chain_kind = 1; chain_seg = seg; }
-        i0 = i1;
+        if (begins && !ends) chain = ChainEntry{0, seg.x, seg.y, 0};
     }
     if (threadIdx.x == 0) {
-        ChainEntry e = {-1, 0, 0, 0};
-        if (chain_kind != 0) {
-            const long long seg_end = (long long)pre[chain_seg.x] * Hkv * a.units + ((long long)chain_seg.y * a.units + chain_seg.z + 1) * chain_seg.w;
-            e = ChainEntry{cta_of(seg_end - 1, total, ctas), chain_seg.x, chain_seg.y, chain_seg.z};
+        if (chain.last_cta == 0) {
+            const long long end = (long long)pre[chain.b] * Hkv + (long long)(chain.h + 1) * (pre[chain.b + 1] - pre[chain.b]);
+            chain.last_cta = cta_of(end - 1, total, ctas);
         }
-        a.chains[blockIdx.x] = e;
+        a.chains[blockIdx.x] = chain;
     }
 }
 
 // ---------------------------------------------------------------------------------------------- many rows: tensor memory
-// More than 16 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
+// More than 32 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
 // of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 20 warps:
 //   10, 11  ask for the bytes of K and V (TMA, kQStages steps ahead) and their scales;
 //   12-15, 16-19  widen K's, and V's, to fp16, exactly, into the two-slot rings that the products read (128-byte swizzle).  Each of
@@ -797,7 +810,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     if (threadIdx.x == 0) {
         const long long total = (long long)pre[a.n] * Hkv * a.units;
         const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than four steps of a tile each
-        const long long c_lo = min((long long)blockIdx.x, ctas) * total / ctas, c_hi = min((long long)blockIdx.x + 1, ctas) * total / ctas;
+        const long long c_lo = cta_begin(min((long long)blockIdx.x, ctas), total, ctas), c_hi = cta_begin(min((long long)blockIdx.x + 1, ctas), total, ctas);
         // both ends move up to the next step's begin
         Place at = {};
         sm->x = sm->hi = total;
@@ -1348,17 +1361,18 @@ static int make_pool_map(CUtensorMap* m, const void* base, long long rows, int b
 }
 
 static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+// Column blocks of the kernel of few rows, 0: too many rows for it.
+static int few_blocks(int rows) { return rows <= 8 * kMostBlocks ? (rows + 7) / 8 : 0; }
 // Partial rows: two sets a CTA, and for the kernel of few rows one a warp for the pieces parked on the way.
-static bool few_rows(int rows) { return rows <= kBlockRows; }
-static size_t partial_rows(int ctas, bool few) {
-    return few ? (size_t)ctas * (2 + kDecodeWarps) * kBlockRows : (size_t)ctas * 2 * kQRows;
+static size_t partial_rows(int ctas, int blocks) {
+    return blocks > 0 ? (size_t)ctas * (2 + kDecodeWarps) * 8 * blocks : (size_t)ctas * 2 * kQRows;
 }
 static size_t prefix_bytes(int n) { return ((size_t)n + 1) * sizeof(int); }
 
 size_t page_attn_scratch_bytes(int n, int L_q, int Hq, int Hkv) {
     (void)n;
     const int ctas = num_sms();
-    const size_t rows = partial_rows(ctas, few_rows(L_q * (Hq / Hkv)));
+    const size_t rows = partial_rows(ctas, few_blocks(L_q * (Hq / Hkv)));
     return round256((size_t)ctas * sizeof(ChainEntry)) + round256(rows * sizeof(float2)) + rows * kD * sizeof(float);
 }
 
@@ -1368,14 +1382,15 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     PageAttnArgs a;
     a.p = pool; a.n = n; a.L_q = L_q; a.Hq = Hq; a.G = Hq / pool.Hkv;
     a.rows = L_q * a.G;
-    const bool few = few_rows(a.rows);
+    const int blocks = few_blocks(a.rows);
+    const bool few = blocks > 0;
     a.units = few ? 1 : (a.rows + 127) / 128;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.seqs = seqs; a.lens = lens; a.table = table;
     a.q = reinterpret_cast<const __nv_bfloat16*>(q); a.out = reinterpret_cast<__nv_bfloat16*>(out); a.lse = lse;
     char* at = reinterpret_cast<char*>(scratch);
     a.chains = reinterpret_cast<ChainEntry*>(at); at += round256((size_t)ctas * sizeof(ChainEntry));
-    a.part_ml = reinterpret_cast<float2*>(at); at += round256(partial_rows(ctas, few) * sizeof(float2));
+    a.part_ml = reinterpret_cast<float2*>(at); at += round256(partial_rows(ctas, blocks) * sizeof(float2));
     a.part_o = reinterpret_cast<float*>(at);
     a.status = status;
     const long long rows = (long long)pool.n_pages * pool.Hkv * pool.T;
@@ -1387,7 +1402,10 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64 || !attr_done[dev].load(std::memory_order_acquire)) {
-        cudaError_t e = cudaFuncSetAttribute(page_decode_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kDecodeSmem + prefix_bytes(kPageMaxSeqs)));
+        cudaError_t e = cudaSuccess;
+        for (auto* kernel : {page_decode_kernel<1>, page_decode_kernel<2>, page_decode_kernel<3>, page_decode_kernel<4>})
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kDecodeSmem + prefix_bytes(kPageMaxSeqs)));
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(page_question_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQuestionSmem + prefix_bytes(kPageMaxSeqs)));
         // the question kernel's warpgroups trade registers: their shares add up to what 96 a thread give the block at launch
@@ -1397,11 +1415,12 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
         if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
         if (dev >= 0 && dev < 64) attr_done[dev].store(true, std::memory_order_release);
     }
-    cudaError_t e = few ? launch_kernel(page_decode_kernel, dim3(ctas), dim3(kDecodeWarps * 32), kDecodeSmem + prefix_bytes(n), stream, mk, mv, a)
+    auto* decode = blocks == 1 ? page_decode_kernel<1> : blocks == 2 ? page_decode_kernel<2> : blocks == 3 ? page_decode_kernel<3> : page_decode_kernel<4>;
+    cudaError_t e = few ? launch_kernel(decode, dim3(ctas), dim3(kDecodeWarps * 32), kDecodeSmem + prefix_bytes(n), stream, mk, mv, a)
                         : launch_kernel(page_question_kernel, dim3(ctas), dim3(kQThreads), kQuestionSmem + prefix_bytes(n), stream, mk, mv, a);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
-    e = few ? launch_kernel(page_merge_kernel<4>, dim3(ctas, kBlockRows / 2), dim3(256), 0, stream, a, (int)kBlockRows)
+    e = few ? launch_kernel(page_merge_kernel<4>, dim3(ctas, 4 * blocks), dim3(256), 0, stream, a, 8 * blocks)
             : launch_kernel(page_merge_kernel<1>, dim3(ctas, kQRows / 8), dim3(256), 0, stream, a, (int)kQRows);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
