@@ -42,27 +42,30 @@ struct ChainEntry {
 // rows and query rows as its eight columns, S^T = K Q^T and O^T = V^T P^T, so that one token of a group of up to eight heads wastes
 // nothing, and a widened tile of K or V serves all kN column blocks.  (There are 4 flops per byte and row: the cache's way from HBM
 // is what counts, not the tensor cores' rate, and a warp that needs nobody else keeps its loads in flight all the time.)  A warp
-// walks its stretch of the work axis in steps of 32 keys: it asks for the tiles of K and V kDepth steps ahead (TMA into a ring of
-// its own, rows of 128 bytes with the 128-byte swizzle), multiplies, keeps the running maximum and sum, and multiplies again.
+// walks its stretch of the work axis in steps of 32 keys: it asks for the tiles of K and V some steps ahead (asynchronous 16-byte
+// copies into a ring of its own, whose 16-byte pieces are XOR-ed with the row number so that eight rows of a column lie in
+// different banks), multiplies, keeps the running maximum and sum, and multiplies again.  (Tiled copies were slower here: a warp has
+// to issue them one by one, with everything in uniform registers, and at pages of 16 tokens a step takes four: 1160 clocks a step.)
 //   8-bit values are exact in fp16, and so are the query rows once each is scaled by a power of two to a largest magnitude of
 //   2^14 .. 2^15 (elements 2^-31 of that and below are rounded), so the logits are products of the given numbers with fp32 sums.
 //   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
 //   largest and some bits down to 2^-34 (as bf16 it would have 8), while sums of p stay in fp32.
 constexpr int kStep = 32;
-constexpr int kDecodeWarps = 8, kDepth = 3;
 constexpr int kMostBlocks = 4;                       // column blocks of eight rows
 constexpr int kTile = kStep * kD;                    // 4 KB: K or V of one step
 constexpr float kPExp = 9.f;
-
+// Warps of a CTA (one CTA an SM), and steps a warp asks ahead: as many warps as the registers of one column block leave room for,
+// since each waits on its own chain of products half of the time.
+__host__ __device__ constexpr int decode_warps(int blocks) { return blocks == 1 ? 12 : 8; }
+__host__ __device__ constexpr int decode_depth(int blocks) { return blocks == 1 ? 2 : 3; }
 struct DecodeStage { float ks[2], vs[2]; };          // scales of the step's first and second 16 keys; negative: no such page
-struct DecodeWarp {
-    uint64_t full[kDepth];
-    DecodeStage sc[kDepth];
-};
 __host__ __device__ constexpr int piece_floats(int rows) { return rows * kD + 2 * rows; }       // an unfinished segment's rows, maxima and sums
-constexpr size_t kRingBytes = (size_t)kDecodeWarps * kDepth * 2 * kTile;
-constexpr size_t kDecodeSmem = 1024 + kRingBytes + sizeof(DecodeWarp) * kDecodeWarps;
-static_assert(kDecodeWarps * piece_floats(8 * kMostBlocks) * sizeof(float) <= kRingBytes, "the pieces take the ring's place at the end");
+__host__ __device__ constexpr size_t ring_bytes(int blocks) { return (size_t)decode_warps(blocks) * decode_depth(blocks) * 2 * kTile; }
+__host__ __device__ constexpr size_t decode_smem(int blocks) {
+    return 1024 + ring_bytes(blocks) + (size_t)decode_warps(blocks) * decode_depth(blocks) * sizeof(DecodeStage);
+}
+static_assert(decode_warps(1) * piece_floats(8) * sizeof(float) <= ring_bytes(1) && decode_warps(2) <= 16 &&
+              decode_warps(kMostBlocks) * piece_floats(8 * kMostBlocks) * sizeof(float) <= ring_bytes(kMostBlocks), "the pieces take the ring's place at the end");
 
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
     asm volatile(
@@ -221,30 +224,20 @@ __device__ __forceinline__ float partial_weight(float2 ml, float mx) {
 }
 
 template <int kN>
-__global__ void __launch_bounds__(kDecodeWarps * 32, 1)
-page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
-    constexpr int kRows = 8 * kN, kPiece = piece_floats(kRows);
+__global__ void __launch_bounds__(decode_warps(kN) * 32, 1)
+page_decode_kernel(const PageAttnArgs a) {
+    constexpr int kRows = 8 * kN, kPiece = piece_floats(kRows), kDecodeWarps = decode_warps(kN), kDepth = decode_depth(kN);
     extern __shared__ unsigned char decode_smem_raw[];
     unsigned char* const smem = decode_smem_raw + ((1024u - (smem_u32(decode_smem_raw) & 1023u)) & 1023u);      // (stays a shared address to the compiler)
-    DecodeWarp* const warps = reinterpret_cast<DecodeWarp*>(smem + kRingBytes);
-    int* const pre = reinterpret_cast<int*>(warps + kDecodeWarps);
+    DecodeStage* const stages = reinterpret_cast<DecodeStage*>(smem + ring_bytes(kN));
+    int* const pre = reinterpret_cast<int*>(stages + kDecodeWarps * kDepth);
     __shared__ int warp_sums[kDecodeWarps];
-    __shared__ int abort_flag;
     __shared__ int piece_kind[2 * kDecodeWarps];         // of each warp, parked and last: 1 there, 2 begins its segment, 4 ends it
     __shared__ int2 piece_seg[2 * kDecodeWarps];         // (b, h)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    DecodeWarp& me = warps[warp];
+    DecodeStage* const sc_ring = stages + warp * kDepth;
     unsigned char* const ring = smem + warp * (kDepth * 2 * kTile);
-    if (lane == 0) {
-        for (int s = 0; s < kDepth; ++s) mbar_init(&me.full[s], 5);      // one arrival with the byte count, four with the scales
-        mbar_fence_init();
-    }
-    if (threadIdx.x == 0) {
-        abort_flag = 0;
-        tma_prefetch_desc(&tmap_k);
-        tma_prefetch_desc(&tmap_v);
-    }
     if (threadIdx.x < 2 * kDecodeWarps) piece_kind[threadIdx.x] = 0;
     pdl_wait();
     pdl_launch_dependents();
@@ -257,14 +250,14 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const long long lo = cta_lo + warp * span / kDecodeWarps, hi = cta_lo + (warp + 1) * span / kDecodeWarps;
 
     const int T = a.p.T, Hkv = a.p.Hkv, page_bits = 31 - __clz(T);
-    const uint32_t box_bytes = (uint32_t)(min(T, kStep) * kD);
-    volatile int* const abort = &abort_flag;
     Place at = {};
     if (lo < hi) at = place_at<1>(a, pre, lo);
     // ---- the loads run ahead of the products with a place of their own
     Place ahead = at;
     long long ahead_at = lo;
     int ids = -1, ids_first = -64;               // page numbers of 32 pages of the place's sequence, one a lane
+    const uint32_t ring_at = smem_u32(ring);
+    const uint32_t dst0 = (uint32_t)((lane >> 3) * kD + (((lane & 7) ^ (lane >> 3)) << 4)), dst1 = (uint32_t)((lane >> 3) * kD + 512 + (((lane & 7) ^ (lane >> 3) ^ 4) << 4));
     auto issue = [&](int slot) {
         const int key0 = ahead.step * kStep, page0 = key0 >> page_bits;
         if ((unsigned)(page0 - ids_first) >= 31u) {
@@ -277,30 +270,30 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 ids = -1;
             }
         }
-        const int id0 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first), id1 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + 1);
-        const int id = (lane & 1) && T < kStep ? id1 : id0;
-        if (lane < 4) {
-            // lanes 0, 1: K's scale of the first and second half; 2, 3: V's
-            float* const dst = lane < 2 ? &me.sc[slot].ks[lane] : &me.sc[slot].vs[lane - 2];
-            if (id >= 0) {
-                const float* const src = (lane < 2 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + ahead.h;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&me.full[slot])) : "memory");
-            } else {
-                *dst = -1.f;
-                mbar_arrive(&me.full[slot]);
+        const int id0 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first), id1 = __shfl_sync(0xFFFFFFFFu, ids, page0 - ids_first + (T < kStep ? 1 : 0));
+        // A lane copies the 16 bytes at 16 lane of each 512 (four rows); a half of 16 keys lies in one page.  No page: zeros.
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int id = half == 0 ? id0 : id1;
+            const size_t row = id < 0 ? 0 : ((size_t)(id * Hkv + ahead.h) << page_bits) + ((key0 + 16 * half) & (T - 1));
+            const uint8_t* const k_src = a.p.k8 + row * kD + 16 * lane;
+            const uint8_t* const v_src = a.p.v8 + row * kD + 16 * lane;
+            const uint32_t k_dst = ring_at + (uint32_t)(slot * 2 * kTile + half * 2048), bytes = id < 0 ? 0u : 16u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                cp_async16(k_dst + (i & 1 ? dst1 : dst0) + (i >> 1) * 1024, k_src + i * 512, bytes);
+                cp_async16(k_dst + kTile + (i & 1 ? dst1 : dst0) + (i >> 1) * 1024, v_src + i * 512, bytes);
             }
         }
-        // lanes 0 and 1 copy a box of K and of V each (the second only where the step takes two pages)
-        const bool copies = id >= 0 && (lane == 0 || (lane == 1 && T < kStep));
-        const unsigned boxes = __popc(__ballot_sync(0xFFFFFFFFu, copies));
-        if (lane == 0) mbar_arrive_expect_tx(&me.full[slot], 2u * boxes * box_bytes);
-        __syncwarp();
-        if (copies) {
-            unsigned char* const dst = ring + slot * 2 * kTile + lane * box_bytes;
-            const int row = ((id * Hkv + ahead.h) << page_bits) + (key0 & (T - 1));      // (a second box begins its page: T is 16 then)
-            tma_load_2d(dst, &tmap_k, &me.full[slot], 0, row);
-            tma_load_2d(dst + kTile, &tmap_v, &me.full[slot], 0, row);
+        if (lane < 4) {
+            // lanes 0, 1: K's scale of the first and second half; 2, 3: V's
+            const int id = lane & 1 ? id1 : id0;
+            float* const dst = lane < 2 ? &sc_ring[slot].ks[lane] : &sc_ring[slot].vs[lane - 2];
+            if (id >= 0)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;"
+                             ::"r"(smem_u32(dst)), "l"((lane < 2 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + ahead.h) : "memory");
+            else
+                *dst = -1.f;
         }
         __syncwarp();
         ++ahead_at;
@@ -309,14 +302,17 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             ids_first = -64;
         }
     };
-    if (lo < hi)
-        for (int s = 0; s < kDepth && ahead_at < hi; ++s) issue(s);
+    // one group of copies per slot, an empty one where nothing is left: the group of the oldest slot is always kDepth - 1 groups back
+#pragma unroll
+    for (int s = 0; s < kDepth; ++s) {
+        if (ahead_at < hi) issue(s);
+        cp_async_commit();
+    }
     int slot = 0;
-    uint32_t phase = 0;
-    bool ok = true, tail = false;
+    bool tail = false;
     float o[kN][8][4];       // [column block][16 channels]: channels 16 c + 2 g and + 1 of rows 2 t (elements 0, 2) and 2 t + 1 (1, 3)
     float m[kN][2], l[kN][2];
-    for (long long x = lo; x < hi && ok;) {
+    for (long long x = lo; x < hi;) {
         // ---- a segment, or the stretch of it that is this warp's
         const int first_step = at.step;
         uint32_t qf[kN][8][2];
@@ -361,13 +357,10 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 for (int u = 0; u < 4; ++u) o[n][c][u] = 0.f;
         }
         const int first_limit = at.len - a.L_q;       // of the first row
-        for (; at.step < at.n_steps && x < hi; ++at.step, ++x) {
-            ok = mbar_wait(&me.full[slot], phase, abort, a.status, 251);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
-            const uint32_t k_at = smem_u32(ring) + (uint32_t)(slot * 2 * kTile), v_at = k_at + kTile;
-            const DecodeStage sc = me.sc[slot];
-            const int key0 = at.step * kStep;
+        // One step, in two forms: `odd` ones have keys that some row does not see, or that have no page.
+        auto step = [&](auto odd_c, int key0, const DecodeStage sc) {
+            constexpr bool odd = decltype(odd_c)::value;
+            const uint32_t k_at = ring_at + (uint32_t)(slot * 2 * kTile), v_at = k_at + kTile;
             // S^T: 32 keys in two tiles of 16.  A lane's four bytes of a key are four neighbouring channels: two k-slots and, eight
             // further, two more (the order of the channels within a k-step is free, and Q's fragments have it too).
             float s[kN][2][4];
@@ -392,8 +385,6 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         for (int n = 0; n < kN; ++n) mma16816(s[n][i], f, qf[n][c + cc][0], qf[n][c + cc][1]);
                     }
             }
-            // a step with keys that some row does not see, or without a page
-            const bool odd = key0 + kStep - 1 > first_limit || sc.ks[0] < 0.f || sc.ks[1] < 0.f;
             float shift[2], vm[2], back[2];      // vs = vm * 2^shift, 1 <= vm < 2; back = 2^-shift: the sums are of p itself
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -493,11 +484,19 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     }
                 }
             }
+        };
+        for (; at.step < at.n_steps && x < hi; ++at.step, ++x) {
+            cp_async_wait_group<kDepth - 1>();
+            __syncwarp();
+            const DecodeStage sc = sc_ring[slot];
+            const int key0 = at.step * kStep;
+            if (key0 + kStep - 1 > first_limit || sc.ks[0] < 0.f || sc.ks[1] < 0.f) step(std::integral_constant<bool, true>{}, key0, sc);
+            else step(std::integral_constant<bool, false>{}, key0, sc);
             __syncwarp();          // every lane is done with the slot
             if (ahead_at < hi) issue(slot);
-            if (++slot == kDepth) { slot = 0; phase ^= 1u; }
+            cp_async_commit();
+            if (++slot == kDepth) slot = 0;
         }
-        if (!ok) break;
 #pragma unroll
         for (int n = 0; n < kN; ++n)
 #pragma unroll
@@ -548,15 +547,8 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         if (x < hi) next_segment<1>(a, pre, at);
     }
-    if (!ok) {      // loads in flight get a bounded chance to land before the CTA retires
-        for (int s = 0; s < kDepth; ++s)
-            for (int i = 0; i < 4096 && !mbar_try_wait(&me.full[s], 0) && !mbar_try_wait(&me.full[s], 1); ++i) {}
-    }
+    cp_async_wait_group<0>();      // (the last groups are empty)
     __syncthreads();
-    if (abort_flag != 0) {
-        if (threadIdx.x == 0) a.chains[blockIdx.x] = ChainEntry{-1, 0, 0, 0};
-        return;
-    }
     // ---- the warps' unfinished pieces: neighbours of one segment are merged; what is still unfinished is the CTA's
     float* const pieces = reinterpret_cast<float*>(smem);
     if (tail) {
@@ -593,8 +585,7 @@ page_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                                 : __ldcg(a.part_ml + ((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (lane >> 1)) * kRows + r);
             float mx = ml.x;
 #pragma unroll
-            for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
-            mx = __shfl_sync(0xFFFFFFFFu, mx, 0);
+            for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
             const float mine = partial_weight(ml, mx);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             float sum = 0.f;
@@ -1361,13 +1352,21 @@ static int make_pool_map(CUtensorMap* m, const void* base, long long rows, int b
 }
 
 static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+static size_t prefix_bytes(int n) { return ((size_t)n + 1) * sizeof(int); }
 // Column blocks of the kernel of few rows, 0: too many rows for it.
 static int few_blocks(int rows) { return rows <= 8 * kMostBlocks ? (rows + 7) / 8 : 0; }
 // Partial rows: two sets a CTA, and for the kernel of few rows one a warp for the pieces parked on the way.
 static size_t partial_rows(int ctas, int blocks) {
-    return blocks > 0 ? (size_t)ctas * (2 + kDecodeWarps) * 8 * blocks : (size_t)ctas * 2 * kQRows;
+    return blocks > 0 ? (size_t)ctas * (2 + decode_warps(blocks)) * 8 * blocks : (size_t)ctas * 2 * kQRows;
 }
-static size_t prefix_bytes(int n) { return ((size_t)n + 1) * sizeof(int); }
+template <int kN>
+static cudaError_t prepare_decode() {
+    return cudaFuncSetAttribute(page_decode_kernel<kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(decode_smem(kN) + prefix_bytes(kPageMaxSeqs)));
+}
+template <int kN>
+static cudaError_t launch_decode(const PageAttnArgs& a, int ctas, cudaStream_t stream) {
+    return launch_kernel(page_decode_kernel<kN>, dim3(ctas), dim3(decode_warps(kN) * 32), decode_smem(kN) + prefix_bytes(a.n), stream, a);
+}
 
 size_t page_attn_scratch_bytes(int n, int L_q, int Hq, int Hkv) {
     (void)n;
@@ -1393,19 +1392,14 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     a.part_ml = reinterpret_cast<float2*>(at); at += round256(partial_rows(ctas, blocks) * sizeof(float2));
     a.part_o = reinterpret_cast<float*>(at);
     a.status = status;
-    const long long rows = (long long)pool.n_pages * pool.Hkv * pool.T;
-    CUtensorMap mk, mv;
-    const int step = few ? kStep : kQStep, box = pool.T < step ? pool.T : step;
-    if (int rc = make_pool_map(&mk, pool.k8, rows, box)) return rc;
-    if (int rc = make_pool_map(&mv, pool.v8, rows, box)) return rc;
     static std::atomic<bool> attr_done[64];
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64 || !attr_done[dev].load(std::memory_order_acquire)) {
-        cudaError_t e = cudaSuccess;
-        for (auto* kernel : {page_decode_kernel<1>, page_decode_kernel<2>, page_decode_kernel<3>, page_decode_kernel<4>})
-            if (e == cudaSuccess)
-                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kDecodeSmem + prefix_bytes(kPageMaxSeqs)));
+        cudaError_t e = prepare_decode<1>();
+        if (e == cudaSuccess) e = prepare_decode<2>();
+        if (e == cudaSuccess) e = prepare_decode<3>();
+        if (e == cudaSuccess) e = prepare_decode<4>();
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(page_question_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQuestionSmem + prefix_bytes(kPageMaxSeqs)));
         // the question kernel's warpgroups trade registers: their shares add up to what 96 a thread give the block at launch
@@ -1415,9 +1409,17 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
         if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
         if (dev >= 0 && dev < 64) attr_done[dev].store(true, std::memory_order_release);
     }
-    auto* decode = blocks == 1 ? page_decode_kernel<1> : blocks == 2 ? page_decode_kernel<2> : blocks == 3 ? page_decode_kernel<3> : page_decode_kernel<4>;
-    cudaError_t e = few ? launch_kernel(decode, dim3(ctas), dim3(kDecodeWarps * 32), kDecodeSmem + prefix_bytes(n), stream, mk, mv, a)
-                        : launch_kernel(page_question_kernel, dim3(ctas), dim3(kQThreads), kQuestionSmem + prefix_bytes(n), stream, mk, mv, a);
+    cudaError_t e;
+    if (few) {
+        e = blocks == 1 ? launch_decode<1>(a, ctas, stream) : blocks == 2 ? launch_decode<2>(a, ctas, stream)
+          : blocks == 3 ? launch_decode<3>(a, ctas, stream) : launch_decode<4>(a, ctas, stream);
+    } else {
+        const long long rows = (long long)pool.n_pages * pool.Hkv * pool.T;
+        CUtensorMap mk, mv;
+        if (int rc = make_pool_map(&mk, pool.k8, rows, pool.T < kQStep ? pool.T : kQStep)) return rc;
+        if (int rc = make_pool_map(&mv, pool.v8, rows, pool.T < kQStep ? pool.T : kQStep)) return rc;
+        e = launch_kernel(page_question_kernel, dim3(ctas), dim3(kQThreads), kQuestionSmem + prefix_bytes(n), stream, mk, mv, a);
+    }
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
     e = few ? launch_kernel(page_merge_kernel<4>, dim3(ctas, 4 * blocks), dim3(256), 0, stream, a, 8 * blocks)
