@@ -302,12 +302,6 @@ page_decode_kernel(const PageAttnArgs a) {
             ids_first = -64;
         }
     };
-    // one group of copies per slot, an empty one where nothing is left: the group of the oldest slot is always kDepth - 1 groups back
-#pragma unroll
-    for (int s = 0; s < kDepth; ++s) {
-        if (ahead_at < hi) issue(s);
-        cp_async_commit();
-    }
     int slot = 0;
     bool tail = false;
     float o[kN][8][4];       // [column block][16 channels]: channels 16 c + 2 g and + 1 of rows 2 t (elements 0, 2) and 2 t + 1 (1, 3)
@@ -323,16 +317,28 @@ page_decode_kernel(const PageAttnArgs a) {
             const int row = 8 * n + g;
             const bool there = row < a.rows;
             const uint2* const src = reinterpret_cast<const uint2*>(a.q + (((size_t)at.b * a.L_q + row / a.G) * a.Hq + at.h * a.G + row % a.G) * kD) + t;
-            uint32_t big = 0;
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
                 const uint2 v = there ? __ldg(src + kk * 4) : make_uint2(0u, 0u);
                 qf[n][kk][0] = v.x; qf[n][kk][1] = v.y;
+            }
+        }
+        if (x == lo) {
+            // One group of copies per slot, an empty one where nothing is left: the group of the oldest slot is always kDepth - 1
+            // groups back.  (Asked for here, with the first rows of Q on their way.)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t bits = ((u & 2 ? v.y : v.x) >> (16 * (u & 1))) & 0x7FFFu;
-                    big = max(big, bits < 0x7F80u ? bits : 0u);
-                }
+            for (int d = 0; d < kDepth; ++d) {
+                if (ahead_at < hi) issue(d);
+                cp_async_commit();
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const uint32_t bits = (qf[n][j >> 2][(j >> 1) & 1] >> (16 * (j & 1))) & 0x7FFFu;
+                big = max(big, bits < 0x7F80u ? bits : 0u);
             }
             big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
             big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
