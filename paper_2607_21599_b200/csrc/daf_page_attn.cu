@@ -38,7 +38,7 @@ struct ChainEntry {
 };
 
 // ---------------------------------------------------------------------------------------------------- few rows: warps on their own
-// Up to 32 rows of a KV head go through the warp-wide matrix instruction, eight at a time: with keys (and then channels) as its 16
+// Up to 24 rows of a KV head go through the warp-wide matrix instruction, eight at a time: with keys (and then channels) as its 16
 // rows and query rows as its eight columns, S^T = K Q^T and O^T = V^T P^T, so that one token of a group of up to eight heads wastes
 // nothing, and a widened tile of K or V serves all kN column blocks.  (There are 4 flops per byte and row: the cache's way from HBM
 // is what counts, not the tensor cores' rate, and a warp that needs nobody else keeps its loads in flight all the time.)  A warp
@@ -51,7 +51,7 @@ struct ChainEntry {
 //   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
 //   largest and some bits down to 2^-34 (as bf16 it would have 8), while sums of p stay in fp32.
 constexpr int kStep = 32;
-constexpr int kMostBlocks = 4;                       // column blocks of eight rows
+constexpr int kMostBlocks = 3;                       // column blocks of eight rows
 constexpr int kTile = kStep * kD;                    // 4 KB: K or V of one step
 constexpr float kPExp = 9.f;
 // Warps of a CTA (one CTA an SM), and steps a warp asks ahead: as many warps as the registers of one column block leave room for,
@@ -156,8 +156,18 @@ __device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, int* 
 __device__ __forceinline__ long long axis_div(long long x, long long y) {
     return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
-// Where CTA c's stretch begins when `ctas` of them share `total`: floor(c total / ctas).
-__device__ __forceinline__ long long cta_begin(long long c, long long total, long long ctas) { return axis_div(c * total, ctas); }
+// `total` places shared by `ctas`: the first `more` take each + 1, the others `each`.
+struct Shares { long long each, more; };
+__device__ __forceinline__ Shares share(long long total, long long ctas) {
+    const long long each = axis_div(total, ctas);
+    return Shares{each, total - each * ctas};
+}
+__device__ __forceinline__ long long cta_begin(const Shares& s, long long c) { return c * s.each + min(c, s.more); }
+// The CTA whose stretch holds place `at`.
+__device__ __forceinline__ int cta_of(const Shares& s, long long at) {
+    const long long longer = s.more * (s.each + 1);
+    return (int)(at < longer ? axis_div(at, s.each + 1) : s.more + axis_div(at - longer, s.each));
+}
 
 template <int kW>
 __device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* pre, Place& x) {
@@ -205,14 +215,6 @@ __device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* p
     if (x.b >= a.n) return (long long)pre[a.n] * a.p.Hkv * a.units;
     return (long long)pre[x.b] * a.p.Hkv * a.units + (long long)x.n_steps * (x.h * a.units + kW * x.block) + (long long)x.step * x.width;
 }
-// The CTA whose stretch holds axis position `at` when `ctas` of them share `total`.
-__device__ __forceinline__ int cta_of(long long at, long long total, long long ctas) {
-    long long c = min(axis_div(at * ctas, total), ctas - 1);
-    while (c + 1 < ctas && cta_begin(c + 1, total, ctas) <= at) ++c;
-    while (c > 0 && cta_begin(c, total, ctas) > at) --c;
-    return (int)c;
-}
-
 // A row's factor 1 / sum (a row that saw nothing: 0), its log-sum-exp, and the weight of a partial with (maximum, sum) in a merge
 // whose largest maximum is mx.  A maximum of -inf with a sum other than 0 is a row of NaN logits: it stays one.
 __device__ __forceinline__ float row_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
@@ -245,9 +247,10 @@ page_decode_kernel(const PageAttnArgs a) {
     const long long total = (long long)pre[a.n] * a.p.Hkv;
     // CTAs that take part: no more than give each of its warps a step
     const long long ctas = min((long long)gridDim.x, (total + kDecodeWarps - 1) / kDecodeWarps);
-    const long long cta_lo = cta_begin(min((long long)blockIdx.x, ctas), total, ctas);
-    const long long span = cta_begin(min((long long)blockIdx.x + 1, ctas), total, ctas) - cta_lo;
-    const long long lo = cta_lo + warp * span / kDecodeWarps, hi = cta_lo + (warp + 1) * span / kDecodeWarps;
+    const Shares shares = share(total, ctas);
+    const long long cta_lo = cta_begin(shares, min((long long)blockIdx.x, ctas));
+    const long long span = cta_begin(shares, min((long long)blockIdx.x + 1, ctas)) - cta_lo;
+    const long long lo = cta_lo + axis_div(warp * span, kDecodeWarps), hi = cta_lo + axis_div((warp + 1) * span, kDecodeWarps);
 
     const int T = a.p.T, Hkv = a.p.Hkv, page_bits = 31 - __clz(T);
     Place at = {};
@@ -594,14 +597,21 @@ page_decode_kernel(const PageAttnArgs a) {
             for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
             const float mine = partial_weight(ml, mx);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            float sum = 0.f;
-            for (unsigned rest = group; rest != 0; rest &= rest - 1) {
-                const int i = __ffs(rest) - 1;
+            float sum = mine * ml.y;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            auto add = [&](int i, const float4* src) {
                 const float w = __shfl_sync(0xFFFFFFFFu, mine, i);
-                const float4 v = (i & 1) ? reinterpret_cast<const float4*>(pieces + (i >> 1) * kPiece + r * kD)[lane]
-                                         : __ldcg(reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kRows + r) * kD) + lane);
-                sum += w * __shfl_sync(0xFFFFFFFFu, ml.y, i);
-                acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+                if (w != 0.f) {                        // (the others' memory holds anything)
+                    const float4 v = src[lane];
+                    acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kDecodeWarps; ++i) add(2 * i + 1, reinterpret_cast<const float4*>(pieces + i * kPiece + r * kD));
+            for (unsigned rest = group & 0x55555555u; rest != 0; rest &= rest - 1) {
+                const int i = __ffs(rest) - 1;
+                add(i, reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kRows + r) * kD));
             }
             if (begins && ends) {
                 const int tok = r / a.G, head = seg.y * a.G + r % a.G;
@@ -617,17 +627,17 @@ page_decode_kernel(const PageAttnArgs a) {
         }
         if (begins && !ends) chain = ChainEntry{0, seg.x, seg.y, 0};
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == (kDecodeWarps - 1) * 32) {       // (a warp with the fewest rows to merge)
         if (chain.last_cta == 0) {
             const long long end = (long long)pre[chain.b] * Hkv + (long long)(chain.h + 1) * (pre[chain.b + 1] - pre[chain.b]);
-            chain.last_cta = cta_of(end - 1, total, ctas);
+            chain.last_cta = cta_of(shares, end - 1);
         }
         a.chains[blockIdx.x] = chain;
     }
 }
 
 // ---------------------------------------------------------------------------------------------- many rows: tensor memory
-// More than 32 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
+// More than 24 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
 // of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 20 warps:
 //   10, 11  ask for the bytes of K and V (TMA, kQStages steps ahead) and their scales;
 //   12-15, 16-19  widen K's, and V's, to fp16, exactly, into the two-slot rings that the products read (128-byte swizzle).  Each of
@@ -667,7 +677,8 @@ struct QuestionSmem {
     // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
     Place at;
     int step1, n_t, first_limit, last_limit;      // steps at.step .. step1 - 1, of which the first n_t have keys that some row sees
-    long long x, hi, total, ctas;
+    long long x, hi;
+    Shares shares;
     ChainEntry chain;
 };
 constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQTile + 4 * (size_t)kQSlot + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
@@ -807,7 +818,8 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     if (threadIdx.x == 0) {
         const long long total = (long long)pre[a.n] * Hkv * a.units;
         const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than four steps of a tile each
-        const long long c_lo = cta_begin(min((long long)blockIdx.x, ctas), total, ctas), c_hi = cta_begin(min((long long)blockIdx.x + 1, ctas), total, ctas);
+        const Shares shares = share(total, ctas);
+        const long long c_lo = cta_begin(shares, min((long long)blockIdx.x, ctas)), c_hi = cta_begin(shares, min((long long)blockIdx.x + 1, ctas));
         // both ends move up to the next step's begin
         Place at = {};
         sm->x = sm->hi = total;
@@ -816,8 +828,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         sm->at = at;
         sm->step1 = 0;
         sm->used = 0;
-        sm->total = total;
-        sm->ctas = ctas;
+        sm->shares = shares;
         sm->chain = ChainEntry{-1, 0, 0, 0};
     }
     // Three of the five warpgroups need few registers: 256 x 144 + 384 x 64 = 640 x 96
@@ -843,7 +854,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     if (at.step == 0 && step1 < at.n_steps) {
                         Place end = at;
                         end.step = at.n_steps - 1;
-                        sm->chain = ChainEntry{cta_of(axis_at<2>(a, pre, end), sm->total, sm->ctas), at.b, at.h, at.block};
+                        sm->chain = ChainEntry{cta_of(sm->shares, axis_at<2>(a, pre, end)), at.b, at.h, at.block};
                     }
                 }
                 if (sm->used)                   // the barriers start anew with every piece: nothing is under way on them
@@ -1266,12 +1277,12 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     }
 }
 
-// Merge of the segments that lie in several CTAs: kWarps warps per row of a segment that CTA blockIdx.x begins.  Few rows with many
-// partials (one answer over a long context: 37) are bound by the trips to L2, so that several warps share a row's partials; of many
-// rows with few each takes one warp.
+// Merge of the segments that lie in several CTAs: kWarps warps per row of a segment that CTA blockIdx.x begins.  Bound by the trips
+// to L2, so a warp asks for its first kAtOnce partials together with the row's maxima: few rows with many partials (one answer over a
+// long context: 37) take eight warps a row, many rows with few partials one.
 template <int kWarps>
 __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, int block_rows) {
-    constexpr int kRows = 8 / kWarps;
+    constexpr int kRows = 8 / kWarps, kAtOnce = kWarps == 1 ? 8 : 5;
     __shared__ float4 acc_s[8][32];
     __shared__ float sum_s[8];
     pdl_wait();
@@ -1283,22 +1294,33 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
     const int row = e.block * block_rows + r;
     const bool there = r < block_rows && row < a.rows;
     // partial i of the row: the first CTA's second set, then the following CTAs' first sets
-    auto set_of = [&](int i) { return i == 0 ? (size_t)first * 2 + 1 : (size_t)(first + i) * 2; };
     const int n = there ? e.last_cta - first + 1 : 0;
+    auto at = [&](int i) { return (i == 0 ? (size_t)first * 2 + 1 : (size_t)(first + i) * 2) * block_rows + r; };
+    float2 ml[kAtOnce];
+    float4 v[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+        const int i = part + u * kWarps;
+        ml[u] = i < n ? __ldcg(a.part_ml + at(i)) : make_float2(-INFINITY, 0.f);
+        v[u] = i < n ? __ldcg(reinterpret_cast<const float4*>(a.part_o + at(i) * kD) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     float mx = -INFINITY;
-    for (int i = lane; i < n; i += 32) mx = fmaxf(mx, __ldcg(&a.part_ml[set_of(i) * block_rows + r].x));
+    for (int i = lane; i < n; i += 32) mx = fmaxf(mx, __ldcg(&a.part_ml[at(i)].x));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
+    auto add = [&](float2 x, float4 y) {
+        const float w = partial_weight(x, mx);
+        if (w == 0.f) return;
+        sum += w * x.y;
+        acc.x += w * y.x; acc.y += w * y.y; acc.z += w * y.z; acc.w += w * y.w;
+    };
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) add(ml[u], v[u]);
 #pragma unroll 4
-    for (int i = part; i < n; i += kWarps) {
-        const float2 ml = __ldcg(&a.part_ml[set_of(i) * block_rows + r]);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + (set_of(i) * block_rows + r) * kD) + lane);
-        const float w = partial_weight(ml, mx);
-        sum += w * ml.y;
-        acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
-    }
+    for (int i = part + kAtOnce * kWarps; i < n; i += kWarps)
+        add(__ldcg(a.part_ml + at(i)), __ldcg(reinterpret_cast<const float4*>(a.part_o + at(i) * kD) + lane));
     if (kWarps > 1) {
         acc_s[warp][lane] = acc;
         if (lane == 0) sum_s[warp] = sum;
@@ -1306,8 +1328,8 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
         if (part != 0) return;
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) {
-            const float4 v = acc_s[warp + w][lane];
-            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+            const float4 y = acc_s[warp + w][lane];
+            acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
             sum += sum_s[warp + w];
         }
     }
@@ -1405,7 +1427,6 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
         cudaError_t e = prepare_decode<1>();
         if (e == cudaSuccess) e = prepare_decode<2>();
         if (e == cudaSuccess) e = prepare_decode<3>();
-        if (e == cudaSuccess) e = prepare_decode<4>();
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(page_question_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQuestionSmem + prefix_bytes(kPageMaxSeqs)));
         // the question kernel's warpgroups trade registers: their shares add up to what 96 a thread give the block at launch
@@ -1418,7 +1439,7 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     cudaError_t e;
     if (few) {
         e = blocks == 1 ? launch_decode<1>(a, ctas, stream) : blocks == 2 ? launch_decode<2>(a, ctas, stream)
-          : blocks == 3 ? launch_decode<3>(a, ctas, stream) : launch_decode<4>(a, ctas, stream);
+          : launch_decode<3>(a, ctas, stream);
     } else {
         const long long rows = (long long)pool.n_pages * pool.Hkv * pool.T;
         CUtensorMap mk, mv;
@@ -1428,7 +1449,7 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     }
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
-    e = few ? launch_kernel(page_merge_kernel<4>, dim3(ctas, 4 * blocks), dim3(256), 0, stream, a, 8 * blocks)
+    e = few ? launch_kernel(page_merge_kernel<8>, dim3(ctas, 8 * blocks), dim3(256), 0, stream, a, 8 * blocks)
             : launch_kernel(page_merge_kernel<1>, dim3(ctas, kQRows / 8), dim3(256), 0, stream, a, (int)kQRows);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
