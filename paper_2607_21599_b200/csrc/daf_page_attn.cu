@@ -6,6 +6,7 @@
 // which a second kernel merges.
 #include <cuda_fp16.h>
 #include <math.h>
+#include <stddef.h>
 
 #include <atomic>
 #include <type_traits>
@@ -72,9 +73,6 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uin
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
         : "memory");
-}
-__device__ __forceinline__ void mbar_inval(uint64_t* bar) {
-    asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -650,6 +648,7 @@ page_decode_kernel(const PageAttnArgs a) {
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 64;
 constexpr int kQStages = 4;
+constexpr int kQConsts = 16;       // steps whose constants are kept: they are written up to kQStages + 6 steps ahead of their last reader
 constexpr int kQRows = 256;
 constexpr int kQThreads = 640;
 constexpr int kQTile = 128 * kD * 2;                  // 32 KB: 128 rows of Q, two 64-column halves
@@ -664,14 +663,14 @@ struct QuestionSmem {
     uint64_t k_full[2], v_full[2];
     uint64_t q_full[2];
     uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];      // [group][half]
-    uint64_t c_full[8];
-    float4 chunk[8][4];             // of eight steps and each 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
-    int missing[8];                 // some keys of the step have no page
-    float scales[kQStages][8];      // K's, then V's, of the step's chunks of 16 keys, as they arrive with the bytes of K
+    uint64_t c_full[kQConsts];
+    float4 chunk[kQConsts][4];      // of a step's chunks of 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
+    int missing[kQConsts];          // some keys of the step have no page
+    float row_factor[2][128];       // what a row's logits are to be multiplied by, apart from ks
     float2 ml[128];                 // the second group's row maxima and sums (blocks of one tile)
     uint32_t tmem_base;
     int abort_flag;
-    int used;                       // the barriers have been initialised
+    unsigned long long odd;         // which barriers have completed an odd number of phases
     int go[2][2];                   // [K, V][step mod 2] what the polling warp found
     int poison;                     // a NaN was taken out of a value that some rows must not see
     // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
@@ -681,6 +680,11 @@ struct QuestionSmem {
     Shares shares;
     ChainEntry chain;
 };
+constexpr int kBarEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK = (int)(offsetof(QuestionSmem, k_full) / 8),
+              kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8), kBarS = (int)(offsetof(QuestionSmem, s_full) / 8),
+              kBarP = (int)(offsetof(QuestionSmem, p_full) / 8), kBarPv = (int)(offsetof(QuestionSmem, pv_done) / 8),
+              kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
+static_assert(offsetof(QuestionSmem, st_full) == 0 && kQStages == 4 && (kBarS & 1) == 0 && kBars <= 64, "what bar_uses and wait_phase rest on");
 constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQTile + 4 * (size_t)kQSlot + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
 __host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
@@ -766,10 +770,23 @@ __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4*
     return alpha;
 }
 
-// The bounded wait of this kernel (a second at most, or until another thread has given up): it only leaves the number of the wait in
+// How many phases barrier i completes in a piece of n_t steps.
+__device__ __forceinline__ int bar_uses(int i, int n_t, bool pair) {
+    if (i < kBarK) return (n_t - (i & 3) + 3) >> 2;                      // every fourth step (kQStages)
+    if (i < kBarQ) return (n_t - (i & 1) + 1) >> 1;
+    if (i < kBarS) return i == kBarQ || pair ? 1 : 0;
+    if (i < kBarC) {
+        const int j = (i - kBarS) & 3, steps = pair ? n_t : (n_t - (j >> 1) + 1) >> 1;       // of the group
+        return (steps - (j & 1) + 1) >> 1;
+    }
+    return i < kBars ? (n_t - (i - kBarC) + kQConsts - 1) / kQConsts : 0;
+}
+
+// The bounded wait of this kernel, `parity` as if the piece of work were the CTA's first (a second at most, or until another thread has given up): it only leaves the number of the wait in
 // the abort flag, which one thread reports at the end.  The warps' loops are many, and what they keep in the instruction caches
 // counts: with longer waits and every rare case unrolled, warps that had work found no instruction a sixth of the time.
-__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile int* abort, int where) {
+__device__ __forceinline__ bool wait_phase(QuestionSmem* sm, unsigned long long odd, uint64_t* bar, uint32_t parity, volatile int* abort, int where) {
+    parity ^= (uint32_t)(odd >> ((smem_u32(bar) - smem_u32(sm)) >> 3)) & 1u;
     if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long t0 = global_ns();
     for (;;) {
@@ -804,8 +821,18 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     }
     if (threadIdx.x == 0) {
         sm->abort_flag = 0;
+        sm->odd = 0;
         tma_prefetch_desc(&tmap_k);
         tma_prefetch_desc(&tmap_v);
+    }
+    if (warp == 1) {
+        uint64_t* const bars = reinterpret_cast<uint64_t*>(stage_smem + 2 * kQStages * kQStage);
+        for (int i = lane; i < kBars; i += 32) {
+            // four warps (or lanes) arrive; at the others a copy's bytes or a product
+            const bool by_four = (i >= kBarEmpty && i < kBarS) || (i >= kBarP && i < kBarPv) || i >= kBarC;
+            mbar_init(bars + i, by_four ? 4 : 1);
+        }
+        mbar_fence_init();
     }
     pdl_wait();
     pdl_launch_dependents();
@@ -827,13 +854,14 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         if (c_lo < total) { at = place_at<2>(a, pre, c_lo); sm->x = axis_at<2>(a, pre, at); }
         sm->at = at;
         sm->step1 = 0;
-        sm->used = 0;
         sm->shares = shares;
         sm->chain = ChainEntry{-1, 0, 0, 0};
     }
     // Three of the five warpgroups need few registers: 256 x 144 + 384 x 64 = 640 x 96
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+        int prev_t = 0;                 // steps and width of the piece before
+        bool prev_pair = false, any_before = false;
         for (;;) {
             // ---- one segment, or this CTA's stretch of it
             if (threadIdx.x == 0) {
@@ -857,83 +885,84 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         sm->chain = ChainEntry{cta_of(sm->shares, axis_at<2>(a, pre, end)), at.b, at.h, at.block};
                     }
                 }
-                if (sm->used)                   // the barriers start anew with every piece: nothing is under way on them
-                    for (uint64_t* bar = sm->st_full[0]; bar != sm->c_full + 8; ++bar) mbar_inval(bar);
-                sm->used = 1;
-                for (int i = 0; i < kQStages; ++i) {
-                    mbar_init(&sm->st_full[0][i], 1 + 8); mbar_init(&sm->st_full[1][i], 1);
-                    mbar_init(&sm->st_empty[0][i], 4); mbar_init(&sm->st_empty[1][i], 4);
-                }
-                for (int i = 0; i < 2; ++i) {
-                    mbar_init(&sm->k_full[i], 4); mbar_init(&sm->v_full[i], 4); mbar_init(&sm->q_full[i], 4);
-                    for (int j = 0; j < 2; ++j) { mbar_init(&sm->s_full[i][j], 1); mbar_init(&sm->p_full[i][j], 4); mbar_init(&sm->pv_done[i][j], 1); }
-                }
-                for (int i = 0; i < 8; ++i) mbar_init(&sm->c_full[i], 1);
                 sm->poison = 0;
-                mbar_fence_init();
+            }
+            // The barriers count on from piece to piece: bit i of `odd` says whether barrier i has completed an odd number of phases.
+            if (warp == 1) {
+                const unsigned first = __ballot_sync(0xFFFFFFFFu, any_before && (bar_uses(lane, prev_t, prev_pair) & 1));
+                const unsigned second = __ballot_sync(0xFFFFFFFFu, any_before && (bar_uses(lane + 32, prev_t, prev_pair) & 1));
+                if (lane == 0) sm->odd ^= ((unsigned long long)second << 32) | first;
             }
             __syncthreads();
             if (sm->step1 == 0) break;
             bool ok = true;
             const int n_t = sm->n_t, step0 = sm->at.step;
+            const unsigned long long odd = sm->odd;
             const bool pair = sm->at.width == 2;
+            prev_t = n_t; prev_pair = pair; any_before = true;
             // ------------------------------------------------------------------------------------- softmax, a row per thread
             const int g = warp >> 2, rt = threadIdx.x & 127;
             const int row = sm->at.block * kQRows + (pair ? g * 128 : 0) + rt;
             const bool valid = row < a.rows;
             const int limit = valid ? sm->at.len - a.L_q + row / a.G : sm->last_limit;
             const int n_u = pair ? n_t : (n_t - g + 1) / 2;
-            float c;
             {
-                // this thread's row of Q, scaled to a largest magnitude of 2^14 .. 2^15, as fp16 in the layout of a tiled copy
-                uint32_t big = 0;
-                const uint4* const src = reinterpret_cast<const uint4*>(a.q + (((size_t)sm->at.b * a.L_q + row / a.G) * a.Hq + sm->at.h * a.G + row % a.G) * kD);
+                // The warp's 32 rows of Q, sixteen lanes a row, each row scaled to a largest magnitude of 2^14 .. 2^15, as fp16 in the
+                // layout of a tiled copy.  (A row a thread, its loads scattered over 32 rows, took 6 us a piece.)
+                const int sub = lane >> 4, cidx = lane & 15, r0 = (warp & 3) * 32 + sub;
+                const int from = sm->at.block * kQRows + (pair ? g * 128 : 0) + r0, d_tok = 2 / a.G, d_head = 2 % a.G;
+                int tok = from / a.G, head = from - tok * a.G;
+                const __nv_bfloat16* const src = a.q + ((size_t)sm->at.b * a.L_q * a.Hq + sm->at.h * a.G) * kD + cidx * 8;
 #pragma unroll
-                for (int i = 0; i < 16; i += 8) {
+                for (int i0 = 0; i0 < 16; i0 += 8) {
                     uint4 w[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = valid ? __ldg(src + i + j) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < 8; ++i) {
+                        w[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (from + 2 * (i0 + i) < a.rows) w[i] = __ldg(reinterpret_cast<const uint4*>(src + ((size_t)tok * a.Hq + head) * kD));
+                        tok += d_tok; head += d_head;
+                        if (head >= a.G) { head -= a.G; ++tok; }
+                    }
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const uint32_t v = (j & 3) == 0 ? w[j >> 2].x : (j & 3) == 1 ? w[j >> 2].y : (j & 3) == 2 ? w[j >> 2].z : w[j >> 2].w;
-                        const uint32_t b0 = v & 0x7FFFu, b1 = (v >> 16) & 0x7FFFu;
-                        big = max(big, max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u));
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = r0 + 2 * (i0 + i);
+                        uint32_t* const x = &w[i].x;
+                        uint32_t big = 0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t b0 = x[j] & 0x7FFFu, b1 = (x[j] >> 16) & 0x7FFFu;
+                            big = max(big, max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u));
+                        }
+#pragma unroll
+                        for (int d = 1; d < 16; d <<= 1) big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, d));
+                        const int e = max((int)(big >> 7) - 127, -100);
+                        const float up = __int_as_float((14 - e + 127) << 23);
+                        if (cidx == 0) sm->row_factor[g][r] = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = pack_f16(__uint_as_float(x[j] << 16) * up, __uint_as_float(x[j] & 0xFFFF0000u) * up);
+                        if (pair || g == 0)
+                            *reinterpret_cast<uint4*>(q_smem + g * kQTile + (cidx >> 3) * kQHalf + r * 128 + (((cidx & 7) ^ (r & 7)) << 4)) = w[i];
                     }
                 }
-                const int e = max((int)(big >> 7) - 127, -100);
-                const float up = __int_as_float((14 - e + 127) << 23);
-                c = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
-                if (pair || g == 0) {
-                    unsigned char* const dst = q_smem + g * kQTile + rt * 128;
-#pragma unroll 4
-                    for (int i = 0; i < 16; ++i) {       // (read again: it is in L1, and the registers are needed elsewhere)
-                        const uint4 w = valid ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
-                        uint4 y;
-                        y.x = pack_f16(__uint_as_float(w.x << 16) * up, __uint_as_float(w.x & 0xFFFF0000u) * up);
-                        y.y = pack_f16(__uint_as_float(w.y << 16) * up, __uint_as_float(w.y & 0xFFFF0000u) * up);
-                        y.z = pack_f16(__uint_as_float(w.z << 16) * up, __uint_as_float(w.z & 0xFFFF0000u) * up);
-                        y.w = pack_f16(__uint_as_float(w.w << 16) * up, __uint_as_float(w.w & 0xFFFF0000u) * up);
-                        *reinterpret_cast<uint4*>(dst + (i >> 3) * kQHalf + (((i & 7) ^ (rt & 7)) << 4)) = y;
-                    }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm->q_full[g]);
-                }
+                if (pair || g == 0) fence_proxy_async();
+                __syncwarp();
+                if (lane == 0 && (pair || g == 0)) mbar_arrive(&sm->q_full[g]);
             }
+            const float c = sm->row_factor[g][rt];
             const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
             const uint32_t s_addr = tmem + (uint32_t)(g * 256) + lane_addr, o_addr = s_addr + 128u;
             float m = -INFINITY, l = 0.f;
             for (int u = 0; u < n_u; ++u) {
                 const int t = pair ? u : 2 * u + g, b = u & 1;
-                ok = wait_phase(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, 271);
-                if (ok) ok = wait_phase(&sm->s_full[g][b], (uint32_t)((u >> 1) & 1), abort, 272);
+                ok = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 271);
+                if (ok) ok = wait_phase(sm, odd, &sm->s_full[g][b], (uint32_t)((u >> 1) & 1), abort, 272);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t & 7], sm->missing[t & 7] != 0, (step0 + t) * kQStep, limit, c, m, l);
+                const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t % kQConsts], sm->missing[t % kQConsts] != 0, (step0 + t) * kQStep, limit, c, m, l);
                 if (u > 0 && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
                     // the product before must have completed before O is touched
-                    ok = wait_phase(&sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, 273);
+                    ok = wait_phase(sm, odd, &sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, 273);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) break;
                     tc_fence_after();
@@ -954,7 +983,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             }
             // both last products (each on a barrier of its own)
             for (int u = max(0, n_u - 2); u < n_u && ok; ++u) {
-                ok = wait_phase(&sm->pv_done[g][u & 1], (uint32_t)((u >> 1) & 1), abort, 274);
+                ok = wait_phase(sm, odd, &sm->pv_done[g][u & 1], (uint32_t)((u >> 1) & 1), abort, 274);
                 ok = __all_sync(0xFFFFFFFFu, ok);
             }
             tc_fence_after();
@@ -993,57 +1022,75 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             if (ok && (pair || g == 0)) {      // (whole warps: the reads of tensor memory are theirs)
                 const Place at = sm->at;
                 const int tok = row / a.G, head = at.h * a.G + row % a.G;
-                const bool begins = step0 == 0, ends = sm->step1 == at.n_steps;
+                const bool begins = step0 == 0, whole = begins && sm->step1 == at.n_steps;
                 const float inv = row_inverse(l);
-                const size_t set = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
+                // Rows leave through the tile of Q, which is done with: 256 bytes of each of the warp's 32 rows at a time (a whole bf16 row,
+                // or half of an fp32 one), 16-byte pieces XOR-ed with the row number, and out again with sixteen lanes a row.
+                unsigned char* const stage = q_smem + (pair ? g : 0) * kQTile + (warp & 3) * 8192;
+                const size_t out_row = ((size_t)at.b * a.L_q + tok) * a.Hq + head;
+                const size_t set_row = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
+                const unsigned long long dst = reinterpret_cast<unsigned long long>(whole ? reinterpret_cast<char*>(a.out) + out_row * (kD * 2)
+                                                                                          : reinterpret_cast<char*>(a.part_o) + set_row * (kD * 4));
+                const unsigned rows_there = __ballot_sync(0xFFFFFFFFu, valid);
+                const bool poisoned = sm->poison != 0;
+                for (int pass = 0; pass < (whole ? 1 : 2); ++pass) {
 #pragma unroll 1
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t r[16];
-                    float o[16];
-                    if (n_u > 0) {
-                        tmem_ld16(o_addr + (uint32_t)(16 * i), r);
-                        tc_wait_ld();
-                    }
+                    for (int i = 0; i < (whole ? 8 : 4); ++i) {
+                        const int c16 = pass * 4 + i;      // 16 channels
+                        uint32_t r[16];
+                        float o[16];
+                        if (n_u > 0) {
+                            tmem_ld16(o_addr + (uint32_t)(16 * c16), r);
+                            tc_wait_ld();
+                        }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[j] = n_u > 0 ? __uint_as_float(r[j]) : 0.f;
-                    if (!pair) {
+                        for (int j = 0; j < 16; ++j) o[j] = n_u > 0 ? __uint_as_float(r[j]) : 0.f;
+                        if (!pair) {
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
-                            const float4 y = *reinterpret_cast<const float4*>(other + (((4 * i + j / 4) ^ lane) << 2));
-                            o[j] = w0 * o[j] + w1 * y.x; o[j + 1] = w0 * o[j + 1] + w1 * y.y;
-                            o[j + 2] = w0 * o[j + 2] + w1 * y.z; o[j + 3] = w0 * o[j + 3] + w1 * y.w;
+                            for (int j = 0; j < 16; j += 4) {
+                                const float4 y = *reinterpret_cast<const float4*>(other + (((4 * c16 + j / 4) ^ lane) << 2));
+                                o[j] = w0 * o[j] + w1 * y.x; o[j + 1] = w0 * o[j + 1] + w1 * y.y;
+                                o[j + 2] = w0 * o[j + 2] + w1 * y.z; o[j + 3] = w0 * o[j + 3] + w1 * y.w;
+                            }
+                        }
+                        if (poisoned && valid) {
+                            // values that were NaN, in keys that this row sees and the block's first does not
+                            const int from = max(sm->first_limit + 1, step0 * kQStep), to = min(min(limit, at.len - 1), (step0 + n_t) * kQStep - 1);
+                            for (int key = from; key <= to; ++key) {
+                                const int id = __ldg(a.table + (size_t)at.seq * a.p.max_pages + key / T);
+                                if ((unsigned)id >= (unsigned)a.p.n_pages) continue;
+                                const uint8_t* const v = a.p.v8 + (((size_t)id * Hkv + at.h) * T + key % T) * kD + 16 * c16;
+#pragma unroll
+                                for (int j = 0; j < 16; ++j)
+                                    if ((__ldg(v + j) & 0x7F) == 0x7F) o[j] = __int_as_float(0x7FC00000);
+                            }
+                        }
+                        unsigned char* const mine = stage + lane * 256;
+                        if (whole) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                *reinterpret_cast<uint4*>(mine + (((2 * i + j) ^ (lane & 15)) << 4)) =
+                                    make_uint4(pack_bf16(o[8 * j] * inv, o[8 * j + 1] * inv), pack_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
+                                               pack_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv), pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                *reinterpret_cast<float4*>(mine + (((4 * i + j) ^ (lane & 15)) << 4)) = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                         }
                     }
-                    if (!valid) continue;
-                    if (sm->poison != 0) {
-                        // values that were NaN, in keys that this row sees and the block's first does not
-                        const int from = max(sm->first_limit + 1, step0 * kQStep), to = min(min(limit, at.len - 1), (step0 + n_t) * kQStep - 1);
-                        for (int key = from; key <= to; ++key) {
-                            const int id = __ldg(a.table + (size_t)at.seq * a.p.max_pages + key / T);
-                            if ((unsigned)id >= (unsigned)a.p.n_pages) continue;
-                            const uint8_t* const v = a.p.v8 + (((size_t)id * Hkv + at.h) * T + key % T) * kD + 16 * i;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if ((__ldg(v + j) & 0x7F) == 0x7F) o[j] = __int_as_float(0x7FC00000);
-                        }
+                    __syncwarp();
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = 2 * i + (lane >> 4), p = lane & 15;
+                        const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 256 + ((p ^ (r & 15)) << 4));
+                        char* const to = reinterpret_cast<char*>(__shfl_sync(0xFFFFFFFFu, dst, r)) + pass * 256 + p * 16;
+                        if ((rows_there >> r) & 1u) *reinterpret_cast<uint4*>(to) = v;
                     }
-                    if (begins && ends) {
-                        uint4* const dst = reinterpret_cast<uint4*>(a.out + (((size_t)at.b * a.L_q + tok) * a.Hq + head) * kD) + 2 * i;
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            dst[j] = make_uint4(pack_bf16(o[8 * j] * inv, o[8 * j + 1] * inv), pack_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
-                                                pack_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv), pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
-                    } else {
-                        float4* const dst = reinterpret_cast<float4*>(a.part_o + set * kD) + 4 * i;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                    }
+                    __syncwarp();
                 }
-                if (!valid) {
-                } else if (begins && ends) {
-                    if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + head) * a.L_q + tok] = row_lse(m, l);
-                } else {
-                    a.part_ml[set] = make_float2(m, l);
+                if (valid) {
+                    if (!whole) a.part_ml[set_row] = make_float2(m, l);
+                    else if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + head) * a.L_q + tok] = row_lse(m, l);
                 }
             }
             tc_fence_before();
@@ -1058,18 +1105,20 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             if (sm->step1 == 0) break;
             bool ok = true;
             const int n_t = sm->n_t, step0 = sm->at.step;
+            const unsigned long long odd = sm->odd;
             const bool pair = sm->at.width == 2;
             if (warp == 10 || warp == 11) {
                 // ---------------------------------------------------------------------------------------- bytes and scales
                 const int kv = warp - 10, seq = sm->at.seq, h = sm->at.h, len = sm->at.len;
                 const bool reports = kv == 0 && h == 0 && sm->at.block == 0;
+                float ks = -1.f, vs = -1.f;         // (K's warp) the scales of the pages in ids
                 const int page_bits = 31 - __clz(T), box = min(T, kQStep), pages = kQStep / box;      // copies of a step
                 const int chunk_page = box < kQStep ? ((lane & 3) * 16) >> page_bits : 0;             // page of a chunk of 16 keys
                 int ids = -1, ids_end = 0;          // page numbers of 32 pages that end in front of ids_end, one a lane
                 for (int t = 0; t < n_t && ok; ++t) {
                     const int slot = t % kQStages;
                     if (t >= kQStages) {
-                        ok = __all_sync(0xFFFFFFFFu, wait_phase(&sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, 260));
+                        ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, 260));
                         if (!ok) break;
                     }
                     uint64_t* const full = &sm->st_full[kv][slot];
@@ -1083,23 +1132,12 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                             if (needed && reports) report_status(a.status, DAF_ERR_BOUNDS, 261, ids);
                             ids = -1;
                         }
-                    }
-                    const int at0 = page0 - (ids_end - 32);
-                    if (kv == 0) {
-                        // lanes 0-3: K's scales of the chunks, 4-7: V's
-                        const int id = __shfl_sync(0xFFFFFFFFu, ids, at0 + chunk_page);
-                        if (lane < 8) {
-                            float* const dst = &sm->scales[slot][lane];
-                            if (id >= 0) {
-                                const float* const src = (lane < 4 ? a.p.k_scale : a.p.v_scale) + (size_t)id * Hkv + h;
-                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-                                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
-                            } else {
-                                *dst = -1.f;
-                                mbar_arrive(full);
-                            }
+                        if (kv == 0) {
+                            ks = ids >= 0 ? __ldg(a.p.k_scale + (size_t)ids * Hkv + h) : -1.f;
+                            vs = ids >= 0 ? __ldg(a.p.v_scale + (size_t)ids * Hkv + h) : -1.f;
                         }
                     }
+                    const int at0 = page0 - (ids_end - 32);
                     const int mine = __shfl_sync(0xFFFFFFFFu, ids, (at0 + lane) & 31);
                     const unsigned there = __ballot_sync(0xFFFFFFFFu, lane < pages && mine >= 0);
                     if (lane == 0) mbar_arrive_expect_tx(full, (uint32_t)(__popc(there) * box * kD));
@@ -1108,6 +1146,19 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         tma_load_2d(stage_smem + (kv * kQStages + slot) * kQStage + lane * box * kD, kv == 0 ? &tmap_k : &tmap_v, full, 0,
                                     (mine * Hkv + h) * T + (key0 & (T - 1)));       // (not 0 only where a page holds several steps)
                     __syncwarp();
+                    if (kv == 0) {
+                        // the constants of the step's chunks, a lane each
+                        const float k1 = __shfl_sync(0xFFFFFFFFu, ks, at0 + chunk_page), v1 = __shfl_sync(0xFFFFFFFFu, vs, at0 + chunk_page);
+                        const bool missing = __any_sync(0xFFFFFFFFu, lane < 4 && k1 < 0.f);
+                        if (lane < 4) {
+                            const int bits = __float_as_int(v1), e = v1 > 0.f ? max((bits >> 23) - 127, -126) : 0;
+                            sm->chunk[t % kQConsts][lane] = make_float4(k1, (float)e, __int_as_float((127 - e) << 23),
+                                                                        v1 > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f);
+                            if (lane == 0) sm->missing[t % kQConsts] = missing;
+                            mbar_arrive(&sm->c_full[t % kQConsts]);
+                        }
+                        __syncwarp();
+                    }
                 }
                 if (!ok)       // loads in flight get a bounded chance to land before the CTA retires
                     for (int i = 0; i < kQStages && lane == 0; ++i)
@@ -1124,15 +1175,14 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     const int slot = t % kQStages, b = t & 1;
                     // one of the four warps polls, the others sleep at a barrier (twelve polling warps took half of the issue slots)
                     if (cw == 0) {
-                        bool there = wait_phase(&sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, 262);
-                        // (the constants of a step, written by a warp that widens K)
-                        if (kv == 1 && there) there = wait_phase(&sm->c_full[t & 7], (uint32_t)((t >> 3) & 1), abort, 275);
+                        bool there = wait_phase(sm, odd, &sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, 262);
+                        if (kv == 1 && there) there = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 275);
                         if (there && t >= 2) {
                             // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
                             const int u = pair ? t - 2 : (t >> 1) - 1;
                             uint64_t* const freed = (kv == 0 ? sm->s_full[0] : sm->pv_done[0]) + (u & 1);
-                            there = wait_phase(freed + (pair ? 0 : 2 * b), (uint32_t)((u >> 1) & 1), abort, 263);
-                            if (there && pair) there = wait_phase(freed + 2, (uint32_t)((u >> 1) & 1), abort, 264);
+                            there = wait_phase(sm, odd, freed + (pair ? 0 : 2 * b), (uint32_t)((u >> 1) & 1), abort, 263);
+                            if (there && pair) there = wait_phase(sm, odd, freed + 2, (uint32_t)((u >> 1) & 1), abort, 264);
                         }
                         there = __all_sync(0xFFFFFFFFu, there);
                         if (lane == 0) sm->go[kv][b] = there;
@@ -1141,17 +1191,8 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     if (!sm->go[kv][b]) break;
                     unsigned char* const src = stage_smem + (kv * kQStages + slot) * kQStage + (16 * cw + r8) * kD;
                     float vm = 1.f;
-                    if (kv == 0) {
-                        if (cw == 0 && lane < 4) {
-                            const float* const sc = sm->scales[slot];
-                            const float vs = sc[4 + lane];
-                            const int bits = __float_as_int(vs), e = vs > 0.f ? max((bits >> 23) - 127, -126) : 0;
-                            sm->chunk[t & 7][lane] = make_float4(sc[lane], (float)e, __int_as_float((127 - e) << 23),
-                                                                 vs > 0.f ? __int_as_float((bits & 0x7FFFFF) | 0x3F800000) : 1.f);
-                            if (lane == 0) sm->missing[t & 7] = sc[0] < 0.f || sc[1] < 0.f || sc[2] < 0.f || sc[3] < 0.f;
-                        }
-                    } else {
-                        const float4 sc = sm->chunk[t & 7][cw];
+                    if (kv == 1) {
+                        const float4 sc = sm->chunk[t % kQConsts][cw];
                         const int key0 = (step0 + t) * kQStep;
                         vm = sc.w;
                         if (key0 + kQStep - 1 > first_limit || sc.x < 0.f) {
@@ -1173,7 +1214,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         }
                     }
                     unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot + (16 * cw + r8) * 128;
-#pragma unroll 2
+#pragma unroll
                     for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
                         const uint4 w = *reinterpret_cast<const uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
                         uint32_t h[8] = {widen2(w.x), widen2(w.x >> 16), widen2(w.y), widen2(w.y >> 16),
@@ -1194,7 +1235,6 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        if (kv == 0 && cw == 0) mbar_arrive(&sm->c_full[t & 7]);
                         mbar_arrive(kv == 0 ? &sm->k_full[b] : &sm->v_full[b]);
                         mbar_arrive(&sm->st_empty[kv][slot]);
                     }
@@ -1222,10 +1262,10 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                                       k0 + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQSlotHalf / 16)), idesc_qk, kk > 0 ? 1u : 0u);
                         tc_commit(&sm->s_full[g][b]);
                     };
-                    ok = wait_phase(&sm->q_full[pair ? g : 0], 0, abort, 266);
+                    ok = wait_phase(sm, odd, &sm->q_full[pair ? g : 0], 0, abort, 266);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     for (int u = 0; u < 2 && u < n_u && ok; ++u) {
-                        ok = wait_phase(&sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 267);
+                        ok = wait_phase(sm, odd, &sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 267);
                         ok = __all_sync(0xFFFFFFFFu, ok);
                         if (!ok) break;
                         tc_fence_after();
@@ -1234,8 +1274,8 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     }
                     for (int u = 0; u < n_u && ok; ++u) {
                         const int b = u & 1;
-                        bool there = wait_phase(&sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 268);
-                        if (there) there = wait_phase(&sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, 269);
+                        bool there = wait_phase(sm, odd, &sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 268);
+                        if (there) there = wait_phase(sm, odd, &sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, 269);
                         ok = __all_sync(0xFFFFFFFFu, there);
                         if (!ok) break;
                         tc_fence_after();
@@ -1249,7 +1289,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         }
                         __syncwarp();
                         if (u + 2 < n_u) {
-                            ok = __all_sync(0xFFFFFFFFu, wait_phase(&sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, 270));
+                            ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, 270));
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) issue_qk(b);
@@ -1281,64 +1321,82 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
 // to L2, so a warp asks for its first kAtOnce partials together with the row's maxima: few rows with many partials (one answer over a
 // long context: 37) take eight warps a row, many rows with few partials one.
 template <int kWarps>
-__global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, int block_rows) {
+__global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, int block_rows, int ctas) {
     constexpr int kRows = 8 / kWarps, kAtOnce = kWarps == 1 ? 8 : 5;
     __shared__ float4 acc_s[8][32];
     __shared__ float sum_s[8];
+    __shared__ int begin_cta[256], counts[8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
     pdl_wait();
     pdl_launch_dependents();
-    const ChainEntry e = a.chains[blockIdx.x];
-    if (e.last_cta < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
-    const int first = blockIdx.x, r = blockIdx.y * kRows + warp / kWarps;
-    const int row = e.block * block_rows + r;
-    const bool there = r < block_rows && row < a.rows;
-    // partial i of the row: the first CTA's second set, then the following CTAs' first sets
-    const int n = there ? e.last_cta - first + 1 : 0;
-    auto at = [&](int i) { return (i == 0 ? (size_t)first * 2 + 1 : (size_t)(first + i) * 2) * block_rows + r; };
-    float2 ml[kAtOnce];
-    float4 v[kAtOnce];
+    // the CTAs that begin such a segment, in order: every block numbers them alike (at most 256 CTAs, a thread each)
+    const bool begins = (int)threadIdx.x < ctas && a.chains[threadIdx.x].last_cta >= 0;
+    const unsigned some = __ballot_sync(0xFFFFFFFFu, begins);
+    if (lane == 0) counts[warp] = __popc(some);
+    __syncthreads();
+    int n_begin = 0, before = __popc(some & ((1u << lane) - 1u));
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-        const int i = part + u * kWarps;
-        ml[u] = i < n ? __ldcg(a.part_ml + at(i)) : make_float2(-INFINITY, 0.f);
-        v[u] = i < n ? __ldcg(reinterpret_cast<const float4*>(a.part_o + at(i) * kD) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = 0; w < 8; ++w) {
+        if (w < warp) before += counts[w];
+        n_begin += counts[w];
     }
-    float mx = -INFINITY;
-    for (int i = lane; i < n; i += 32) mx = fmaxf(mx, __ldcg(&a.part_ml[at(i)].x));
+    if (begins) begin_cta[before] = (int)threadIdx.x;
+    __syncthreads();
+    const int groups = (block_rows + kRows - 1) / kRows;
+    for (int item = blockIdx.x; item < n_begin * groups; item += gridDim.x) {
+        const int first = begin_cta[item / groups], r = (item % groups) * kRows + warp / kWarps;
+        const ChainEntry e = a.chains[first];
+        const int row = e.block * block_rows + r;
+        const bool there = r < block_rows && row < a.rows;
+        // partial i of the row: the first CTA's second set, then the following CTAs' first sets
+        const int n = there ? e.last_cta - first + 1 : 0;
+        auto at = [&](int i) { return (i == 0 ? (size_t)first * 2 + 1 : (size_t)(first + i) * 2) * block_rows + r; };
+        float2 ml[kAtOnce];
+        float4 v[kAtOnce];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    auto add = [&](float2 x, float4 y) {
-        const float w = partial_weight(x, mx);
-        if (w == 0.f) return;
-        sum += w * x.y;
-        acc.x += w * y.x; acc.y += w * y.y; acc.z += w * y.z; acc.w += w * y.w;
-    };
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) add(ml[u], v[u]);
-#pragma unroll 4
-    for (int i = part + kAtOnce * kWarps; i < n; i += kWarps)
-        add(__ldcg(a.part_ml + at(i)), __ldcg(reinterpret_cast<const float4*>(a.part_o + at(i) * kD) + lane));
-    if (kWarps > 1) {
-        acc_s[warp][lane] = acc;
-        if (lane == 0) sum_s[warp] = sum;
-        __syncthreads();
-        if (part != 0) return;
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) {
-            const float4 y = acc_s[warp + w][lane];
-            acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
-            sum += sum_s[warp + w];
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = part + u * kWarps;
+            ml[u] = i < n ? __ldcg(a.part_ml + at(i)) : make_float2(-INFINITY, 0.f);
+            v[u] = i < n ? __ldcg(reinterpret_cast<const float4*>(a.part_o + at(i) * kD) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
+        float mx = -INFINITY;
+        for (int i = lane; i < n; i += 32) mx = fmaxf(mx, __ldcg(&a.part_ml[at(i)].x));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+        auto add = [&](float2 x, float4 y) {
+            const float w = partial_weight(x, mx);
+            if (w == 0.f) return;
+            sum += w * x.y;
+            acc.x += w * y.x; acc.y += w * y.y; acc.z += w * y.z; acc.w += w * y.w;
+        };
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) add(ml[u], v[u]);
+#pragma unroll 4
+        for (int i = part + kAtOnce * kWarps; i < n; i += kWarps)
+            add(__ldcg(a.part_ml + at(i)), __ldcg(reinterpret_cast<const float4*>(a.part_o + at(i) * kD) + lane));
+        if (kWarps > 1) {
+            __syncthreads();
+            acc_s[warp][lane] = acc;
+            if (lane == 0) sum_s[warp] = sum;
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll
+                for (int w = 1; w < kWarps; ++w) {
+                    const float4 y = acc_s[warp + w][lane];
+                    acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
+                    sum += sum_s[warp + w];
+                }
+            }
+        }
+        if (!there || part != 0) continue;
+        const int tok = row / a.G, head = e.h * a.G + row % a.G;
+        const float inv = row_inverse(sum);
+        reinterpret_cast<uint2*>(a.out + (((size_t)e.b * a.L_q + tok) * a.Hq + head) * kD)[lane] =
+            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (a.lse != nullptr && lane == 0) a.lse[((size_t)e.b * a.Hq + head) * a.L_q + tok] = row_lse(mx, sum);
     }
-    if (!there) return;
-    const int tok = row / a.G, head = e.h * a.G + row % a.G;
-    const float inv = row_inverse(sum);
-    reinterpret_cast<uint2*>(a.out + (((size_t)e.b * a.L_q + tok) * a.Hq + head) * kD)[lane] =
-        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    if (a.lse != nullptr && lane == 0) a.lse[((size_t)e.b * a.Hq + head) * a.L_q + tok] = row_lse(mx, sum);
 }
 
 // ------------------------------------------------------------------------------------------------------------------ host side
@@ -1396,16 +1454,19 @@ static cudaError_t launch_decode(const PageAttnArgs& a, int ctas, cudaStream_t s
     return launch_kernel(page_decode_kernel<kN>, dim3(ctas), dim3(decode_warps(kN) * 32), decode_smem(kN) + prefix_bytes(a.n), stream, a);
 }
 
+// One CTA an SM (the merge keeps the numbers of up to 256 of them).
+static int page_ctas() { return num_sms() < 256 ? num_sms() : 256; }
+
 size_t page_attn_scratch_bytes(int n, int L_q, int Hq, int Hkv) {
     (void)n;
-    const int ctas = num_sms();
+    const int ctas = page_ctas();
     const size_t rows = partial_rows(ctas, few_blocks(L_q * (Hq / Hkv)));
     return round256((size_t)ctas * sizeof(ChainEntry)) + round256(rows * sizeof(float2)) + rows * kD * sizeof(float);
 }
 
 int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t* lens, int L_q, int Hq, float scale, const void* q,
                      const int32_t* table, void* out, float* lse, DeviceStatus* status, void* scratch, cudaStream_t stream) {
-    const int ctas = num_sms();
+    const int ctas = page_ctas();
     PageAttnArgs a;
     a.p = pool; a.n = n; a.L_q = L_q; a.Hq = Hq; a.G = Hq / pool.Hkv;
     a.rows = L_q * a.G;
@@ -1449,8 +1510,8 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     }
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
-    e = few ? launch_kernel(page_merge_kernel<8>, dim3(ctas, 8 * blocks), dim3(256), 0, stream, a, 8 * blocks)
-            : launch_kernel(page_merge_kernel<1>, dim3(ctas, kQRows / 8), dim3(256), 0, stream, a, (int)kQRows);
+    e = few ? launch_kernel(page_merge_kernel<8>, dim3(2 * ctas), dim3(256), 0, stream, a, 8 * blocks, ctas)
+            : launch_kernel(page_merge_kernel<1>, dim3(3 * ctas), dim3(256), 0, stream, a, (int)kQRows, ctas);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
     return check_launch();
