@@ -1329,23 +1329,29 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
     pdl_wait();
     pdl_launch_dependents();
-    // the CTAs that begin such a segment, in order: every block numbers them alike (at most 256 CTAs, a thread each)
-    const bool begins = (int)threadIdx.x < ctas && a.chains[threadIdx.x].last_cta >= 0;
-    const unsigned some = __ballot_sync(0xFFFFFFFFu, begins);
-    if (lane == 0) counts[warp] = __popc(some);
-    __syncthreads();
-    int n_begin = 0, before = __popc(some & ((1u << lane) - 1u));
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        if (w < warp) before += counts[w];
-        n_begin += counts[w];
-    }
-    if (begins) begin_cta[before] = (int)threadIdx.x;
-    __syncthreads();
+    // Few rows: a block per CTA and row.  Many: the CTAs that begin such a segment, in order, so that every block numbers them alike
+    // (at most 256, a thread each), since most blocks of a full grid would only find that there is nothing to do.
     const int groups = (block_rows + kRows - 1) / kRows;
-    for (int item = blockIdx.x; item < n_begin * groups; item += gridDim.x) {
-        const int first = begin_cta[item / groups], r = (item % groups) * kRows + warp / kWarps;
+    int n_begin = 1;
+    if (kWarps == 1) {
+        const bool begins = (int)threadIdx.x < ctas && a.chains[threadIdx.x].last_cta >= 0;
+        const unsigned some = __ballot_sync(0xFFFFFFFFu, begins);
+        if (lane == 0) counts[warp] = __popc(some);
+        __syncthreads();
+        int before = __popc(some & ((1u << lane) - 1u));
+        n_begin = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if (w < warp) before += counts[w];
+            n_begin += counts[w];
+        }
+        if (begins) begin_cta[before] = (int)threadIdx.x;
+        __syncthreads();
+    }
+    for (int item = kWarps == 1 ? blockIdx.x : blockIdx.y; item < n_begin * groups; item += kWarps == 1 ? gridDim.x : gridDim.y) {
+        const int first = kWarps == 1 ? begin_cta[item / groups] : blockIdx.x, r = (item % groups) * kRows + warp / kWarps;
         const ChainEntry e = a.chains[first];
+        if (kWarps > 1 && e.last_cta < 0) return;
         const int row = e.block * block_rows + r;
         const bool there = r < block_rows && row < a.rows;
         // partial i of the row: the first CTA's second set, then the following CTAs' first sets
@@ -1510,7 +1516,7 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     }
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
-    e = few ? launch_kernel(page_merge_kernel<8>, dim3(2 * ctas), dim3(256), 0, stream, a, 8 * blocks, ctas)
+    e = few ? launch_kernel(page_merge_kernel<8>, dim3(ctas, 8 * blocks), dim3(256), 0, stream, a, 8 * blocks, ctas)
             : launch_kernel(page_merge_kernel<1>, dim3(3 * ctas), dim3(256), 0, stream, a, (int)kQRows, ctas);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
