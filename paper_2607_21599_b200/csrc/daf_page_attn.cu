@@ -637,36 +637,37 @@ page_decode_kernel(const PageAttnArgs a) {
 // ---------------------------------------------------------------------------------------------- many rows: tensor memory
 // More than 24 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
 // of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 20 warps:
-//   10, 11  ask for the bytes of K and V (TMA, kQStages steps ahead) and their scales;
-//   12-15, 16-19  widen K's, and V's, to fp16, exactly, into the two-slot rings that the products read (128-byte swizzle).  Each of
+//   10, 11  ask for the bytes of K and V (TMA, kQStages steps ahead);
+//   12-15, 16-19  widen K's, and V's, to fp16, exactly, into four-slot rings that the products read (128-byte swizzle).  Each of
 //          these is a chain of waits, reads, conversions and writes, so K and V have warps of their own;
-//   8, 9   issue a tile group's products: S = Q K^T into one of two halves, O += P V with P from tensor memory;
+//   8, 9   issue a tile group's products: S = Q K^T with Q from tensor memory, O += P V with P from tensor memory, over S;
 //   0-3, 4-7  a tile group's softmax, a row per thread, and its epilogue.
-// A block of two tiles shares every widened K and V (the bytes pass through shared memory once for both, and shared memory is what
-// bounds this loop: per step 64 KB of operand reads for each tile, 32 KB written and 32 KB of bytes in and out).  A block of one tile
-// gives its even steps to one group and its odd ones to the other, and the two halves of the result are merged in shared memory.
+// A block of two tiles shares every widened K and V.  A block of one tile gives its even steps to one group and its odd ones to the
+// other, and the two halves of the result are merged in shared memory.  A group's 256 columns of tensor memory: O 128, Q (fp16) 64,
+// S 64.  One S is enough because the groups take turns: while one's products run, the other's softmax does; and with Q there instead
+// of in shared memory a step of two tiles passes 128 KB through shared memory (64 of operand reads, 32 written and 32 of bytes in and
+// out) instead of 192, which had bound the loop.
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 64;
 constexpr int kQStages = 4;
-constexpr int kQConsts = 16;       // steps whose constants are kept: they are written up to kQStages + 6 steps ahead of their last reader
+constexpr int kQSlots = 4;
+constexpr int kQConsts = 16;       // steps whose constants are kept: they are written up to kQStages + kQSlots + 2 steps ahead of their last reader
 constexpr int kQRows = 256;
 constexpr int kQThreads = 640;
-constexpr int kQTile = 128 * kD * 2;                  // 32 KB: 128 rows of Q, two 64-column halves
-constexpr int kQHalf = kQTile / 2;
 constexpr int kQSlot = kQStep * kD * 2;               // 16 KB: K or V of a step, widened, two 64-column halves
 constexpr int kQSlotHalf = kQSlot / 2;
 constexpr int kQStage = kQStep * kD;                  // 8 KB: the bytes of K or V of a step
+constexpr int kQRing = kQSlots * kQSlot;              // 64 KB; V's holds the raw rows of Q (two tiles of 32 KB) when a piece begins
+constexpr uint32_t kColQ = 128, kColS = 192;          // columns of a group, behind O
 constexpr float kLazy = 6.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
 
 struct QuestionSmem {
-    uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V]
-    uint64_t k_full[2], v_full[2];
-    uint64_t q_full[2];
-    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];      // [group][half]
+    uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V] a step's bytes
+    uint64_t full[2][kQSlots], empty[2][kQSlots];             // [K, V] its widened rows
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];      // [group]
     uint64_t c_full[kQConsts];
     float4 chunk[kQConsts][4];      // of a step's chunks of 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
     int missing[kQConsts];          // some keys of the step have no page
-    float row_factor[2][128];       // what a row's logits are to be multiplied by, apart from ks
     float2 ml[128];                 // the second group's row maxima and sums (blocks of one tile)
     uint32_t tmem_base;
     int abort_flag;
@@ -680,12 +681,12 @@ struct QuestionSmem {
     Shares shares;
     ChainEntry chain;
 };
-constexpr int kBarEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK = (int)(offsetof(QuestionSmem, k_full) / 8),
-              kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8), kBarS = (int)(offsetof(QuestionSmem, s_full) / 8),
-              kBarP = (int)(offsetof(QuestionSmem, p_full) / 8), kBarPv = (int)(offsetof(QuestionSmem, pv_done) / 8),
-              kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
-static_assert(offsetof(QuestionSmem, st_full) == 0 && kQStages == 4 && (kBarS & 1) == 0 && kBars <= 64, "what bar_uses and wait_phase rest on");
-constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQTile + 4 * (size_t)kQSlot + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
+constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarFull = (int)(offsetof(QuestionSmem, full) / 8),
+              kBarEmpty = (int)(offsetof(QuestionSmem, empty) / 8), kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
+              kBarS = (int)(offsetof(QuestionSmem, s_full) / 8), kBarP = (int)(offsetof(QuestionSmem, p_full) / 8),
+              kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
+static_assert(offsetof(QuestionSmem, st_full) == 0 && kQStages == 4 && kQSlots == 4 && (kBarS & 1) == 0 && kBars <= 64, "what the barriers' numbers rest on");
+constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQRing + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
 __host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
     return (1u << 4) | (b_mn_major << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);      // fp16 x fp16 -> fp32
@@ -772,19 +773,18 @@ __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4*
 
 // How many phases barrier i completes in a piece of n_t steps.
 __device__ __forceinline__ int bar_uses(int i, int n_t, bool pair) {
-    if (i < kBarK) return (n_t - (i & 3) + 3) >> 2;                      // every fourth step (kQStages)
-    if (i < kBarQ) return (n_t - (i & 1) + 1) >> 1;
-    if (i < kBarS) return i == kBarQ || pair ? 1 : 0;
+    if (i < kBarQ) return (n_t - (i & 3) + 3) >> 2;                      // every fourth step
     if (i < kBarC) {
-        const int j = (i - kBarS) & 3, steps = pair ? n_t : (n_t - (j >> 1) + 1) >> 1;       // of the group
-        return (steps - (j & 1) + 1) >> 1;
+        const int g = i & 1, steps = pair ? n_t : (n_t - g + 1) >> 1;    // of the group
+        return i < kBarS ? 1 : i < kBarO ? steps : (steps > 0 ? 1 : 0);
     }
     return i < kBars ? (n_t - (i - kBarC) + kQConsts - 1) / kQConsts : 0;
 }
 
-// The bounded wait of this kernel, `parity` as if the piece of work were the CTA's first (a second at most, or until another thread has given up): it only leaves the number of the wait in
-// the abort flag, which one thread reports at the end.  The warps' loops are many, and what they keep in the instruction caches
-// counts: with longer waits and every rare case unrolled, warps that had work found no instruction a sixth of the time.
+// The bounded wait of this kernel, `parity` as if the piece of work were the CTA's first (a second at most, or until another thread has
+// given up): it only leaves the number of the wait in the abort flag, which one thread reports at the end.  The warps' loops are
+// many, and what they keep in the instruction caches counts: with longer waits and every rare case unrolled, warps that had work
+// found no instruction a sixth of the time.
 __device__ __forceinline__ bool wait_phase(QuestionSmem* sm, unsigned long long odd, uint64_t* bar, uint32_t parity, volatile int* abort, int where) {
     parity ^= (uint32_t)(odd >> ((smem_u32(bar) - smem_u32(sm)) >> 3)) & 1u;
     if (mbar_try_wait(bar, parity)) return true;
@@ -805,10 +805,8 @@ __global__ void __launch_bounds__(kQThreads, 1)
 page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
     extern __shared__ unsigned char question_smem_raw[];
     unsigned char* const smem = question_smem_raw + ((1024u - (smem_u32(question_smem_raw) & 1023u)) & 1023u);      // (stays a shared address to the compiler)
-    unsigned char* const q_smem = smem;                          // two tiles
-    unsigned char* const k_smem = q_smem + 2 * kQTile;           // two slots
-    unsigned char* const v_smem = k_smem + 2 * kQSlot;
-    unsigned char* const stage_smem = v_smem + 2 * kQSlot;
+    unsigned char* const ring = smem;                            // K's four slots, then V's
+    unsigned char* const stage_smem = ring + 2 * kQRing;
     QuestionSmem* const sm = reinterpret_cast<QuestionSmem*>(stage_smem + 2 * kQStages * kQStage);
     int* const pre = reinterpret_cast<int*>(sm + 1);
     __shared__ int warp_sums[kQThreads / 32];
@@ -826,11 +824,11 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         tma_prefetch_desc(&tmap_v);
     }
     if (warp == 1) {
-        uint64_t* const bars = reinterpret_cast<uint64_t*>(stage_smem + 2 * kQStages * kQStage);
+        uint64_t* const bars = reinterpret_cast<uint64_t*>(sm);
         for (int i = lane; i < kBars; i += 32) {
-            // four warps (or lanes) arrive; at the others a copy's bytes or a product
-            const bool by_four = (i >= kBarEmpty && i < kBarS) || (i >= kBarP && i < kBarPv) || i >= kBarC;
-            mbar_init(bars + i, by_four ? 4 : 1);
+            // four warps (or lanes) arrive, or both groups' products, or one copy's bytes or product
+            const bool by_four = (i >= kBarStEmpty && i < kBarEmpty) || (i >= kBarQ && i < kBarS) || (i >= kBarP && i < kBarO) || i >= kBarC;
+            mbar_init(bars + i, by_four ? 4 : i >= kBarEmpty && i < kBarQ ? 2 : 1);
         }
         mbar_fence_init();
     }
@@ -842,20 +840,24 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     tc_fence_after();
     const uint32_t tmem = sm->tmem_base;
     const int T = a.p.T, Hkv = a.p.Hkv;
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
         const long long total = (long long)pre[a.n] * Hkv * a.units;
         const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than four steps of a tile each
         const Shares shares = share(total, ctas);
-        const long long c_lo = cta_begin(shares, min((long long)blockIdx.x, ctas)), c_hi = cta_begin(shares, min((long long)blockIdx.x + 1, ctas));
-        // both ends move up to the next step's begin
+        // lane 0 finds the stretch's begin, lane 1 its end; both move up to the next step's begin
+        const long long from = cta_begin(shares, min((long long)blockIdx.x + min(lane, 1), ctas));
         Place at = {};
-        sm->x = sm->hi = total;
-        if (c_hi < total) { at = place_at<2>(a, pre, c_hi); sm->hi = axis_at<2>(a, pre, at); }
-        if (c_lo < total) { at = place_at<2>(a, pre, c_lo); sm->x = axis_at<2>(a, pre, at); }
-        sm->at = at;
-        sm->step1 = 0;
-        sm->shares = shares;
-        sm->chain = ChainEntry{-1, 0, 0, 0};
+        long long x = total;
+        if (from < total) { at = place_at<2>(a, pre, from); x = axis_at<2>(a, pre, at); }
+        const long long hi = __shfl_sync(0xFFFFFFFFu, x, 1);
+        if (lane == 0) {
+            sm->x = x;
+            sm->hi = hi;
+            sm->at = at;
+            sm->step1 = 0;
+            sm->shares = shares;
+            sm->chain = ChainEntry{-1, 0, 0, 0};
+        }
     }
     // Three of the five warpgroups need few registers: 256 x 144 + 384 x 64 = 640 x 96
     if (warp < 8) {
@@ -873,7 +875,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const Place at = sm->at;
                 sm->step1 = 0;
                 if (sm->x < sm->hi) {
-                    const int step1 = (int)min((long long)at.n_steps, at.step + (sm->hi - sm->x) / at.width);
+                    const int step1 = (int)min((long long)at.n_steps, at.step + ((sm->hi - sm->x) >> (at.width - 1)));       // (a width is 1 or 2)
                     const int row0 = at.block * kQRows, last_row = min(a.rows, row0 + kQRows) - 1;
                     sm->step1 = step1;
                     sm->first_limit = at.len - a.L_q + row0 / a.G;
@@ -888,9 +890,9 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 sm->poison = 0;
             }
             // The barriers count on from piece to piece: bit i of `odd` says whether barrier i has completed an odd number of phases.
-            if (warp == 1) {
-                const unsigned first = __ballot_sync(0xFFFFFFFFu, any_before && (bar_uses(lane, prev_t, prev_pair) & 1));
-                const unsigned second = __ballot_sync(0xFFFFFFFFu, any_before && (bar_uses(lane + 32, prev_t, prev_pair) & 1));
+            if (warp == 1 && any_before) {
+                const unsigned first = __ballot_sync(0xFFFFFFFFu, bar_uses(lane, prev_t, prev_pair) & 1);
+                const unsigned second = __ballot_sync(0xFFFFFFFFu, bar_uses(lane + 32, prev_t, prev_pair) & 1);
                 if (lane == 0) sm->odd ^= ((unsigned long long)second << 32) | first;
             }
             __syncthreads();
@@ -902,108 +904,113 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             prev_t = n_t; prev_pair = pair; any_before = true;
             // ------------------------------------------------------------------------------------- softmax, a row per thread
             const int g = warp >> 2, rt = threadIdx.x & 127;
-            const int row = sm->at.block * kQRows + (pair ? g * 128 : 0) + rt;
+            const int tile_row = sm->at.block * kQRows + (pair ? g * 128 : 0), row = tile_row + rt;
             const bool valid = row < a.rows;
-            const int limit = valid ? sm->at.len - a.L_q + row / a.G : sm->last_limit;
-            const int n_u = pair ? n_t : (n_t - g + 1) / 2;
+            const int tok = row / a.G, head = row - tok * a.G;          // (head of the group)
+            const int limit = valid ? sm->at.len - a.L_q + tok : sm->last_limit;
+            const int n_u = pair ? n_t : (n_t - g + 1) >> 1;
+            const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+            const uint32_t o_addr = tmem + (uint32_t)(g * 256) + lane_addr, s_addr = o_addr + kColS;
+            float c;
             {
-                // The warp's 32 rows of Q, sixteen lanes a row, each row scaled to a largest magnitude of 2^14 .. 2^15, as fp16 in the
-                // layout of a tiled copy.  (A row a thread, its loads scattered over 32 rows, took 6 us a piece.)
-                const int sub = lane >> 4, cidx = lane & 15, r0 = (warp & 3) * 32 + sub;
-                const int from = sm->at.block * kQRows + (pair ? g * 128 : 0) + r0, d_tok = 2 / a.G, d_head = 2 % a.G;
-                int tok = from / a.G, head = from - tok * a.G;
-                const __nv_bfloat16* const src = a.q + ((size_t)sm->at.b * a.L_q * a.Hq + sm->at.h * a.G) * kD + cidx * 8;
+                // The warp's 32 rows of Q: raw into the ring that V's widened rows will use, sixteen lanes a row, pieces of 16 bytes XOR-ed with
+                // the row number.  Each thread then scales its own row to a largest magnitude of 2^14 .. 2^15 and puts it into tensor
+                // memory as fp16.  (Both groups of a block of one tile load the same rows; only the first puts them there.)
+                const int sub = lane >> 4, piece = lane & 15, r0 = (warp & 3) * 32 + sub, d_tok = 2 / a.G, d_head = 2 % a.G;
+                unsigned char* const raw = ring + kQRing + g * (128 * 256);
+                int tk = (tile_row + r0) / a.G, hd = tile_row + r0 - tk * a.G;
+                const __nv_bfloat16* src = a.q + (((size_t)sm->at.b * a.L_q + tk) * a.Hq + sm->at.h * a.G + hd) * kD + piece * 8;
+#pragma unroll 2
+                for (int r = r0; r < r0 + 32; r += 2) {
+                    const bool there = tile_row + r < a.rows;
+                    cp_async16(smem_u32(raw + r * 256 + ((piece ^ (r & 15)) << 4)), there ? src : a.q, there ? 16u : 0u);
+                    src += ((long long)d_tok * a.Hq + d_head) * kD;
+                    hd += d_head;
+                    if (hd >= a.G) { hd -= a.G; src += (long long)(a.Hq - a.G) * kD; }
+                }
+                cp_async_commit();
+                cp_async_wait_group<0>();
+                __syncwarp();
+                const uint4* const mine = reinterpret_cast<const uint4*>(raw + rt * 256);
+                uint32_t big = 0;
+#pragma unroll 4
+                for (int i = 0; i < 16; ++i) {
+                    const uint4 w = mine[i ^ (rt & 15)];
 #pragma unroll
-                for (int i0 = 0; i0 < 16; i0 += 8) {
-                    uint4 w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        w[i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (from + 2 * (i0 + i) < a.rows) w[i] = __ldg(reinterpret_cast<const uint4*>(src + ((size_t)tok * a.Hq + head) * kD));
-                        tok += d_tok; head += d_head;
-                        if (head >= a.G) { head -= a.G; ++tok; }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int r = r0 + 2 * (i0 + i);
-                        uint32_t* const x = &w[i].x;
-                        uint32_t big = 0;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t b0 = x[j] & 0x7FFFu, b1 = (x[j] >> 16) & 0x7FFFu;
-                            big = max(big, max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u));
-                        }
-#pragma unroll
-                        for (int d = 1; d < 16; d <<= 1) big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, d));
-                        const int e = max((int)(big >> 7) - 127, -100);
-                        const float up = __int_as_float((14 - e + 127) << 23);
-                        if (cidx == 0) sm->row_factor[g][r] = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] = pack_f16(__uint_as_float(x[j] << 16) * up, __uint_as_float(x[j] & 0xFFFF0000u) * up);
-                        if (pair || g == 0)
-                            *reinterpret_cast<uint4*>(q_smem + g * kQTile + (cidx >> 3) * kQHalf + r * 128 + (((cidx & 7) ^ (r & 7)) << 4)) = w[i];
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t x = (j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w), b0 = x & 0x7FFFu, b1 = (x >> 16) & 0x7FFFu;
+                        big = max(big, max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u));
                     }
                 }
-                if (pair || g == 0) fence_proxy_async();
+                const int e = max((int)(big >> 7) - 127, -100);
+                const float up = __int_as_float((14 - e + 127) << 23);
+                c = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
+                if (pair || g == 0) {
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t y[16];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint4 w = mine[(4 * i + j) ^ (rt & 15)];
+                            y[4 * j] = pack_f16(__uint_as_float(w.x << 16) * up, __uint_as_float(w.x & 0xFFFF0000u) * up);
+                            y[4 * j + 1] = pack_f16(__uint_as_float(w.y << 16) * up, __uint_as_float(w.y & 0xFFFF0000u) * up);
+                            y[4 * j + 2] = pack_f16(__uint_as_float(w.z << 16) * up, __uint_as_float(w.z & 0xFFFF0000u) * up);
+                            y[4 * j + 3] = pack_f16(__uint_as_float(w.w << 16) * up, __uint_as_float(w.w & 0xFFFF0000u) * up);
+                        }
+                        tmem_st16(o_addr + kColQ + (uint32_t)(16 * i), y);
+                    }
+                    tc_wait_st();
+                    tc_fence_before();
+                }
                 __syncwarp();
-                if (lane == 0 && (pair || g == 0)) mbar_arrive(&sm->q_full[g]);
+                if (lane == 0) mbar_arrive(&sm->q_full[g]);
             }
-            const float c = sm->row_factor[g][rt];
-            const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-            const uint32_t s_addr = tmem + (uint32_t)(g * 256) + lane_addr, o_addr = s_addr + 128u;
             float m = -INFINITY, l = 0.f;
             for (int u = 0; u < n_u; ++u) {
-                const int t = pair ? u : 2 * u + g, b = u & 1;
+                const int t = pair ? u : 2 * u + g;
                 ok = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 271);
-                if (ok) ok = wait_phase(sm, odd, &sm->s_full[g][b], (uint32_t)((u >> 1) & 1), abort, 272);
+                if (ok) ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const float alpha = question_softmax(s_addr + (uint32_t)(b * kQStep), sm->chunk[t % kQConsts], sm->missing[t % kQConsts] != 0, (step0 + t) * kQStep, limit, c, m, l);
+                const float alpha = question_softmax(s_addr, sm->chunk[t % kQConsts], sm->missing[t % kQConsts] != 0, (step0 + t) * kQStep, limit, c, m, l);
                 if (u > 0 && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
-                    // the product before must have completed before O is touched
-                    ok = wait_phase(sm, odd, &sm->pv_done[g][(u - 1) & 1], (uint32_t)(((u - 1) >> 1) & 1), abort, 273);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t r[32];
-                        tmem_ld32(o_addr + (uint32_t)(32 * i), r);
+                    // (the logits came behind the product before, so O is quiet)
+#pragma unroll 1
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t r[16];
+                        tmem_ld16(o_addr + (uint32_t)(16 * i), r);
                         tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
-                        tmem_st32(o_addr + (uint32_t)(32 * i), r);
+                        for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
+                        tmem_st16(o_addr + (uint32_t)(16 * i), r);
                     }
                 }
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sm->p_full[g][b]);
+                if (lane == 0) mbar_arrive(&sm->p_full[g]);
             }
-            // both last products (each on a barrier of its own)
-            for (int u = max(0, n_u - 2); u < n_u && ok; ++u) {
-                ok = wait_phase(sm, odd, &sm->pv_done[g][u & 1], (uint32_t)((u >> 1) & 1), abort, 274);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-            }
+            if (ok && n_u > 0) ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->o_full[g], 0, abort, 274));
             tc_fence_after();
-            // ---- epilogue.  A block of one tile: the second group hands its rows to the first through the rings, which are idle now.
+            // ---- epilogue, through the rings once both groups are done with them.  A block of one tile: the second group hands its rows to
+            // the first.
             float w0 = 1.f, w1 = 0.f;
-            float* const other = reinterpret_cast<float*>(k_smem) + rt * kD;
-            static_assert(4 * kQSlot >= 128 * kD * (int)sizeof(float), "the rings hold a tile of fp32 rows");
+            float* const other = reinterpret_cast<float*>(ring + kQRing) + rt * kD;
+            static_assert(kQRing >= 128 * kD * (int)sizeof(float) && kQRing >= 8 * 8192, "a tile of fp32 rows, and 8 KB a warp");
+            asm volatile("bar.sync 1, 256;" ::: "memory");
             if (!pair) {
-                asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (g == 1 && ok) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t r[32];
+#pragma unroll 1
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t r[16];
                         if (n_u > 0) {
-                            tmem_ld32(o_addr + (uint32_t)(32 * i), r);
+                            tmem_ld16(o_addr + (uint32_t)(16 * i), r);
                             tc_wait_ld();
                         }
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            *reinterpret_cast<float4*>(other + (((8 * i + j / 4) ^ lane) << 2)) =
+                        for (int j = 0; j < 16; j += 4)
+                            *reinterpret_cast<float4*>(other + (((4 * i + j / 4) ^ lane) << 2)) =
                                 n_u > 0 ? make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]))
                                         : make_float4(0.f, 0.f, 0.f, 0.f);
                     }
@@ -1021,13 +1028,12 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             }
             if (ok && (pair || g == 0)) {      // (whole warps: the reads of tensor memory are theirs)
                 const Place at = sm->at;
-                const int tok = row / a.G, head = at.h * a.G + row % a.G;
                 const bool begins = step0 == 0, whole = begins && sm->step1 == at.n_steps;
                 const float inv = row_inverse(l);
-                // Rows leave through the tile of Q, which is done with: 256 bytes of each of the warp's 32 rows at a time (a whole bf16 row,
-                // or half of an fp32 one), 16-byte pieces XOR-ed with the row number, and out again with sixteen lanes a row.
-                unsigned char* const stage = q_smem + (pair ? g : 0) * kQTile + (warp & 3) * 8192;
-                const size_t out_row = ((size_t)at.b * a.L_q + tok) * a.Hq + head;
+                // 256 bytes of each of the warp's 32 rows at a time (a whole bf16 row, or half of an fp32 one), 16-byte pieces XOR-ed with the
+                // row number, and out again with sixteen lanes a row.
+                unsigned char* const stage = ring + warp * 8192;
+                const size_t out_row = ((size_t)at.b * a.L_q + tok) * a.Hq + at.h * a.G + head;
                 const size_t set_row = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
                 const unsigned long long dst = reinterpret_cast<unsigned long long>(whole ? reinterpret_cast<char*>(a.out) + out_row * (kD * 2)
                                                                                           : reinterpret_cast<char*>(a.part_o) + set_row * (kD * 4));
@@ -1090,11 +1096,11 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 }
                 if (valid) {
                     if (!whole) a.part_ml[set_row] = make_float2(m, l);
-                    else if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + head) * a.L_q + tok] = row_lse(m, l);
+                    else if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + at.h * a.G + head) * a.L_q + tok] = row_lse(m, l);
                 }
             }
             tc_fence_before();
-            __syncthreads();       // the barriers, rings and tensor memory are free
+            __syncthreads();       // the rings and tensor memory are free
             tc_fence_after();
             if (sm->abort_flag != 0) break;
         }
@@ -1172,24 +1178,22 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
                 const int kv = warp >= 16;
                 for (int t = 0; t < n_t; ++t) {
-                    const int slot = t % kQStages, b = t & 1;
+                    const int slot = t % kQSlots;
                     // one of the four warps polls, the others sleep at a barrier (twelve polling warps took half of the issue slots)
                     if (cw == 0) {
-                        bool there = wait_phase(sm, odd, &sm->st_full[kv][slot], (uint32_t)((t / kQStages) & 1), abort, 262);
+                        bool there = wait_phase(sm, odd, &sm->st_full[kv][t % kQStages], (uint32_t)((t / kQStages) & 1), abort, 262);
                         if (kv == 1 && there) there = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 275);
-                        if (there && t >= 2) {
-                            // the step whose products read this slot before: of both groups, or of the one that has the slot to itself
-                            const int u = pair ? t - 2 : (t >> 1) - 1;
-                            uint64_t* const freed = (kv == 0 ? sm->s_full[0] : sm->pv_done[0]) + (u & 1);
-                            there = wait_phase(sm, odd, freed + (pair ? 0 : 2 * b), (uint32_t)((u >> 1) & 1), abort, 263);
-                            if (there && pair) there = wait_phase(sm, odd, freed + 2, (uint32_t)((u >> 1) & 1), abort, 264);
+                        if (kv == 1 && there && t == 0) {      // the raw rows of Q are out of the ring
+                            there = wait_phase(sm, odd, &sm->q_full[0], 0, abort, 276);
+                            if (there) there = wait_phase(sm, odd, &sm->q_full[1], 0, abort, 277);
                         }
+                        if (there && t >= kQSlots) there = wait_phase(sm, odd, &sm->empty[kv][slot], (uint32_t)((t / kQSlots - 1) & 1), abort, 263);
                         there = __all_sync(0xFFFFFFFFu, there);
-                        if (lane == 0) sm->go[kv][b] = there;
+                        if (lane == 0) sm->go[kv][t & 1] = there;
                     }
                     asm volatile("bar.sync %0, 128;" ::"r"(2 + kv) : "memory");
-                    if (!sm->go[kv][b]) break;
-                    unsigned char* const src = stage_smem + (kv * kQStages + slot) * kQStage + (16 * cw + r8) * kD;
+                    if (!sm->go[kv][t & 1]) break;
+                    unsigned char* const src = stage_smem + (kv * kQStages + t % kQStages) * kQStage + (16 * cw + r8) * kD;
                     float vm = 1.f;
                     if (kv == 1) {
                         const float4 sc = sm->chunk[t % kQConsts][cw];
@@ -1213,15 +1217,16 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                             }
                         }
                     }
-                    unsigned char* const dst = (kv == 0 ? k_smem : v_smem) + b * kQSlot + (16 * cw + r8) * 128;
+                    unsigned char* const dst = ring + kv * kQRing + slot * kQSlot + (16 * cw + r8) * 128;
+                    uint4 w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
-                        const uint4 w = *reinterpret_cast<const uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
-                        uint32_t h[8] = {widen2(w.x), widen2(w.x >> 16), widen2(w.y), widen2(w.y >> 16),
-                                         widen2(w.z), widen2(w.z >> 16), widen2(w.w), widen2(w.w >> 16)};
+                    for (int i = 0; i < 4; ++i)      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
+                        w[i] = *reinterpret_cast<const uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
                         unsigned char* const row = dst + (i & 1) * kQSlotHalf + 8 * (i >> 1) * 128;
-                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+                        *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(widen2(w[i].x), widen2(w[i].x >> 16), widen2(w[i].y), widen2(w[i].y >> 16));
+                        *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(widen2(w[i].z), widen2(w[i].z >> 16), widen2(w[i].w), widen2(w[i].w >> 16));
                     }
                     if (vm != 1.f) {       // what V's scale is beside a power of two (nothing, as daf_page_write leaves them): each lane its own pieces
                         const __half2 f = __float2half2_rn(vm);
@@ -1235,71 +1240,68 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(kv == 0 ? &sm->k_full[b] : &sm->v_full[b]);
-                        mbar_arrive(&sm->st_empty[kv][slot]);
+                        mbar_arrive(&sm->full[kv][slot]);
+                        mbar_arrive(&sm->st_empty[kv][t % kQStages]);
                     }
                 }
             } else if (warp < 10) {
                 // --------------------------------------------------------------------------------------------------- products
                 const int g = warp - 8;
-                const int n_u = pair ? n_t : (n_t - g + 1) / 2;          // steps of this group
+                const int n_u = pair ? n_t : (n_t - g + 1) >> 1;          // steps of this group
                 if (n_u > 0) {
                     constexpr uint32_t idesc_qk = make_idesc_f16(128, kQStep, 0), idesc_pv = make_idesc_f16(128, kD, 1);
-                    const uint32_t qa = smem_u32(q_smem + (pair ? g : 0) * kQTile);
-                    const uint32_t s_col = tmem + (uint32_t)(g * 256), o_col = s_col + 128u;
-                    // descriptors of the first 16 channels (or keys); the others, and the other slot's, differ in the address, in 16-byte units
-                    const uint64_t qd = make_smem_desc(qa, 16, 1024);
-                    const uint64_t kd = make_smem_desc(smem_u32(k_smem + (pair ? 0 : g) * kQSlot), 16, 1024);
-                    const uint64_t vd = make_smem_desc(smem_u32(v_smem + (pair ? 0 : g) * kQSlot), kQSlotHalf, 1024);
-                    const uint64_t next_slot = pair ? kQSlot / 16 : 0;
-                    auto slot_of = [&](int u) { return pair ? u & 1 : g; };
-                    auto use_of = [&](int u) { return pair ? u >> 1 : u; };       // how often the slot was filled before
-                    auto issue_qk = [&](int b) {
-                        const uint64_t k0 = kd + (b ? next_slot : 0);
+                    const uint32_t o_col = tmem + (uint32_t)(g * 256), s_col = o_col + kColS, q_col = tmem + (uint32_t)((pair ? g : 0) * 256) + kColQ;
+                    // descriptors of the first slot's first 16 channels (or keys); the others differ in the address, in 16-byte units
+                    const uint64_t kd = make_smem_desc(smem_u32(ring), 16, 1024), vd = make_smem_desc(smem_u32(ring + kQRing), kQSlotHalf, 1024);
+                    // Frees a slot: one arrival of each group's products, or two of the one group that a step of a block of one tile has.
+                    auto free_slot = [&](uint64_t* bar) {
+                        tc_commit(bar);
+                        if (!pair) tc_commit(bar);
+                    };
+                    auto issue_qk = [&](int slot) {
+                        const uint64_t k0 = kd + (uint64_t)(slot * (kQSlot / 16));
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)
-                            tc_mma_ss(s_col + (uint32_t)(b * kQStep), qd + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQHalf / 16)),
-                                      k0 + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQSlotHalf / 16)), idesc_qk, kk > 0 ? 1u : 0u);
-                        tc_commit(&sm->s_full[g][b]);
+                            tc_mma_ts(s_col, q_col + (uint32_t)(kk * 8), k0 + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQSlotHalf / 16)), idesc_qk, kk > 0 ? 1u : 0u);
+                        tc_commit(&sm->s_full[g]);
+                        free_slot(&sm->empty[0][slot]);
                     };
                     ok = wait_phase(sm, odd, &sm->q_full[pair ? g : 0], 0, abort, 266);
+                    if (ok) ok = wait_phase(sm, odd, &sm->full[0][pair ? 0 : g], 0, abort, 267);
                     ok = __all_sync(0xFFFFFFFFu, ok);
-                    for (int u = 0; u < 2 && u < n_u && ok; ++u) {
-                        ok = wait_phase(sm, odd, &sm->k_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 267);
-                        ok = __all_sync(0xFFFFFFFFu, ok);
-                        if (!ok) break;
+                    if (ok) {
                         tc_fence_after();
-                        if (elect_one()) issue_qk(u);
+                        if (elect_one()) issue_qk(pair ? 0 : g);
                         __syncwarp();
                     }
                     for (int u = 0; u < n_u && ok; ++u) {
-                        const int b = u & 1;
-                        bool there = wait_phase(sm, odd, &sm->v_full[slot_of(u)], (uint32_t)(use_of(u) & 1), abort, 268);
-                        if (there) there = wait_phase(sm, odd, &sm->p_full[g][b], (uint32_t)((u >> 1) & 1), abort, 269);
+                        const int t = pair ? u : 2 * u + g, next = pair ? t + 1 : t + 2;
+                        bool there = wait_phase(sm, odd, &sm->full[1][t % kQSlots], (uint32_t)((t / kQSlots) & 1), abort, 268);
+                        if (there) there = wait_phase(sm, odd, &sm->p_full[g], (uint32_t)(u & 1), abort, 269);
                         ok = __all_sync(0xFFFFFFFFu, there);
                         if (!ok) break;
                         tc_fence_after();
                         if (elect_one()) {
-                            const uint64_t v0 = vd + (b ? next_slot : 0);
+                            const uint64_t v0 = vd + (uint64_t)((t % kQSlots) * (kQSlot / 16));
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk)
-                                tc_mma_ts(o_col, s_col + (uint32_t)(b * kQStep + kk * 8), v0 + (uint64_t)(kk * 128), idesc_pv,
-                                          (u == 0 && kk == 0) ? 0u : 1u);
-                            tc_commit(&sm->pv_done[g][b]);
+                                tc_mma_ts(o_col, s_col + (uint32_t)(kk * 8), v0 + (uint64_t)(kk * 128), idesc_pv, (u == 0 && kk == 0) ? 0u : 1u);
+                            free_slot(&sm->empty[1][t % kQSlots]);
+                            if (u + 1 == n_u) tc_commit(&sm->o_full[g]);
                         }
                         __syncwarp();
-                        if (u + 2 < n_u) {
-                            ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->k_full[slot_of(u + 2)], (uint32_t)(use_of(u + 2) & 1), abort, 270));
+                        if (u + 1 < n_u) {
+                            ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->full[0][next % kQSlots], (uint32_t)((next / kQSlots) & 1), abort, 270));
                             if (!ok) break;
                             tc_fence_after();
-                            if (elect_one()) issue_qk(b);
+                            if (elect_one()) issue_qk(next % kQSlots);
                             __syncwarp();
                         }
                     }
                 }
             }
             tc_fence_before();
-            __syncthreads();       // the barriers, rings and tensor memory are free
+            __syncthreads();       // the rings and tensor memory are free
             tc_fence_after();
             if (sm->abort_flag != 0) break;
         }
