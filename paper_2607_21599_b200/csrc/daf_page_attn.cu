@@ -636,43 +636,47 @@ page_decode_kernel(const PageAttnArgs a) {
 
 // ---------------------------------------------------------------------------------------------- many rows: tensor memory
 // More than 24 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
-// of 128 consecutive rows, in steps of 64 keys.  One CTA per SM, 20 warps:
-//   10, 11  ask for the bytes of K and V (TMA, kQStages steps ahead);
-//   12-15, 16-19  widen K's, and V's, to fp16, exactly, into four-slot rings that the products read (128-byte swizzle).  Each of
-//          these is a chain of waits, reads, conversions and writes, so K and V have warps of their own;
-//   8, 9   issue a tile group's products: S = Q K^T with Q from tensor memory, O += P V with P from tensor memory, over S;
+// of 128 consecutive rows, in steps of 128 keys.  One CTA per SM, 20 warps:
+//   10, 11  ask for the bytes of K and V (TMA, kQStages half steps ahead);
+//   12-15, 16-19  widen K's, and V's, to fp16, exactly, into the buffers that the products read (128-byte swizzle), half a step at a
+//          time.  Each of these is a chain of waits, reads, conversions and writes, so K and V have warps of their own;
+//   8, 9   issue a tile group's products: S = Q K^T, O += P V with P from tensor memory, over S, by halves as they come;
 //   0-3, 4-7  a tile group's softmax, a row per thread, and its epilogue.
 // A block of two tiles shares every widened K and V.  A block of one tile gives its even steps to one group and its odd ones to the
-// other, and the two halves of the result are merged in shared memory.  A group's 256 columns of tensor memory: O 128, Q (fp16) 64,
-// S 64.  One S is enough because the groups take turns: while one's products run, the other's softmax does; and with Q there instead
-// of in shared memory a step of two tiles passes 128 KB through shared memory (64 of operand reads, 32 written and 32 of bytes in and
-// out) instead of 192, which had bound the loop.
+// other, and the two halves of the result are merged in shared memory.  A group's 256 columns of tensor memory are O and S, 128
+// each.  One S is enough because the groups take turns: while one's products run, the other's softmax does.  (Steps of 64 keys with
+// two S a group: 114 us for 128 tokens of 28 / 4 heads over 32k keys, the products of both groups and the widening bound by shared
+// memory; with Q in tensor memory and one S: 110, the products' latency as long as a softmax step.)
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
-constexpr int kQStep = 64;
-constexpr int kQStages = 4;
-constexpr int kQSlots = 4;
-constexpr int kQConsts = 16;       // steps whose constants are kept: they are written up to kQStages + kQSlots + 2 steps ahead of their last reader
+constexpr int kQStep = 128, kQSub = 64;
+constexpr int kQStages = 2;        // half steps
+constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
 constexpr int kQThreads = 640;
-constexpr int kQSlot = kQStep * kD * 2;               // 16 KB: K or V of a step, widened, two 64-column halves
+constexpr int kQTile = 128 * kD * 2;                  // 32 KB: 128 rows of Q or K as fp16, two 64-column halves
+constexpr int kQHalf = kQTile / 2;
+constexpr int kQSlot = kQSub * kD * 2;                // 16 KB: V of half a step, widened, two 64-column halves
 constexpr int kQSlotHalf = kQSlot / 2;
-constexpr int kQStage = kQStep * kD;                  // 8 KB: the bytes of K or V of a step
-constexpr int kQRing = kQSlots * kQSlot;              // 64 KB; V's holds the raw rows of Q (two tiles of 32 KB) when a piece begins
-constexpr uint32_t kColQ = 128, kColS = 192;          // columns of a group, behind O
+constexpr int kQStage = kQSub * kD;                   // 8 KB: the bytes of K or V of half a step
+constexpr uint32_t kColS = 128;                       // columns of a group, behind O
 constexpr float kLazy = 6.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
+// Shared memory: Q's two tiles; V's two slots; K's two buffers.  A block of one tile has four slots of V, the last two in the second
+// tile of Q.  When a piece begins K's buffers hold the raw rows of Q, at its end they and Q's tiles what leaves the CTA.
+constexpr int kQOffV = 2 * kQTile, kQOffK = kQOffV + 2 * kQSlot, kQOffStage = kQOffK + 2 * kQTile;
 
 struct QuestionSmem {
-    uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V] a step's bytes
-    uint64_t full[2][kQSlots], empty[2][kQSlots];             // [K, V] its widened rows
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];      // [group]
+    uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V] the bytes of half a step
+    uint64_t k_full[2], k_empty[2];                           // [buffer] a step's K, widened
+    uint64_t v_full[4], v_empty[4];                           // [slot] half a step's V, widened
+    uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2];   // [group], [half]
     uint64_t c_full[kQConsts];
-    float4 chunk[kQConsts][4];      // of a step's chunks of 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
-    int missing[kQConsts];          // some keys of the step have no page
+    float4 chunk[kQConsts][4];      // of half a step's chunks of 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
+    int missing[kQConsts];          // some keys of the half step have no page
     float2 ml[128];                 // the second group's row maxima and sums (blocks of one tile)
     uint32_t tmem_base;
     int abort_flag;
     unsigned long long odd;         // which barriers have completed an odd number of phases
-    int go[2][2];                   // [K, V][step mod 2] what the polling warp found
+    int go[2][2];                   // [K, V][half step mod 2] what the polling warp found
     int poison;                     // a NaN was taken out of a value that some rows must not see
     // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
     Place at;
@@ -681,12 +685,13 @@ struct QuestionSmem {
     Shares shares;
     ChainEntry chain;
 };
-constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarFull = (int)(offsetof(QuestionSmem, full) / 8),
-              kBarEmpty = (int)(offsetof(QuestionSmem, empty) / 8), kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
+constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK = (int)(offsetof(QuestionSmem, k_full) / 8),
+              kBarKEmpty = (int)(offsetof(QuestionSmem, k_empty) / 8), kBarV = (int)(offsetof(QuestionSmem, v_full) / 8),
+              kBarVEmpty = (int)(offsetof(QuestionSmem, v_empty) / 8), kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
               kBarS = (int)(offsetof(QuestionSmem, s_full) / 8), kBarP = (int)(offsetof(QuestionSmem, p_full) / 8),
               kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
-static_assert(offsetof(QuestionSmem, st_full) == 0 && kQStages == 4 && kQSlots == 4 && (kBarS & 1) == 0 && kBars <= 64, "what the barriers' numbers rest on");
-constexpr size_t kQuestionSmem = 1024 + 2 * (size_t)kQRing + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
+static_assert(offsetof(QuestionSmem, st_full) == 0 && kQStages == 2 && kBars <= 64, "what the barriers' numbers rest on");
+constexpr size_t kQuestionSmem = 1024 + kQOffStage + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
 __host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
     return (1u << 4) | (b_mn_major << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);      // fp16 x fp16 -> fp32
@@ -702,17 +707,21 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "memory");
 }
 
-// One softmax step of one row over 64 keys: P over the first half of the logits' columns, running maximum and sum; returns the factor
-// for the row of O (1 unless the maximum grew by more than kLazy).  c: the row's factor for its logits.
-__device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4* chunk, bool missing, int key0, int limit, float c, float& m, float& l) {
+// One softmax step of one row over 128 keys: P over the first half of the logits' columns, running maximum and sum.  `rescale` is called
+// ahead of the first P with the factor for the row of O (1 unless the maximum grew by more than kLazy), `half_done` when half of P is
+// on its way to tensor memory.  c: the row's factor for its logits; chunk: two half steps' constants.  The logits are fetched twice,
+// for the maximum and for the exponentials: a thread has no room for 128 of them.
+template <typename Rescale, typename HalfDone>
+__device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* const (&chunk)[2], bool missing, int key0, int limit, float c,
+                                                 float& m, float& l, Rescale rescale, HalfDone half_done) {
     if (__any_sync(0xFFFFFFFFu, key0 + kQStep - 1 > limit || missing)) {
         // rare (the last steps of a sequence): logits of keys that the row does not see become -inf where they are
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             uint32_t r[16];
             tmem_ld16(s_addr + (uint32_t)(16 * i), r);
             tc_wait_ld();
-            const int last = chunk[i].x < 0.f ? -1 : limit - key0 - 16 * i;
+            const int last = chunk[i >> 2][i & 3].x < 0.f ? -1 : limit - key0 - 16 * i;
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (j > last) r[j] = 0xFF800000u;
@@ -720,22 +729,21 @@ __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4*
         }
         tc_wait_st();
     }
+    float top = -INFINITY;
     uint32_t sr[2][32];
     tmem_ld32(s_addr, sr[0]);
-    tc_wait_ld();
-    tmem_ld32(s_addr + 32u, sr[1]);
-    float top = -INFINITY;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        if (half == 1) tc_wait_ld();
+    for (int q = 0; q < 4; ++q) {
+        tc_wait_ld();
+        tmem_ld32(s_addr + (uint32_t)(32 * ((q + 1) & 3)), sr[(q + 1) & 1]);      // (after the last quarter the first again, for its exponentials)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float2 k2 = *reinterpret_cast<const float2*>(chunk + 2 * half + i);
+            const float2 k2 = *reinterpret_cast<const float2*>(chunk[q >> 1] + 2 * (q & 1) + i);
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
-                mx[0] = fmax3(mx[0], __uint_as_float(sr[half][16 * i + j]), __uint_as_float(sr[half][16 * i + j + 1]));
-                mx[1] = fmax3(mx[1], __uint_as_float(sr[half][16 * i + j + 2]), __uint_as_float(sr[half][16 * i + j + 3]));
+                mx[0] = fmax3(mx[0], __uint_as_float(sr[q & 1][16 * i + j]), __uint_as_float(sr[q & 1][16 * i + j + 1]));
+                mx[1] = fmax3(mx[1], __uint_as_float(sr[q & 1][16 * i + j + 2]), __uint_as_float(sr[q & 1][16 * i + j + 3]));
             }
             top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), c * fabsf(k2.x), k2.y));
         }
@@ -744,19 +752,22 @@ __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4*
     if (m != -INFINITY && now - m <= kLazy) now = m;
     const float used = now == -INFINITY ? 0.f : now - kPExp;
     const float alpha = m == -INFINITY ? 1.f : fast_exp2(m - now);
+    rescale(alpha);
     float sum = 0.f;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (int q = 0; q < 4; ++q) {
+        tc_wait_ld();
+        if (q < 3) tmem_ld32(s_addr + (uint32_t)(32 * (q + 1)), sr[(q + 1) & 1]);
         uint32_t pr[16];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float4 k4 = chunk[2 * half + i];
+            const float4 k4 = chunk[q >> 1][2 * (q & 1) + i];
             const float f = c * fabsf(k4.x), d = k4.y - used;
             const uint64_t f2 = pack_f32x2(f, f), d2 = pack_f32x2(d, d);
             uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
-                const uint64_t x = ffma2(pack_f32x2(__uint_as_float(sr[half][16 * i + j]), __uint_as_float(sr[half][16 * i + j + 1])), f2, d2);
+                const uint64_t x = ffma2(pack_f32x2(__uint_as_float(sr[q & 1][16 * i + j]), __uint_as_float(sr[q & 1][16 * i + j + 1])), f2, d2);
                 const float p0 = fast_exp2(f32x2_lo(x)), p1 = fast_exp2(f32x2_hi(x));
                 acc[(j >> 1) & 1] = fadd2(acc[(j >> 1) & 1], pack_f32x2(p0, p1));
                 pr[8 * i + (j >> 1)] = pack_f16(p0, p1);
@@ -764,21 +775,28 @@ __device__ __forceinline__ float question_softmax(uint32_t s_addr, const float4*
             const uint64_t both = fadd2(acc[0], acc[1]);
             sum = fmaf(f32x2_lo(both) + f32x2_hi(both), k4.z, sum);
         }
-        tmem_st16(s_addr + (uint32_t)(16 * half), pr);
+        // a quarter of P takes 16 columns, over logits that have been fetched (the next quarter's are on their way: columns further up)
+        tmem_st16(s_addr + (uint32_t)(16 * q), pr);
+        if (q & 1) half_done(q >> 1);
     }
     l = l * alpha + sum;
     m = now;
-    return alpha;
 }
 
 // How many phases barrier i completes in a piece of n_t steps.
 __device__ __forceinline__ int bar_uses(int i, int n_t, bool pair) {
-    if (i < kBarQ) return (n_t - (i & 3) + 3) >> 2;                      // every fourth step
-    if (i < kBarC) {
-        const int g = i & 1, steps = pair ? n_t : (n_t - g + 1) >> 1;    // of the group
-        return i < kBarS ? 1 : i < kBarO ? steps : (steps > 0 ? 1 : 0);
+    if (i < kBarK) return n_t;                                           // every other half step
+    if (i < kBarV) return (n_t - (i & 1) + 1) >> 1;
+    if (i < kBarQ) {
+        const int slot = (i - kBarV) & 3;
+        return pair ? (slot < 2 ? n_t : 0) : (n_t - (slot >> 1) + 1) >> 1;
     }
-    return i < kBars ? (n_t - (i - kBarC) + kQConsts - 1) / kQConsts : 0;
+    if (i < kBarS) return 1;
+    if (i < kBarC) {
+        const int g = i < kBarP || i >= kBarO ? i & 1 : ((i - kBarP) >> 1), steps = pair ? n_t : (n_t - g + 1) >> 1;    // of the group
+        return i < kBarO ? steps : (steps > 0 ? 1 : 0);
+    }
+    return i < kBars ? (2 * n_t - (i - kBarC) + kQConsts - 1) / kQConsts : 0;
 }
 
 // The bounded wait of this kernel, `parity` as if the piece of work were the CTA's first (a second at most, or until another thread has
@@ -801,12 +819,15 @@ __device__ __forceinline__ bool wait_phase(QuestionSmem* sm, unsigned long long 
     }
 }
 
+// Where slot i of V lies: two of their own, two in the second tile of Q (blocks of one tile).
+__host__ __device__ constexpr int v_slot(int i) { return i < 2 ? kQOffV + i * kQSlot : kQTile + (i - 2) * kQSlot; }
+
 __global__ void __launch_bounds__(kQThreads, 1)
 page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PageAttnArgs a) {
     extern __shared__ unsigned char question_smem_raw[];
     unsigned char* const smem = question_smem_raw + ((1024u - (smem_u32(question_smem_raw) & 1023u)) & 1023u);      // (stays a shared address to the compiler)
-    unsigned char* const ring = smem;                            // K's four slots, then V's
-    unsigned char* const stage_smem = ring + 2 * kQRing;
+    unsigned char* const k_smem = smem + kQOffK;
+    unsigned char* const stage_smem = smem + kQOffStage;
     QuestionSmem* const sm = reinterpret_cast<QuestionSmem*>(stage_smem + 2 * kQStages * kQStage);
     int* const pre = reinterpret_cast<int*>(sm + 1);
     __shared__ int warp_sums[kQThreads / 32];
@@ -827,8 +848,9 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         uint64_t* const bars = reinterpret_cast<uint64_t*>(sm);
         for (int i = lane; i < kBars; i += 32) {
             // four warps (or lanes) arrive, or both groups' products, or one copy's bytes or product
-            const bool by_four = (i >= kBarStEmpty && i < kBarEmpty) || (i >= kBarQ && i < kBarS) || (i >= kBarP && i < kBarO) || i >= kBarC;
-            mbar_init(bars + i, by_four ? 4 : i >= kBarEmpty && i < kBarQ ? 2 : 1);
+            const bool by_four = (i >= kBarStEmpty && i < kBarK) || (i >= kBarV && i < kBarVEmpty) || (i >= kBarQ && i < kBarS) || (i >= kBarP && i < kBarO) || i >= kBarC;
+            const bool by_two = (i >= kBarKEmpty && i < kBarV) || (i >= kBarVEmpty && i < kBarQ);
+            mbar_init(bars + i, i >= kBarK && i < kBarKEmpty ? 8 : by_four ? 4 : by_two ? 2 : 1);      // (K: four warps, two half steps)
         }
         mbar_fence_init();
     }
@@ -842,7 +864,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     const int T = a.p.T, Hkv = a.p.Hkv;
     if (warp == 0) {
         const long long total = (long long)pre[a.n] * Hkv * a.units;
-        const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than four steps of a tile each
+        const long long ctas = min((long long)gridDim.x, (total + 1) / 2);       // no fewer than two steps of a tile each
         const Shares shares = share(total, ctas);
         // lane 0 finds the stretch's begin, lane 1 its end; both move up to the next step's begin
         const long long from = cta_begin(shares, min((long long)blockIdx.x + min(lane, 1), ctas));
@@ -913,11 +935,11 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             const uint32_t o_addr = tmem + (uint32_t)(g * 256) + lane_addr, s_addr = o_addr + kColS;
             float c;
             {
-                // The warp's 32 rows of Q: raw into the ring that V's widened rows will use, sixteen lanes a row, pieces of 16 bytes XOR-ed with
-                // the row number.  Each thread then scales its own row to a largest magnitude of 2^14 .. 2^15 and puts it into tensor
-                // memory as fp16.  (Both groups of a block of one tile load the same rows; only the first puts them there.)
+                // The warp's 32 rows of Q: raw into what will be K's buffers, sixteen lanes a row, pieces of 16 bytes XOR-ed with the row
+                // number.  Each thread then scales its own row to a largest magnitude of 2^14 .. 2^15 and writes it as fp16 in the layout of
+                // a tiled copy.  (Both groups of a block of one tile load the same rows; only the first writes them.)
                 const int sub = lane >> 4, piece = lane & 15, r0 = (warp & 3) * 32 + sub, d_tok = 2 / a.G, d_head = 2 % a.G;
-                unsigned char* const raw = ring + kQRing + g * (128 * 256);
+                unsigned char* const raw = k_smem + g * (128 * 256);
                 int tk = (tile_row + r0) / a.G, hd = tile_row + r0 - tk * a.G;
                 const __nv_bfloat16* src = a.q + (((size_t)sm->at.b * a.L_q + tk) * a.Hq + sm->at.h * a.G + hd) * kD + piece * 8;
 #pragma unroll 2
@@ -946,36 +968,35 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const float up = __int_as_float((14 - e + 127) << 23);
                 c = __int_as_float((e - 14 + 127) << 23) * a.scale_log2;
                 if (pair || g == 0) {
-#pragma unroll 1
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t y[16];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint4 w = mine[(4 * i + j) ^ (rt & 15)];
-                            y[4 * j] = pack_f16(__uint_as_float(w.x << 16) * up, __uint_as_float(w.x & 0xFFFF0000u) * up);
-                            y[4 * j + 1] = pack_f16(__uint_as_float(w.y << 16) * up, __uint_as_float(w.y & 0xFFFF0000u) * up);
-                            y[4 * j + 2] = pack_f16(__uint_as_float(w.z << 16) * up, __uint_as_float(w.z & 0xFFFF0000u) * up);
-                            y[4 * j + 3] = pack_f16(__uint_as_float(w.w << 16) * up, __uint_as_float(w.w & 0xFFFF0000u) * up);
-                        }
-                        tmem_st16(o_addr + kColQ + (uint32_t)(16 * i), y);
+                    unsigned char* const dst = smem + g * kQTile + rt * 128;
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {
+                        const uint4 w = mine[i ^ (rt & 15)];
+                        uint4 y;
+                        y.x = pack_f16(__uint_as_float(w.x << 16) * up, __uint_as_float(w.x & 0xFFFF0000u) * up);
+                        y.y = pack_f16(__uint_as_float(w.y << 16) * up, __uint_as_float(w.y & 0xFFFF0000u) * up);
+                        y.z = pack_f16(__uint_as_float(w.z << 16) * up, __uint_as_float(w.z & 0xFFFF0000u) * up);
+                        y.w = pack_f16(__uint_as_float(w.w << 16) * up, __uint_as_float(w.w & 0xFFFF0000u) * up);
+                        *reinterpret_cast<uint4*>(dst + (i >> 3) * kQHalf + (((i & 7) ^ (rt & 7)) << 4)) = y;
                     }
-                    tc_wait_st();
-                    tc_fence_before();
+                    fence_proxy_async();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm->q_full[g]);
             }
             float m = -INFINITY, l = 0.f;
             for (int u = 0; u < n_u; ++u) {
-                const int t = pair ? u : 2 * u + g;
-                ok = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 271);
+                const int t = pair ? u : 2 * u + g, c0 = (2 * t) % kQConsts;
+                ok = wait_phase(sm, odd, &sm->c_full[c0], (uint32_t)((2 * t / kQConsts) & 1), abort, 271);
+                if (ok) ok = wait_phase(sm, odd, &sm->c_full[c0 + 1], (uint32_t)((2 * t / kQConsts) & 1), abort, 273);
                 if (ok) ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const float alpha = question_softmax(s_addr, sm->chunk[t % kQConsts], sm->missing[t % kQConsts] != 0, (step0 + t) * kQStep, limit, c, m, l);
-                if (u > 0 && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
+                const float4* const chunk[2] = {sm->chunk[c0], sm->chunk[c0 + 1]};
+                auto rescale = [&](float alpha) {
                     // (the logits came behind the product before, so O is quiet)
+                    if (u == 0 || !__any_sync(0xFFFFFFFFu, alpha != 1.f)) return;
 #pragma unroll 1
                     for (int i = 0; i < 8; ++i) {
                         uint32_t r[16];
@@ -985,19 +1006,22 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
                         tmem_st16(o_addr + (uint32_t)(16 * i), r);
                     }
-                }
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm->p_full[g]);
+                };
+                auto half_done = [&](int half) {
+                    tc_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm->p_full[g][half]);
+                };
+                question_softmax(s_addr, chunk, (sm->missing[c0] | sm->missing[c0 + 1]) != 0, (step0 + t) * kQStep, limit, c, m, l, rescale, half_done);
             }
             if (ok && n_u > 0) ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->o_full[g], 0, abort, 274));
             tc_fence_after();
-            // ---- epilogue, through the rings once both groups are done with them.  A block of one tile: the second group hands its rows to
+            // ---- epilogue, through Q's tiles and K's buffers once both groups are done with them.  A block of one tile: the second group hands its rows to
             // the first.
             float w0 = 1.f, w1 = 0.f;
-            float* const other = reinterpret_cast<float*>(ring + kQRing) + rt * kD;
-            static_assert(kQRing >= 128 * kD * (int)sizeof(float) && kQRing >= 8 * 8192, "a tile of fp32 rows, and 8 KB a warp");
+            float* const other = reinterpret_cast<float*>(smem) + rt * kD;
+            static_assert(2 * kQTile >= 128 * kD * (int)sizeof(float) && 2 * kQTile >= 8 * 8192, "a tile of fp32 rows, and 8 KB a warp");
             asm volatile("bar.sync 1, 256;" ::: "memory");
             if (!pair) {
                 if (g == 1 && ok) {
@@ -1032,7 +1056,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const float inv = row_inverse(l);
                 // 256 bytes of each of the warp's 32 rows at a time (a whole bf16 row, or half of an fp32 one), 16-byte pieces XOR-ed with the
                 // row number, and out again with sixteen lanes a row.
-                unsigned char* const stage = ring + warp * 8192;
+                unsigned char* const stage = k_smem + warp * 8192;
                 const size_t out_row = ((size_t)at.b * a.L_q + tok) * a.Hq + at.h * a.G + head;
                 const size_t set_row = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
                 const unsigned long long dst = reinterpret_cast<unsigned long long>(whole ? reinterpret_cast<char*>(a.out) + out_row * (kD * 2)
@@ -1118,17 +1142,17 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const int kv = warp - 10, seq = sm->at.seq, h = sm->at.h, len = sm->at.len;
                 const bool reports = kv == 0 && h == 0 && sm->at.block == 0;
                 float ks = -1.f, vs = -1.f;         // (K's warp) the scales of the pages in ids
-                const int page_bits = 31 - __clz(T), box = min(T, kQStep), pages = kQStep / box;      // copies of a step
-                const int chunk_page = box < kQStep ? ((lane & 3) * 16) >> page_bits : 0;             // page of a chunk of 16 keys
+                const int page_bits = 31 - __clz(T), box = min(T, kQSub), pages = kQSub / box;        // copies of half a step
+                const int chunk_page = box < kQSub ? ((lane & 3) * 16) >> page_bits : 0;             // page of a chunk of 16 keys
                 int ids = -1, ids_end = 0;          // page numbers of 32 pages that end in front of ids_end, one a lane
-                for (int t = 0; t < n_t && ok; ++t) {
+                for (int t = 0; t < 2 * n_t && ok; ++t) {      // (t counts half steps here)
                     const int slot = t % kQStages;
                     if (t >= kQStages) {
                         ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, 260));
                         if (!ok) break;
                     }
                     uint64_t* const full = &sm->st_full[kv][slot];
-                    const int key0 = (step0 + t) * kQStep, page0 = key0 >> page_bits;
+                    const int key0 = step0 * kQStep + t * kQSub, page0 = key0 >> page_bits;
                     if (page0 + pages > ids_end) {
                         ids_end = page0 + 32;
                         const int j = page0 + lane;
@@ -1177,17 +1201,18 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const int first_limit = sm->first_limit, len = sm->at.len;
                 const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
                 const int kv = warp >= 16;
-                for (int t = 0; t < n_t; ++t) {
-                    const int slot = t % kQSlots;
+                for (int t = 0; t < 2 * n_t; ++t) {      // (t counts half steps here)
+                    // K: half of the buffer of its step; V: a slot
+                    const int step = t >> 1, slot = kv == 0 ? step & 1 : pair ? t & 1 : t & 3, uses = kv == 0 || !pair ? step >> 1 : step;
                     // one of the four warps polls, the others sleep at a barrier (twelve polling warps took half of the issue slots)
                     if (cw == 0) {
                         bool there = wait_phase(sm, odd, &sm->st_full[kv][t % kQStages], (uint32_t)((t / kQStages) & 1), abort, 262);
                         if (kv == 1 && there) there = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 275);
-                        if (kv == 1 && there && t == 0) {      // the raw rows of Q are out of the ring
+                        if (there && t == 0 && (kv == 0 || !pair)) {      // the raw rows of Q are out of K's buffers, the second tile is idle
                             there = wait_phase(sm, odd, &sm->q_full[0], 0, abort, 276);
                             if (there) there = wait_phase(sm, odd, &sm->q_full[1], 0, abort, 277);
                         }
-                        if (there && t >= kQSlots) there = wait_phase(sm, odd, &sm->empty[kv][slot], (uint32_t)((t / kQSlots - 1) & 1), abort, 263);
+                        if (there && uses > 0) there = wait_phase(sm, odd, kv == 0 ? &sm->k_empty[slot] : &sm->v_empty[slot], (uint32_t)((uses - 1) & 1), abort, 263);
                         there = __all_sync(0xFFFFFFFFu, there);
                         if (lane == 0) sm->go[kv][t & 1] = there;
                     }
@@ -1197,9 +1222,9 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     float vm = 1.f;
                     if (kv == 1) {
                         const float4 sc = sm->chunk[t % kQConsts][cw];
-                        const int key0 = (step0 + t) * kQStep;
+                        const int key0 = step0 * kQStep + t * kQSub;
                         vm = sc.w;
-                        if (key0 + kQStep - 1 > first_limit || sc.x < 0.f) {
+                        if (key0 + kQSub - 1 > first_limit || sc.x < 0.f) {
                             // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in
                             // a key that only some rows see is taken out, and put into the rows that see it at the end.
 #pragma unroll 1
@@ -1217,14 +1242,15 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                             }
                         }
                     }
-                    unsigned char* const dst = ring + kv * kQRing + slot * kQSlot + (16 * cw + r8) * 128;
+                    const int half_at = kv == 0 ? kQHalf : kQSlotHalf;          // between the two 64-column halves
+                    unsigned char* const dst = smem + (kv == 0 ? kQOffK + slot * kQTile + (t & 1) * (kQSub * 128) : v_slot(slot)) + (16 * cw + r8) * 128;
                     uint4 w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
                         w[i] = *reinterpret_cast<const uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        unsigned char* const row = dst + (i & 1) * kQSlotHalf + 8 * (i >> 1) * 128;
+                        unsigned char* const row = dst + (i & 1) * half_at + 8 * (i >> 1) * 128;
                         *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(widen2(w[i].x), widen2(w[i].x >> 16), widen2(w[i].y), widen2(w[i].y >> 16));
                         *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(widen2(w[i].z), widen2(w[i].z >> 16), widen2(w[i].w), widen2(w[i].w >> 16));
                     }
@@ -1240,7 +1266,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(&sm->full[kv][slot]);
+                        mbar_arrive(kv == 0 ? &sm->k_full[slot] : &sm->v_full[slot]);
                         mbar_arrive(&sm->st_empty[kv][t % kQStages]);
                     }
                 }
@@ -1250,24 +1276,27 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const int n_u = pair ? n_t : (n_t - g + 1) >> 1;          // steps of this group
                 if (n_u > 0) {
                     constexpr uint32_t idesc_qk = make_idesc_f16(128, kQStep, 0), idesc_pv = make_idesc_f16(128, kD, 1);
-                    const uint32_t o_col = tmem + (uint32_t)(g * 256), s_col = o_col + kColS, q_col = tmem + (uint32_t)((pair ? g : 0) * 256) + kColQ;
-                    // descriptors of the first slot's first 16 channels (or keys); the others differ in the address, in 16-byte units
-                    const uint64_t kd = make_smem_desc(smem_u32(ring), 16, 1024), vd = make_smem_desc(smem_u32(ring + kQRing), kQSlotHalf, 1024);
-                    // Frees a slot: one arrival of each group's products, or two of the one group that a step of a block of one tile has.
-                    auto free_slot = [&](uint64_t* bar) {
+                    const uint32_t o_col = tmem + (uint32_t)(g * 256), s_col = o_col + kColS;
+                    // descriptors of the first 16 channels (or keys) of the first buffer (slot); the others differ in the address, in 16-byte units
+                    const uint64_t qd = make_smem_desc(smem_u32(smem + (pair ? g : 0) * kQTile), 16, 1024), kd = make_smem_desc(smem_u32(k_smem), 16, 1024);
+                    const uint64_t vd = make_smem_desc(smem_u32(smem), kQSlotHalf, 1024);
+                    // Frees a buffer or slot: one arrival of each group's products, or two of the one group that a step of a block of one
+                    // tile has.
+                    auto release = [&](uint64_t* bar) {
                         tc_commit(bar);
                         if (!pair) tc_commit(bar);
                     };
-                    auto issue_qk = [&](int slot) {
-                        const uint64_t k0 = kd + (uint64_t)(slot * (kQSlot / 16));
+                    auto issue_qk = [&](int buf) {
+                        const uint64_t k0 = kd + (uint64_t)(buf * (kQTile / 16));
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)
-                            tc_mma_ts(s_col, q_col + (uint32_t)(kk * 8), k0 + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQSlotHalf / 16)), idesc_qk, kk > 0 ? 1u : 0u);
+                            tc_mma_ss(s_col, qd + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQHalf / 16)), k0 + (uint64_t)((kk & 3) * 2 + (kk >> 2) * (kQHalf / 16)), idesc_qk,
+                                      kk > 0 ? 1u : 0u);
                         tc_commit(&sm->s_full[g]);
-                        free_slot(&sm->empty[0][slot]);
+                        release(&sm->k_empty[buf]);
                     };
                     ok = wait_phase(sm, odd, &sm->q_full[pair ? g : 0], 0, abort, 266);
-                    if (ok) ok = wait_phase(sm, odd, &sm->full[0][pair ? 0 : g], 0, abort, 267);
+                    if (ok) ok = wait_phase(sm, odd, &sm->k_full[pair ? 0 : g], 0, abort, 267);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     if (ok) {
                         tc_fence_after();
@@ -1275,26 +1304,31 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         __syncwarp();
                     }
                     for (int u = 0; u < n_u && ok; ++u) {
-                        const int t = pair ? u : 2 * u + g, next = pair ? t + 1 : t + 2;
-                        bool there = wait_phase(sm, odd, &sm->full[1][t % kQSlots], (uint32_t)((t / kQSlots) & 1), abort, 268);
-                        if (there) there = wait_phase(sm, odd, &sm->p_full[g], (uint32_t)(u & 1), abort, 269);
-                        ok = __all_sync(0xFFFFFFFFu, there);
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint64_t v0 = vd + (uint64_t)((t % kQSlots) * (kQSlot / 16));
-#pragma unroll
-                            for (int kk = 0; kk < 4; ++kk)
-                                tc_mma_ts(o_col, s_col + (uint32_t)(kk * 8), v0 + (uint64_t)(kk * 128), idesc_pv, (u == 0 && kk == 0) ? 0u : 1u);
-                            free_slot(&sm->empty[1][t % kQSlots]);
-                            if (u + 1 == n_u) tc_commit(&sm->o_full[g]);
-                        }
-                        __syncwarp();
-                        if (u + 1 < n_u) {
-                            ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->full[0][next % kQSlots], (uint32_t)((next / kQSlots) & 1), abort, 270));
+                        const int t = pair ? u : 2 * u + g;
+#pragma unroll 1
+                        for (int half = 0; half < 2 && ok; ++half) {
+                            const int slot = pair ? half : 2 * g + half;
+                            bool there = wait_phase(sm, odd, &sm->v_full[slot], (uint32_t)(u & 1), abort, 268);
+                            if (there) there = wait_phase(sm, odd, &sm->p_full[g][half], (uint32_t)(u & 1), abort, 269);
+                            ok = __all_sync(0xFFFFFFFFu, there);
                             if (!ok) break;
                             tc_fence_after();
-                            if (elect_one()) issue_qk(next % kQSlots);
+                            if (elect_one()) {
+                                const uint64_t v0 = vd + (uint64_t)(v_slot(slot) / 16);
+#pragma unroll
+                                for (int kk = 0; kk < 4; ++kk)
+                                    tc_mma_ts(o_col, s_col + (uint32_t)(half * 32 + kk * 8), v0 + (uint64_t)(kk * 128), idesc_pv, (u == 0 && half == 0 && kk == 0) ? 0u : 1u);
+                                release(&sm->v_empty[slot]);
+                                if (u + 1 == n_u && half == 1) tc_commit(&sm->o_full[g]);
+                            }
+                            __syncwarp();
+                        }
+                        if (ok && u + 1 < n_u) {
+                            const int next = pair ? t + 1 : t + 2;
+                            ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->k_full[next & 1], (uint32_t)((next >> 1) & 1), abort, 270));
+                            if (!ok) break;
+                            tc_fence_after();
+                            if (elect_one()) issue_qk(next & 1);
                             __syncwarp();
                         }
                     }
@@ -1512,8 +1546,8 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     } else {
         const long long rows = (long long)pool.n_pages * pool.Hkv * pool.T;
         CUtensorMap mk, mv;
-        if (int rc = make_pool_map(&mk, pool.k8, rows, pool.T < kQStep ? pool.T : kQStep)) return rc;
-        if (int rc = make_pool_map(&mv, pool.v8, rows, pool.T < kQStep ? pool.T : kQStep)) return rc;
+        if (int rc = make_pool_map(&mk, pool.k8, rows, pool.T < kQSub ? pool.T : kQSub)) return rc;
+        if (int rc = make_pool_map(&mv, pool.v8, rows, pool.T < kQSub ? pool.T : kQSub)) return rc;
         e = launch_kernel(page_question_kernel, dim3(ctas), dim3(kQThreads), kQuestionSmem + prefix_bytes(n), stream, mk, mv, a);
     }
     count_launch();
