@@ -23,6 +23,7 @@ struct PageAttnArgs {
     int n, L_q, Hq, G;
     int rows;              // query rows of a KV head: L_q * G, row r is token r / G, head r % G of the group
     int units;             // tiles of them: what a step of keys of one (sequence, KV head) costs
+    int pad;               // what a segment costs beyond its steps
     float scale_log2;      // softmax scale * log2(e)
     const int32_t* seqs; const int32_t* lens; const int32_t* table;
     const __nv_bfloat16* q; __nv_bfloat16* out; float* lse;
@@ -105,8 +106,8 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {            // 0xFF w
     return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
 }
 
-// A place on the work axis: a segment is (b, h, block), a block `width` tiles (kW, or one less in the last), and each of its steps
-// takes `width` places.
+// A place on the work axis: a segment is (b, h, block), a block `width` tiles (kW, or one less in the last).  It takes a.pad places, for
+// what it costs beyond its steps, and `width` places for each of them.
 struct Place { int b, h, block, width, step, n_steps, seq, len; };
 
 // Running sums of the sequences' steps (of one tile) in shared memory: pre[b] = steps of sequences 0 .. b - 1.  (4096 sequences of 4M
@@ -182,37 +183,45 @@ __device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* p
     x.n_steps = pre[x.b + 1] - pre[x.b];
     x.seq = a.seqs != nullptr ? __ldg(a.seqs + x.b) : x.b;
 }
-// The first step that begins at or behind `at` (which is less than the total).
+// Places that one tile's row of steps takes, that one (sequence, KV head) takes, and all of them.
+template <int kW>
+__device__ __forceinline__ long long head_places(const PageAttnArgs& a, int n_steps) {
+    return (long long)n_steps * a.units + (long long)a.pad * ((a.units + kW - 1) / kW);
+}
+template <int kW>
+__device__ __forceinline__ long long places_before(const PageAttnArgs& a, const int* pre, int b) {       // of sequences 0 .. b - 1
+    return a.p.Hkv * ((long long)pre[b] * a.units + (long long)b * a.pad * ((a.units + kW - 1) / kW));
+}
+// The first step that begins at or behind `at` (which is less than the total); a place in front of a segment's first step stands for it.
 template <int kW>
 __device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre, long long at) {
-    const long long per = (long long)a.p.Hkv * a.units;
-    int lo = 0, hi = a.n - 1;                    // last b with pre[b] * per <= at
+    int lo = 0, hi = a.n - 1;                    // last b whose places begin at or in front of `at`
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (pre[mid] * per <= at) lo = mid; else hi = mid - 1;
+        if (places_before<kW>(a, pre, mid) <= at) lo = mid; else hi = mid - 1;
     }
     Place x;
     x.b = lo;
     x.len = seq_len(a, lo);
     x.seq = a.seqs != nullptr ? __ldg(a.seqs + lo) : lo;
     x.n_steps = pre[lo + 1] - pre[lo];
-    long long rest = at - pre[lo] * per;
-    const long long head = (long long)x.n_steps * a.units;
+    long long rest = at - places_before<kW>(a, pre, lo);
+    const long long head = head_places<kW>(a, x.n_steps), block = (long long)kW * x.n_steps + a.pad;
     x.h = (int)axis_div(rest, head);
     rest -= x.h * head;
-    x.block = kW == 1 && a.units == 1 ? 0 : (int)axis_div(rest, (long long)kW * x.n_steps);
+    x.block = kW == 1 && a.units == 1 ? 0 : (int)axis_div(rest, block);
     x.width = min(kW, a.units - kW * x.block);
-    rest -= (long long)x.block * kW * x.n_steps;
+    rest = max(rest - x.block * block - a.pad, 0ll);
     x.step = kW == 1 ? (int)rest : (int)((rest + x.width - 1) >> (x.width - 1));       // (a block's width is 1 or 2)
     if (x.step == x.n_steps) next_segment<kW>(a, pre, x);
     return x;
 }
-// Where a place lies on the axis.
+// The last place that stands for a place's step.
 template <int kW>
 __device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* pre, const Place& x) {
-    if (x.b >= a.n) return (long long)pre[a.n] * a.p.Hkv * a.units;
-    return (long long)pre[x.b] * a.p.Hkv * a.units + (long long)x.n_steps * (x.h * a.units + kW * x.block) + (long long)x.step * x.width;
+    return places_before<kW>(a, pre, x.b) + x.h * head_places<kW>(a, x.n_steps) + x.block * ((long long)kW * x.n_steps + a.pad) + a.pad + (long long)x.step * x.width;
 }
+
 // A row's factor 1 / sum (a row that saw nothing: 0), its log-sum-exp, and the weight of a partial with (maximum, sum) in a merge
 // whose largest maximum is mx.  A maximum of -inf with a sum other than 0 is a row of NaN logits: it stays one.
 __device__ __forceinline__ float row_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
@@ -242,7 +251,7 @@ page_decode_kernel(const PageAttnArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     sum_steps<kDecodeWarps * 32>(a, kStep, pre, warp_sums);
-    const long long total = (long long)pre[a.n] * a.p.Hkv;
+    const long long total = places_before<1>(a, pre, a.n);
     // CTAs that take part: no more than give each of its warps a step
     const long long ctas = min((long long)gridDim.x, (total + kDecodeWarps - 1) / kDecodeWarps);
     const Shares shares = share(total, ctas);
@@ -627,8 +636,8 @@ page_decode_kernel(const PageAttnArgs a) {
     }
     if (threadIdx.x == (kDecodeWarps - 1) * 32) {       // (a warp with the fewest rows to merge)
         if (chain.last_cta == 0) {
-            const long long end = (long long)pre[chain.b] * Hkv + (long long)(chain.h + 1) * (pre[chain.b + 1] - pre[chain.b]);
-            chain.last_cta = cta_of(shares, end - 1);
+            const int n_steps = pre[chain.b + 1] - pre[chain.b];
+            chain.last_cta = cta_of(shares, axis_at<1>(a, pre, Place{chain.b, chain.h, 0, 1, n_steps - 1, n_steps, 0, 0}));
         }
         a.chains[blockIdx.x] = chain;
     }
@@ -650,6 +659,7 @@ page_decode_kernel(const PageAttnArgs a) {
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 128, kQSub = 64;
 constexpr int kQStages = 2;        // half steps
+constexpr int kQPad = 8;           // tile steps that a piece of work costs beyond its own (rows of Q in, results out: some 18,000 clocks)
 constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
 constexpr int kQThreads = 640;
@@ -681,7 +691,7 @@ struct QuestionSmem {
     // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
     Place at;
     int step1, n_t, first_limit, last_limit;      // steps at.step .. step1 - 1, of which the first n_t have keys that some row sees
-    long long x, hi;
+    Place end;
     Shares shares;
     ChainEntry chain;
 };
@@ -863,18 +873,16 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     const uint32_t tmem = sm->tmem_base;
     const int T = a.p.T, Hkv = a.p.Hkv;
     if (warp == 0) {
-        const long long total = (long long)pre[a.n] * Hkv * a.units;
+        const long long total = places_before<2>(a, pre, a.n);
         const long long ctas = min((long long)gridDim.x, (total + 1) / 2);       // no fewer than two steps of a tile each
         const Shares shares = share(total, ctas);
         // lane 0 finds the stretch's begin, lane 1 its end; both move up to the next step's begin
         const long long from = cta_begin(shares, min((long long)blockIdx.x + min(lane, 1), ctas));
         Place at = {};
-        long long x = total;
-        if (from < total) { at = place_at<2>(a, pre, from); x = axis_at<2>(a, pre, at); }
-        const long long hi = __shfl_sync(0xFFFFFFFFu, x, 1);
+        at.b = a.n;
+        if (from < total) at = place_at<2>(a, pre, from);
+        if (lane == 1) sm->end = at;
         if (lane == 0) {
-            sm->x = x;
-            sm->hi = hi;
             sm->at = at;
             sm->step1 = 0;
             sm->shares = shares;
@@ -890,23 +898,23 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             // ---- one segment, or this CTA's stretch of it
             if (threadIdx.x == 0) {
                 if (sm->step1 > 0) {            // behind the piece before
-                    sm->x += (long long)(sm->step1 - sm->at.step) * sm->at.width;
                     sm->at.step = sm->step1;
                     if (sm->at.step == sm->at.n_steps) next_segment<2>(a, pre, sm->at);
                 }
-                const Place at = sm->at;
+                const Place at = sm->at, end = sm->end;
                 sm->step1 = 0;
-                if (sm->x < sm->hi) {
-                    const int step1 = (int)min((long long)at.n_steps, at.step + ((sm->hi - sm->x) >> (at.width - 1)));       // (a width is 1 or 2)
+                const bool last = at.b == end.b && at.h == end.h && at.block == end.block;      // the stretch ends in this segment
+                if (at.b < a.n && !(last && at.step >= end.step)) {
+                    const int step1 = last ? end.step : at.n_steps;
                     const int row0 = at.block * kQRows, last_row = min(a.rows, row0 + kQRows) - 1;
                     sm->step1 = step1;
                     sm->first_limit = at.len - a.L_q + row0 / a.G;
                     sm->last_limit = at.len - a.L_q + last_row / a.G;
                     sm->n_t = max(0, min(step1, (sm->last_limit + kQStep) / kQStep) - at.step);       // (a negative limit: none)
                     if (at.step == 0 && step1 < at.n_steps) {
-                        Place end = at;
-                        end.step = at.n_steps - 1;
-                        sm->chain = ChainEntry{cta_of(sm->shares, axis_at<2>(a, pre, end)), at.b, at.h, at.block};
+                        Place tail = at;
+                        tail.step = at.n_steps - 1;
+                        sm->chain = ChainEntry{cta_of(sm->shares, axis_at<2>(a, pre, tail)), at.b, at.h, at.block};
                     }
                 }
                 sm->poison = 0;
@@ -1515,6 +1523,7 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     const int blocks = few_blocks(a.rows);
     const bool few = blocks > 0;
     a.units = few ? 1 : (a.rows + 127) / 128;
+    a.pad = few ? 0 : kQPad;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.seqs = seqs; a.lens = lens; a.table = table;
     a.q = reinterpret_cast<const __nv_bfloat16*>(q); a.out = reinterpret_cast<__nv_bfloat16*>(out); a.lse = lse;
