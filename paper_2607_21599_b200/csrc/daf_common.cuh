@@ -90,7 +90,7 @@ int launch_attention_joint(const void* q_imp, const void* q_fresh, bool q_in_pla
 
 // The paged 8-bit cache (daf_pages.cu: the C ABI of the daf_page_* calls and the kernels that write, read and manage pages;
 // daf_page_attn.cu: the attention over it).
-constexpr int kPageMaxSeqs = 4096;      // sequences of one attention call: their running sums of work lie in shared memory
+constexpr int kPageMaxSeqs = 2048;      // sequences of one attention call: their running sums of work lie in shared memory
 struct Pool {                           // one layer of it
     int n_pages, T, Hkv, n_seqs, max_pages;
     uint8_t* k8; uint8_t* v8; float* k_scale; float* v_scale;

@@ -110,8 +110,8 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {            // 0xFF w
 // what it costs beyond its steps, and `width` places for each of them.
 struct Place { int b, h, block, width, step, n_steps, seq, len; };
 
-// Running sums of the sequences' steps (of one tile) in shared memory: pre[b] = steps of sequences 0 .. b - 1.  (4096 sequences of 4M
-// tokens: 2^29 steps of 32 keys.)
+// Running sums of the sequences' steps (of one tile) in shared memory: pre[b] = steps of sequences 0 .. b - 1.  (2048 sequences of 4M
+// tokens: 2^28 steps of 32 keys.)
 __device__ __forceinline__ int seq_len(const PageAttnArgs& a, int b) {
     int len = __ldg(a.lens + b);
     const int seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b;
@@ -658,7 +658,7 @@ page_decode_kernel(const PageAttnArgs a) {
 // memory; with Q in tensor memory and one S: 110, the products' latency as long as a softmax step.)
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 128, kQSub = 64;
-constexpr int kQStages = 2;        // half steps
+constexpr int kQStages = 3;        // half steps
 constexpr int kQPad = 8;           // tile steps that a piece of work costs beyond its own (rows of Q in, results out: some 18,000 clocks)
 constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
@@ -700,7 +700,7 @@ constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK =
               kBarVEmpty = (int)(offsetof(QuestionSmem, v_empty) / 8), kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
               kBarS = (int)(offsetof(QuestionSmem, s_full) / 8), kBarP = (int)(offsetof(QuestionSmem, p_full) / 8),
               kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
-static_assert(offsetof(QuestionSmem, st_full) == 0 && kQStages == 2 && kBars <= 64, "what the barriers' numbers rest on");
+static_assert(offsetof(QuestionSmem, st_full) == 0 && kBarK % kQStages == 0 && kBarK % 2 == 0 && kBarS % 2 == 0 && kBarO % 2 == 0 && kBars <= 64, "what the barriers' numbers rest on");
 constexpr size_t kQuestionSmem = 1024 + kQOffStage + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
 __host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
@@ -795,7 +795,7 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
 
 // How many phases barrier i completes in a piece of n_t steps.
 __device__ __forceinline__ int bar_uses(int i, int n_t, bool pair) {
-    if (i < kBarK) return n_t;                                           // every other half step
+    if (i < kBarK) return (2 * n_t - i % kQStages + kQStages - 1) / kQStages;      // every third half step
     if (i < kBarV) return (n_t - (i & 1) + 1) >> 1;
     if (i < kBarQ) {
         const int slot = (i - kBarV) & 3;

@@ -154,8 +154,8 @@ def test_counts_layers_and_heads_are_checked():
     assert c["attn"](heads=0) == api.DAF_ERR_INVALID_ARG
     assert c["attn"](heads=5) == api.DAF_ERR_UNSUPPORTED
     assert c["attn"](heads=512) == api.DAF_ERR_UNSUPPORTED
-    assert c["attn"](n=4097) == api.DAF_ERR_UNSUPPORTED
-    assert c["attn"](n=4096, L_q=2000) == api.DAF_ERR_UNSUPPORTED
+    assert c["attn"](n=2049) == api.DAF_ERR_UNSUPPORTED
+    assert c["attn"](n=2048, L_q=4000) == api.DAF_ERR_UNSUPPORTED
     assert c["attn"](L_q=-1) == api.DAF_ERR_INVALID_ARG
     assert c["fork"](n=-1) == api.DAF_ERR_INVALID_ARG
     assert c["fork"](n=5) == api.DAF_ERR_INVALID_ARG               # more items than rows: one would be named twice

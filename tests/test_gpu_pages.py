@@ -436,7 +436,7 @@ def test_rows_of_the_table_in_any_order_and_twice():
         _attend(c, [200, 64, 150, 33, 10], L_q, 4, seqs=seqs, layer=1)
 
 
-@pytest.mark.parametrize("n,L_q,Hq,Hkv", [(300, 1, 4, 2), (4096, 1, 1, 1), (150, 20, 4, 1)])
+@pytest.mark.parametrize("n,L_q,Hq,Hkv", [(300, 1, 4, 2), (2048, 1, 1, 1), (150, 20, 4, 1)])
 def test_many_sequences(n, L_q, Hq, Hkv):
     rng = random.Random(n)
     lens = [rng.randint(0, 60) for _ in range(n)]
