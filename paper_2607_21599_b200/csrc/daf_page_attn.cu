@@ -679,6 +679,7 @@ struct QuestionSmem {
     uint64_t k_full[2], k_empty[2];                           // [buffer] a step's K, widened
     uint64_t v_full[4], v_empty[4];                           // [slot] half a step's V, widened
     uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2];   // [group], [half]
+    uint64_t turn[2][4];                                      // [group][warp] the other group's warp of the scheduler is done with its step
     uint64_t c_full[kQConsts];
     float4 chunk[kQConsts][4];      // of half a step's chunks of 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
     int missing[kQConsts];          // some keys of the half step have no page
@@ -699,7 +700,8 @@ constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK =
               kBarKEmpty = (int)(offsetof(QuestionSmem, k_empty) / 8), kBarV = (int)(offsetof(QuestionSmem, v_full) / 8),
               kBarVEmpty = (int)(offsetof(QuestionSmem, v_empty) / 8), kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
               kBarS = (int)(offsetof(QuestionSmem, s_full) / 8), kBarP = (int)(offsetof(QuestionSmem, p_full) / 8),
-              kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
+              kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarTurn = (int)(offsetof(QuestionSmem, turn) / 8),
+              kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
 static_assert(offsetof(QuestionSmem, st_full) == 0 && kBarK % kQStages == 0 && kBarK % 2 == 0 && kBarS % 2 == 0 && kBarO % 2 == 0 && kBars <= 64, "what the barriers' numbers rest on");
 constexpr size_t kQuestionSmem = 1024 + kQOffStage + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
@@ -802,6 +804,7 @@ __device__ __forceinline__ int bar_uses(int i, int n_t, bool pair) {
         return pair ? (slot < 2 ? n_t : 0) : (n_t - (slot >> 1) + 1) >> 1;
     }
     if (i < kBarS) return 1;
+    if (i >= kBarTurn && i < kBarC) return pair ? n_t : 0;
     if (i < kBarC) {
         const int g = i < kBarP || i >= kBarO ? i & 1 : ((i - kBarP) >> 1), steps = pair ? n_t : (n_t - g + 1) >> 1;    // of the group
         return i < kBarO ? steps : (steps > 0 ? 1 : 0);
@@ -998,6 +1001,9 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 ok = wait_phase(sm, odd, &sm->c_full[c0], (uint32_t)((2 * t / kQConsts) & 1), abort, 271);
                 if (ok) ok = wait_phase(sm, odd, &sm->c_full[c0 + 1], (uint32_t)((2 * t / kQConsts) & 1), abort, 273);
                 if (ok) ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
+                // The groups take turns (a scheduler's two warps, one of each): left to themselves they fall into step, wait for the
+                // exponentials together (16 a clock) and then for their products together.
+                if (ok && pair && (g == 1 || u > 0)) ok = wait_phase(sm, odd, &sm->turn[g][warp & 3], (uint32_t)((g == 1 ? u : u - 1) & 1), abort, 279);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -1022,6 +1028,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     if (lane == 0) mbar_arrive(&sm->p_full[g][half]);
                 };
                 question_softmax(s_addr, chunk, (sm->missing[c0] | sm->missing[c0 + 1]) != 0, (step0 + t) * kQStep, limit, c, m, l, rescale, half_done);
+                if (pair && lane == 0) mbar_arrive(&sm->turn[1 - g][warp & 3]);
             }
             if (ok && n_u > 0) ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->o_full[g], 0, abort, 274));
             tc_fence_after();
