@@ -107,7 +107,7 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {            // 0xFF w
 }
 
 // A place on the work axis: a segment is (b, h, block), a block `width` tiles (kW, or one less in the last).  It takes a.pad places, for
-// what it costs beyond its steps, and `width` places for each of them.
+// what it costs beyond its steps, and weight<kW>(width) places for each of them.
 struct Place { int b, h, block, width, step, n_steps, seq, len; };
 
 // Running sums of the sequences' steps (of one tile) in shared memory: pre[b] = steps of sequences 0 .. b - 1.  (2048 sequences of 4M
@@ -183,14 +183,17 @@ __device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* p
     x.n_steps = pre[x.b + 1] - pre[x.b];
     x.seq = a.seqs != nullptr ? __ldg(a.seqs + x.b) : x.b;
 }
-// Places that one tile's row of steps takes, that one (sequence, KV head) takes, and all of them.
+// What a step costs: in blocks of up to two tiles (many rows), one tile takes 0.68 of the time of two.
+template <int kW>
+__device__ __forceinline__ int weight(int width) { return kW == 1 ? 1 : width + 1; }
+// Places that one (sequence, KV head) takes, and that sequences 0 .. b - 1 take.
 template <int kW>
 __device__ __forceinline__ long long head_places(const PageAttnArgs& a, int n_steps) {
-    return (long long)n_steps * a.units + (long long)a.pad * ((a.units + kW - 1) / kW);
+    return (long long)n_steps * (a.units / kW * weight<kW>(kW) + (a.units % kW != 0 ? weight<kW>(1) : 0)) + (long long)a.pad * ((a.units + kW - 1) / kW);
 }
 template <int kW>
-__device__ __forceinline__ long long places_before(const PageAttnArgs& a, const int* pre, int b) {       // of sequences 0 .. b - 1
-    return a.p.Hkv * ((long long)pre[b] * a.units + (long long)b * a.pad * ((a.units + kW - 1) / kW));
+__device__ __forceinline__ long long places_before(const PageAttnArgs& a, const int* pre, int b) {
+    return a.p.Hkv * (head_places<kW>(a, pre[b]) + (long long)(b - 1) * a.pad * ((a.units + kW - 1) / kW));
 }
 // The first step that begins at or behind `at` (which is less than the total); a place in front of a segment's first step stands for it.
 template <int kW>
@@ -206,20 +209,20 @@ __device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre,
     x.seq = a.seqs != nullptr ? __ldg(a.seqs + lo) : lo;
     x.n_steps = pre[lo + 1] - pre[lo];
     long long rest = at - places_before<kW>(a, pre, lo);
-    const long long head = head_places<kW>(a, x.n_steps), block = (long long)kW * x.n_steps + a.pad;
+    const long long head = head_places<kW>(a, x.n_steps), block = (long long)weight<kW>(kW) * x.n_steps + a.pad;
     x.h = (int)axis_div(rest, head);
     rest -= x.h * head;
     x.block = kW == 1 && a.units == 1 ? 0 : (int)axis_div(rest, block);
     x.width = min(kW, a.units - kW * x.block);
     rest = max(rest - x.block * block - a.pad, 0ll);
-    x.step = kW == 1 ? (int)rest : (int)((rest + x.width - 1) >> (x.width - 1));       // (a block's width is 1 or 2)
+    x.step = kW == 1 ? (int)rest : (int)axis_div(rest + weight<kW>(x.width) - 1, weight<kW>(x.width));
     if (x.step == x.n_steps) next_segment<kW>(a, pre, x);
     return x;
 }
 // The last place that stands for a place's step.
 template <int kW>
 __device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* pre, const Place& x) {
-    return places_before<kW>(a, pre, x.b) + x.h * head_places<kW>(a, x.n_steps) + x.block * ((long long)kW * x.n_steps + a.pad) + a.pad + (long long)x.step * x.width;
+    return places_before<kW>(a, pre, x.b) + x.h * head_places<kW>(a, x.n_steps) + x.block * ((long long)weight<kW>(kW) * x.n_steps + a.pad) + a.pad + (long long)x.step * weight<kW>(x.width);
 }
 
 // A row's factor 1 / sum (a row that saw nothing: 0), its log-sum-exp, and the weight of a partial with (maximum, sum) in a merge
@@ -659,7 +662,7 @@ page_decode_kernel(const PageAttnArgs a) {
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 128, kQSub = 64;
 constexpr int kQStages = 3;        // half steps
-constexpr int kQPad = 8;           // tile steps that a piece of work costs beyond its own (rows of Q in, results out: some 18,000 clocks)
+constexpr int kQPad = 12;          // places (a step of two tiles takes three) that a piece of work costs: rows of Q in, results out, some 18,000 clocks
 constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
 constexpr int kQThreads = 640;
@@ -877,7 +880,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     const int T = a.p.T, Hkv = a.p.Hkv;
     if (warp == 0) {
         const long long total = places_before<2>(a, pre, a.n);
-        const long long ctas = min((long long)gridDim.x, (total + 1) / 2);       // no fewer than two steps of a tile each
+        const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than two steps of a tile each
         const Shares shares = share(total, ctas);
         // lane 0 finds the stretch's begin, lane 1 its end; both move up to the next step's begin
         const long long from = cta_begin(shares, min((long long)blockIdx.x + min(lane, 1), ctas));
@@ -1001,14 +1004,14 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 ok = wait_phase(sm, odd, &sm->c_full[c0], (uint32_t)((2 * t / kQConsts) & 1), abort, 271);
                 if (ok) ok = wait_phase(sm, odd, &sm->c_full[c0 + 1], (uint32_t)((2 * t / kQConsts) & 1), abort, 273);
                 if (ok) ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
-                // The groups take turns (a scheduler's two warps, one of each): left to themselves they fall into step, wait for the
-                // exponentials together (16 a clock) and then for their products together.
-                if (ok && pair && (g == 1 || u > 0)) ok = wait_phase(sm, odd, &sm->turn[g][warp & 3], (uint32_t)((g == 1 ? u : u - 1) & 1), abort, 279);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const float4* const chunk[2] = {sm->chunk[c0], sm->chunk[c0 + 1]};
                 auto rescale = [&](float alpha) {
+                    // The groups take turns (a scheduler's two warps, one of each): left to themselves they fall into step, wait for the
+                    // exponentials together (16 a clock) and then for their products together.
+                    if (ok && pair && (g == 1 || u > 0)) ok = wait_phase(sm, odd, &sm->turn[g][warp & 3], (uint32_t)((g == 1 ? u : u - 1) & 1), abort, 279);
                     // (the logits came behind the product before, so O is quiet)
                     if (u == 0 || !__any_sync(0xFFFFFFFFu, alpha != 1.f)) return;
 #pragma unroll 1
@@ -1029,6 +1032,8 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 };
                 question_softmax(s_addr, chunk, (sm->missing[c0] | sm->missing[c0 + 1]) != 0, (step0 + t) * kQStep, limit, c, m, l, rescale, half_done);
                 if (pair && lane == 0) mbar_arrive(&sm->turn[1 - g][warp & 3]);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
             }
             if (ok && n_u > 0) ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->o_full[g], 0, abort, 274));
             tc_fence_after();
