@@ -25,16 +25,18 @@ __device__ __forceinline__ float4 unpack_e4m3x4(uint32_t w) {
 }
 __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }      // -126 <= e <= 127
 
-// Largest magnitude (bf16 bits, which ascend with it) among the finite ones of four bf16 values.
-__device__ __forceinline__ uint32_t finite_max4(uint2 w) {
+// Largest magnitude (bf16 bits, which ascend with it) among the finite ones of eight bf16 values.
+__device__ __forceinline__ uint32_t finite_max8(uint4 w) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t b = ((i & 2 ? w.y : w.x) >> (16 * (i & 1))) & 0x7FFFu;
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t x = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w, b = (x >> (16 * (i & 1))) & 0x7FFFu;
         m = max(m, b < 0x7F80u ? b : 0u);
     }
     return m;
 }
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 // Exponent of the least power of two s with magnitude <= 448 s (448 = 1.75 * 2^8), at least kMinScaleExp.
 __device__ __forceinline__ int scale_exp(uint32_t bf16_bits) {
     const int e = (int)(bf16_bits >> 7) - 127 - 8 + ((bf16_bits & 0x7Fu) > 0x60u ? 1 : 0);
@@ -66,70 +68,85 @@ __device__ __forceinline__ int first_at_least(const int32_t* idx, int a, int b, 
 }
 
 // One CTA of four warps takes one page, one head, K or V at a time.  Every new row of it is read once and held in registers
-// (kRows rows a warp, four elements a lane) while the CTA finds their largest magnitude; the rows then leave scaled.  Kept bytes are
-// touched only where the scale grows.
-template <int kRows>
+// (sixteen lanes a row, eight elements each) while the CTA finds their largest magnitude; the rows then leave scaled.  Kept bytes are
+// touched only where the scale grows.  kGiven: positions come from a list, through a table in shared memory of which row a token
+// gets; otherwise the rows are the newest tokens, whose addresses need nothing but the length, and are asked for ahead of the page.
+template <int kTokens, bool kGiven>
 __global__ void __launch_bounds__(128) page_write_kernel(const WriteArgs a) {
-    __shared__ int row_of[4 * kRows];          // new row of each token of the page, -1: none
+    constexpr int T = kTokens, kPer = T / 8;      // tokens of a lane
+    __shared__ int row_of[kGiven ? T : 1];        // new row of each token of the page, -1: none
     __shared__ uint32_t warp_max[4];
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int T = 4 * kRows;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = threadIdx.x >> 4, piece = threadIdx.x & 15;
     const int b = blockIdx.x / a.slots, h = blockIdx.y, Hkv = a.p.Hkv;
     const bool reports = h == 0 && blockIdx.z == 0;       // (one of the CTAs that see the same fault)
     const int seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b, len = __ldg(a.lens + b);
     const int r_lo = __ldg(a.row_off + b), r_hi = __ldg(a.row_off + b + 1);
     if (r_hi <= r_lo) return;
     if ((unsigned)seq >= (unsigned)a.p.n_seqs || len < 0 || (long long)len > (long long)a.p.max_pages * T || r_lo < 0 ||
-        (a.idx == nullptr && r_hi - r_lo > len)) {
-        if (reports) report_status(a.status, DAF_ERR_BOUNDS, 200, b);
+        (!kGiven && r_hi - r_lo > len)) {
+        if (reports && threadIdx.x == 0) report_status(a.status, DAF_ERR_BOUNDS, 200, b);
         return;
     }
-    const int start = a.idx == nullptr ? len - (r_hi - r_lo) : 0;       // first token that may be written
-    const int kept_to = a.idx == nullptr ? start : len;                 // tokens below this were there before
-    const __nv_bfloat16* const src = blockIdx.z ? a.v : a.k;
+    const int start = kGiven ? 0 : len - (r_hi - r_lo);       // first token that may be written
+    const int kept_to = kGiven ? len : start;                 // tokens below this were there before
+    const uint4* const src = reinterpret_cast<const uint4*>((blockIdx.z ? a.v : a.k) + (size_t)h * 128) + piece;
     uint8_t* const pool = blockIdx.z ? a.p.v8 : a.p.k8;
     float* const scales = blockIdx.z ? a.p.v_scale : a.p.k_scale;
     for (int j = start / T + (int)(blockIdx.x % a.slots); j * T < len; j += a.slots) {
         const int base = j * T;
-        int ra, rb;
-        if (a.idx == nullptr) {
-            ra = r_lo + max(base, start) - start;
-            rb = r_lo + min(base + T, len) - start;
-        } else {
+        int ra = 0, rb = 1;
+        if (kGiven) {
             ra = first_at_least(a.idx, r_lo, r_hi, base);
             rb = first_at_least(a.idx, ra, r_hi, base + T);
         }
         if (ra >= rb) continue;
         const int page = __ldg(a.table + (size_t)seq * a.p.max_pages + j);
+        uint4 w[kPer];
+        uint32_t news = 0;            // which of this lane's tokens get a new row
+        auto take = [&](int i, int r) {
+            news |= 1u << i;
+            w[i] = __ldg(src + (size_t)r * Hkv * 16);
+        };
+        if (!kGiven) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int at = base + 8 * i + sub;
+                w[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (at >= start && at < len) take(i, r_lo + at - start);
+            }
+        }
         const bool in_pool = (unsigned)page < (unsigned)a.p.n_pages;
         if (!in_pool || (a.refs != nullptr && __ldg(a.refs + page) != 1)) {
-            if (reports) report_status(a.status, DAF_ERR_BOUNDS, in_pool ? 202 : 201, page);
+            if (reports && threadIdx.x == 0) report_status(a.status, DAF_ERR_BOUNDS, in_pool ? 202 : 201, page);
             continue;
-        }
-        for (int t = threadIdx.x; t < T; t += 128) row_of[t] = -1;
-        __syncthreads();
-        for (int r = ra + threadIdx.x; r < rb; r += 128) {
-            const int at = a.idx == nullptr ? r - r_lo + start : __ldg(a.idx + r);
-            if (at >= base && at < min(base + T, len)) atomicMax(&row_of[at - base], r);
-            else if (reports) report_status(a.status, DAF_ERR_BOUNDS, 203, at);       // the list does not ascend
-        }
-        __syncthreads();
-        uint2 w[kRows];
-        uint32_t m = 0;
-        bool keeps = false;
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = row_of[warp + 4 * i];
-            w[i] = make_uint2(0u, 0u);
-            if (r >= 0) w[i] = __ldg(reinterpret_cast<const uint2*>(src + ((size_t)r * Hkv + h) * 128) + lane);
-            else keeps |= base + warp + 4 * i < kept_to;
         }
         float* const scale_at = scales + (size_t)page * Hkv + h;
         const float s_old = __ldcg(scale_at);
+        if (kGiven) {
+            for (int t = threadIdx.x; t < T; t += 128) row_of[t] = -1;
+            __syncthreads();
+            for (int r = ra + threadIdx.x; r < rb; r += 128) {
+                const int at = __ldg(a.idx + r);
+                if (at >= base && at < min(base + T, len)) atomicMax(&row_of[at - base], r);
+                else if (reports) report_status(a.status, DAF_ERR_BOUNDS, 203, at);       // the list does not ascend, or not in the sequence
+            }
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) m = max(m, finite_max4(w[i]));
+            for (int i = 0; i < kPer; ++i) {
+                const int r = row_of[8 * i + sub];
+                w[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (r >= 0) take(i, r);
+            }
+        }
+        uint32_t m = 0;
+        bool keeps = false;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            m = max(m, finite_max8(w[i]));
+            keeps |= !((news >> i) & 1u) && base + 8 * i + sub < kept_to;
+        }
         m = __reduce_max_sync(0xFFFFFFFFu, m);
         if (lane == 0) warp_max[warp] = m;
         keeps = __syncthreads_or(keeps);
@@ -139,20 +156,20 @@ __global__ void __launch_bounds__(128) page_write_kernel(const WriteArgs a) {
             const int bits = __float_as_int(s_old);
             e = max(e, min((bits >> 23) - 127 + ((bits & 0x7FFFFF) != 0 ? 1 : 0), 120));
         }
-        uint32_t* const dst = reinterpret_cast<uint32_t*>(pool + ((size_t)page * Hkv + h) * (T * 128)) + lane;
+        uint2* const dst = reinterpret_cast<uint2*>(pool + ((size_t)page * Hkv + h) * (T * 128)) + piece;
         const float inv = pow2f(-e), s_new = pow2f(e);
         const bool again = keeps && s_new != s_old;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int t = warp + 4 * i;
-            if (row_of[t] >= 0) {
-                const float x0 = __uint_as_float(w[i].x << 16), x1 = __uint_as_float(w[i].x & 0xFFFF0000u);
-                const float x2 = __uint_as_float(w[i].y << 16), x3 = __uint_as_float(w[i].y & 0xFFFF0000u);
-                dst[t * 32] = pack_e4m3x4(x0 * inv, x1 * inv, x2 * inv, x3 * inv);
+        for (int i = 0; i < kPer; ++i) {
+            const int t = 8 * i + sub;
+            if ((news >> i) & 1u) {
+                dst[t * 16] = make_uint2(pack_e4m3x4(bf16_lo(w[i].x) * inv, bf16_hi(w[i].x) * inv, bf16_lo(w[i].y) * inv, bf16_hi(w[i].y) * inv),
+                                         pack_e4m3x4(bf16_lo(w[i].z) * inv, bf16_hi(w[i].z) * inv, bf16_lo(w[i].w) * inv, bf16_hi(w[i].w) * inv));
             } else if (again && base + t < kept_to) {
                 const float f = s_old * inv;
-                const float4 x = unpack_e4m3x4(dst[t * 32]);
-                dst[t * 32] = pack_e4m3x4(x.x * f, x.y * f, x.z * f, x.w * f);
+                const uint2 old = dst[t * 16];
+                const float4 x = unpack_e4m3x4(old.x), y = unpack_e4m3x4(old.y);
+                dst[t * 16] = make_uint2(pack_e4m3x4(x.x * f, x.y * f, x.z * f, x.w * f), pack_e4m3x4(y.x * f, y.y * f, y.z * f, y.w * f));
             }
         }
         if (threadIdx.x == 0) *scale_at = s_new;
@@ -695,8 +712,10 @@ int daf_page_write(const daf_page_params* p, int32_t layer, int32_t n, const int
     a.seqs = seqs; a.lens = lens; a.row_off = row_off; a.idx = idx;
     a.k = reinterpret_cast<const __nv_bfloat16*>(k); a.v = reinterpret_cast<const __nv_bfloat16*>(v);
     a.table = table; a.refs = refs; a.status = reinterpret_cast<DeviceStatus*>(workspace);
-    auto* kernel = p->page_tokens == 16 ? page_write_kernel<4> : p->page_tokens == 32 ? page_write_kernel<8>
-                 : p->page_tokens == 64 ? page_write_kernel<16> : page_write_kernel<32>;
+    auto* kernel = p->page_tokens == 16 ? (idx ? page_write_kernel<16, true> : page_write_kernel<16, false>)
+                 : p->page_tokens == 32 ? (idx ? page_write_kernel<32, true> : page_write_kernel<32, false>)
+                 : p->page_tokens == 64 ? (idx ? page_write_kernel<64, true> : page_write_kernel<64, false>)
+                                        : (idx ? page_write_kernel<128, true> : page_write_kernel<128, false>);
     return launched(launch_kernel(kernel, dim3((unsigned)n * a.slots, p->n_kv_heads, 2), dim3(128), 0, (cudaStream_t)stream, a));
 }
 
