@@ -371,7 +371,8 @@ int64_t daf_launch_count(void);
  * pages from device memory, so that a captured graph can be replayed while they change.
  * Where a call takes `seqs` (int32 [n]), entry b of the call is row seqs[b] of `table`; NULL: row b.  Rows and sequences outside
  * their tensors, and pages outside the pool where a sequence needs one, are skipped and recorded in the workspace's status word
- * (DAF_ERR_BOUNDS from daf_poll_status): nothing faults.  Calls that change the same table, refs or pages must not overlap. */
+ * (DAF_ERR_BOUNDS from daf_poll_status): nothing faults.  Calls that change the same table, refs or pages must not overlap, and a
+ * call that changes pages or rows of the table names a sequence once. */
 typedef struct daf_page_params {
     int32_t n_pages;          /* pages of the pool (of each layer)                               */
     int32_t page_tokens;      /* tokens of a page: 16, 32, 64 or 128                             */

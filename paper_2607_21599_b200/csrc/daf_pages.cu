@@ -89,6 +89,10 @@ __global__ void __launch_bounds__(128) page_write_kernel(const WriteArgs a) {
         if (reports && threadIdx.x == 0) report_status(a.status, DAF_ERR_BOUNDS, 200, b);
         return;
     }
+    if (kGiven && reports && blockIdx.x % a.slots == 0 && threadIdx.x < 2) {      // the first and the last position: the others lie between
+        const int at = __ldg(a.idx + (threadIdx.x == 0 ? r_lo : r_hi - 1));
+        if (at < 0 || at >= len) report_status(a.status, DAF_ERR_BOUNDS, 203, at);
+    }
     const int start = kGiven ? 0 : len - (r_hi - r_lo);       // first token that may be written
     const int kept_to = kGiven ? len : start;                 // tokens below this were there before
     const uint4* const src = reinterpret_cast<const uint4*>((blockIdx.z ? a.v : a.k) + (size_t)h * 128) + piece;
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(128) page_write_kernel(const WriteArgs a) {
             for (int r = ra + threadIdx.x; r < rb; r += 128) {
                 const int at = __ldg(a.idx + r);
                 if (at >= base && at < min(base + T, len)) atomicMax(&row_of[at - base], r);
-                else if (reports) report_status(a.status, DAF_ERR_BOUNDS, 203, at);       // the list does not ascend, or not in the sequence
+                else if (reports) report_status(a.status, DAF_ERR_BOUNDS, 204, at);       // the list does not ascend
             }
             __syncthreads();
 #pragma unroll
@@ -556,6 +560,9 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const Compac
         const unsigned used = used_bits(p);
         const unsigned below = p >= live ? 0u : (live - p >= kPlanRefs ? (1u << kPlanRefs) - 1u : (1u << (live - p)) - 1u);
         unsigned hole = ~used & below, mover = used & ~below;
+#pragma unroll
+        for (int u = 0; u < kPlanRefs; ++u)      // (an entry of the table must not name these)
+            if (p + u >= live && p + u < a.n_pages && !((mover >> u) & 1u)) a.w.fresh[p + u] = -1;
         const unsigned long long at = block_scan(pack2(__popc(hole), __popc(mover)), &sum);
         int h = holes + (int)(at >> 32), v = movers + (int)(at & 0xFFFFFFFFu);
         for (; hole != 0; hole &= hole - 1) a.w.copies[h++].y = p + __ffs(hole) - 1;
@@ -592,8 +599,11 @@ __global__ void __launch_bounds__(kMoveThreads) compact_apply_kernel(const Compa
     const PlanHead head = *a.w.head;
     for (long long i = (long long)blockIdx.x * kMoveThreads + threadIdx.x; i < a.entries; i += (long long)gridDim.x * kMoveThreads) {
         int page = a.table[i];
-        if (page >= a.n_pages) { report_status(a.status, DAF_ERR_BOUNDS, 240, page); page = -1; }
-        else if (page >= head.live) page = a.w.fresh[page];
+        if (page >= head.live) {
+            const int to = page < a.n_pages ? a.w.fresh[page] : -1;
+            if (to < 0) report_status(a.status, DAF_ERR_BOUNDS, 240, page);      // outside the pool, or of no count
+            page = to;
+        }
         a.table_out[i] = page < 0 ? -1 : page;
     }
     move_pages(m, a.w.copies, head.n_copies);
@@ -670,11 +680,15 @@ static int touched_pages(const daf_page_params* p, int rows) {
     const int t = (rows + p->page_tokens - 2) / p->page_tokens + 1;
     return t < p->max_pages ? t : p->max_pages;
 }
-// CTAs for an entry's pages: at least one, all of `pages` unless the grid's first dimension would overflow.
-static int page_slots(int n, int pages) {
-    const long long most = 0x7FFFFFFFll / n;
-    return (int)(pages < most ? pages : most);
+// CTAs for an entry's pages (for each head, K and V apart): one per page, but no more than `most` in the whole grid as long as each
+// entry has one.  The grid's first dimension stays in its range either way.
+static int page_slots(const daf_page_params* p, int n, int pages, long long most) {
+    most /= 2ll * p->n_kv_heads * n;
+    const long long room = 0x7FFFFFFFll / n;
+    if (most > room) most = room;
+    return (int)(pages < most ? pages : most < 1 ? 1 : most);
 }
+constexpr long long kAllPages = 1ll << 40;
 
 }  // namespace daf
 
@@ -708,7 +722,9 @@ int daf_page_write(const daf_page_params* p, int32_t layer, int32_t n, const int
     if (int rc = check_ints(ints, 6)) return rc;
     WriteArgs a;
     a.p = layer_of(p, layer, k8, v8, k_scale, v_scale);
-    a.n = n; a.slots = page_slots(n, idx == nullptr ? touched_pages(p, max_rows) : p->max_pages);
+    a.n = n;
+    // (given positions may lie anywhere in a row of the table: CTAs for all of it, up to some rounds of the GPU)
+    a.slots = idx == nullptr ? page_slots(p, n, touched_pages(p, max_rows), kAllPages) : page_slots(p, n, p->max_pages, 16384);
     a.seqs = seqs; a.lens = lens; a.row_off = row_off; a.idx = idx;
     a.k = reinterpret_cast<const __nv_bfloat16*>(k); a.v = reinterpret_cast<const __nv_bfloat16*>(v);
     a.table = table; a.refs = refs; a.status = reinterpret_cast<DeviceStatus*>(workspace);
@@ -734,7 +750,7 @@ int daf_page_read(const daf_page_params* p, int32_t layer, int32_t n, const int3
     if (int rc = check_ints(ints, 4)) return rc;
     ReadArgs a;
     a.p = layer_of(p, layer, k8, v8, k_scale, v_scale);
-    a.n = n; a.slots = page_slots(n, touched_pages(p, max_rows));
+    a.n = n; a.slots = page_slots(p, n, touched_pages(p, max_rows), kAllPages);
     a.seqs = seqs; a.first = first; a.row_off = row_off; a.table = table;
     a.k = reinterpret_cast<__nv_bfloat16*>(k_rows); a.v = reinterpret_cast<__nv_bfloat16*>(v_rows);
     a.status = reinterpret_cast<DeviceStatus*>(workspace);

@@ -211,6 +211,32 @@ def test_positions_outside_the_sequence_are_skipped():
     c.same()
 
 
+@pytest.mark.parametrize("length,idx,inside", [(64, [-1, 5, 9], [1, 2]), (20, [5, 48, 63], [0]), (20, [64, 65, 1000], []), (0, [0, 1, 2], [])])
+def test_positions_far_outside_the_sequence_are_reported(length, idx, inside):
+    c = Cache(8, 16, 1, 1, 4, seed=8, junk=False)
+    c.give(0, 64)
+    ws = _ws(c)
+    x = _rows(3, 1, 4)
+    api.check(api.daf_page_write(c.p, 0, 1, None, _i32([length]), _i32([0, 3]), _i32(idx), 3, x.to(DEV), x.to(DEV), c.t["table"],
+                                 c.t["refs"], *c.pool(), ws))
+    assert api.daf_poll_status(ws) == api.DAF_ERR_BOUNDS
+    for n in "kv":
+        O.write(c.np[n + "8"], c.np[n + "_scale"], 0, None, [length], [0, len(inside)], [idx[i] for i in inside], x[inside].float().numpy(), c.np["table"])
+    c.same()
+
+
+def test_rows_replaced_in_a_table_of_many_columns():
+    # more columns than an entry has thread blocks: 2 * 8 heads * 4 entries leave each 256
+    c = Cache(2100, 16, 8, 4, 1000, seed=12, junk=False)
+    lens = [16000, 30, 9001, 5000]
+    for s, L in enumerate(lens):
+        c.give(s, L, up=False)
+    c.up()
+    idx = [list(range(s, L, 37 + s)) for s, L in enumerate(lens)]
+    _write(c, lens, [len(i) for i in idx], idx=sum(idx, []), spread=3.0)
+    c.same()
+
+
 # ---------------------------------------------------------------------------------------------------------------------- read
 @pytest.mark.parametrize("T,Hkv", [(16, 1), (32, 8), (64, 4), (128, 3)])
 def test_read(T, Hkv):
@@ -624,6 +650,20 @@ def test_large_pool_and_many_items():
     keep = [rng.randint(0, int((c.np["table"][s] >= 0).sum()) * 16) for s in src]
     assert _fork(c, src, empty, keep, [min(640, k + 40) for k in keep], True) == ""
     _compact(c, in_place=False)
+
+
+def test_compact_reports_entries_whose_page_has_no_count():
+    c = Cache(9, 16, 1, 2, 4, seed=1, junk=False)
+    c.np["table"][0, :3] = [8, 6, 7]
+    c.np["refs"][[8, 7]] = 1                  # nothing counts page 6
+    c.np["table"][1, 0] = 9                   # outside the pool
+    c.up()
+    ws = _ws(c)
+    ws.view(torch.uint8)[256:].fill_(3)       # whatever an earlier call left there
+    api.check(api.daf_page_compact(c.p, c.t["table"], c.t["refs"], c.t["table"], c.t["refs"], None, *c.pool(), ws))
+    assert api.daf_poll_status(ws) == api.DAF_ERR_BOUNDS
+    assert c.t["table"].cpu().tolist() == [[1, -1, 0, -1], [-1, -1, -1, -1]]
+    assert c.t["refs"].cpu().tolist() == [1, 1] + [0] * 7
 
 
 def test_free_reports_rows_and_counts_that_are_wrong():
