@@ -10,7 +10,6 @@
 
 #include <atomic>
 #include <type_traits>
-#include <vector>
 
 #include "daf_common.cuh"
 
@@ -724,8 +723,9 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 
 // One softmax step of one row over 128 keys: P over the first half of the logits' columns, running maximum and sum.  `rescale` is called
 // ahead of the first P with the factor for the row of O (1 unless the maximum grew by more than kLazy), `half_done` when half of P is
-// on its way to tensor memory.  c: the row's factor for its logits; chunk: two half steps' constants.  The logits are fetched twice,
-// for the maximum and for the exponentials: a thread has no room for 128 of them.
+// on its way to tensor memory.  c: the row's factor for its logits; chunk: two half steps' constants.  A thread has no
+// room for 128 logits: the quarters are looked at in the order 2, 3, 0, 1 for the maximum, so that the first two are still there when
+// their exponentials come, and the last two are fetched again.
 template <typename Rescale, typename HalfDone>
 __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* const (&chunk)[2], bool missing, int key0, int limit, float c,
                                                  float& m, float& l, Rescale rescale, HalfDone half_done) {
@@ -746,11 +746,12 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
     }
     float top = -INFINITY;
     uint32_t sr[2][32];
-    tmem_ld32(s_addr, sr[0]);
+    tmem_ld32(s_addr + 64u, sr[0]);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int u = 0; u < 4; ++u) {
+        const int q = (u + 2) & 3;
         tc_wait_ld();
-        tmem_ld32(s_addr + (uint32_t)(32 * ((q + 1) & 3)), sr[(q + 1) & 1]);      // (after the last quarter the first again, for its exponentials)
+        if (u < 3) tmem_ld32(s_addr + (uint32_t)(32 * ((q + 1) & 3)), sr[(q + 1) & 1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const float2 k2 = *reinterpret_cast<const float2*>(chunk[q >> 1] + 2 * (q & 1) + i);
@@ -771,8 +772,8 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
     float sum = 0.f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        tc_wait_ld();
-        if (q < 3) tmem_ld32(s_addr + (uint32_t)(32 * (q + 1)), sr[(q + 1) & 1]);
+        if (q >= 2) tc_wait_ld();
+        if (q == 2) tmem_ld32(s_addr + 96u, sr[1]);
         uint32_t pr[16];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -790,7 +791,8 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
             const uint64_t both = fadd2(acc[0], acc[1]);
             sum = fmaf(f32x2_lo(both) + f32x2_hi(both), k4.z, sum);
         }
-        // a quarter of P takes 16 columns, over logits that have been fetched (the next quarter's are on their way: columns further up)
+        if (q == 0) tmem_ld32(s_addr + 64u, sr[0]);
+        // a quarter of P takes 16 columns, over logits that have been fetched (or are on their way: columns further up)
         tmem_st16(s_addr + (uint32_t)(16 * q), pr);
         if (q & 1) half_done(q >> 1);
     }
@@ -1466,14 +1468,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// K or V of one layer of the pool as rows of 128 bytes, in boxes of `box_rows` rows with the 128-byte swizzle.  Each host thread
-// keeps the maps it encoded last, keyed by everything that goes into them.
+// K or V of one layer of the pool as rows of 128 bytes, in boxes of `box_rows` rows with the 128-byte swizzle.
 static int make_pool_map(CUtensorMap* m, const void* base, long long rows, int box_rows) {
-    struct Slot { const void* base; long long rows; int box; CUtensorMap map; };
-    static thread_local std::vector<Slot> cache;
-    if (cache.empty()) cache.resize(256, Slot{nullptr, 0, 0, {}});
-    Slot& slot = cache[((reinterpret_cast<uintptr_t>(base) >> 8) * 1000003u + (size_t)rows * 31u + (size_t)box_rows) % 256];
-    if (slot.base == base && slot.rows == rows && slot.box == box_rows) { *m = slot.map; return DAF_OK; }
     static std::atomic<EncodeTiledFn> encode{nullptr};
     EncodeTiledFn fn = encode.load(std::memory_order_acquire);
     if (fn == nullptr) {
@@ -1495,7 +1491,6 @@ static int make_pool_map(CUtensorMap* m, const void* base, long long rows, int b
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) { set_cuda_error(cudaErrorInvalidValue); return DAF_ERR_CUDA; }
-    slot = Slot{base, rows, box_rows, *m};
     return DAF_OK;
 }
 
