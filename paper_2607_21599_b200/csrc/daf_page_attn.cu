@@ -685,11 +685,11 @@ struct QuestionSmem {
     uint64_t c_full[kQConsts];
     float4 chunk[kQConsts][4];      // of half a step's chunks of 16 keys: ks (negative: no page), floor(log2 vs), 2^-that, vs / 2^that
     int missing[kQConsts];          // some keys of the half step have no page
-    float2 ml[128];                 // the second group's row maxima and sums (blocks of one tile)
+    float2 ml[2][128];              // [group] row maxima and sums (blocks of one tile)
     uint32_t tmem_base;
     int abort_flag;
     unsigned long long odd;         // which barriers have completed an odd number of phases
-    int go[2][2];                   // [K, V][half step mod 2] what the polling warp found
+    int go[2][2][2];                // [K, V][half step mod 2][step mod 2] what the polling warp found
     int poison;                     // a NaN was taken out of a value that some rows must not see
     // The piece of work under way and the CTA's stretch: kept here rather than in every thread's registers
     Place at;
@@ -700,7 +700,7 @@ struct QuestionSmem {
 };
 constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK = (int)(offsetof(QuestionSmem, k_full) / 8),
               kBarKEmpty = (int)(offsetof(QuestionSmem, k_empty) / 8), kBarV = (int)(offsetof(QuestionSmem, v_full) / 8),
-              kBarVEmpty = (int)(offsetof(QuestionSmem, v_empty) / 8), kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
+              kBarQ = (int)(offsetof(QuestionSmem, q_full) / 8),
               kBarS = (int)(offsetof(QuestionSmem, s_full) / 8), kBarP = (int)(offsetof(QuestionSmem, p_full) / 8),
               kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarTurn = (int)(offsetof(QuestionSmem, turn) / 8),
               kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
@@ -720,6 +720,14 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "r"(taddr)
         : "memory");
 }
+
+// Bytes from shared to global memory, both 16-byte aligned and a multiple of 16 of them; and the wait of the thread that asked until
+// they are written.
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)), "r"(smem_u32(src)), "r"(bytes) : "memory");
+    tma_store_commit();
+}
+__device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // One softmax step of one row over 128 keys: P over the first half of the logits' columns, running maximum and sum.  `rescale` is called
 // ahead of the first P with the factor for the row of O (1 unless the maximum grew by more than kLazy), `half_done` when half of P is
@@ -865,10 +873,10 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     if (warp == 1) {
         uint64_t* const bars = reinterpret_cast<uint64_t*>(sm);
         for (int i = lane; i < kBars; i += 32) {
-            // four warps (or lanes) arrive, or both groups' products, or one copy's bytes or product
-            const bool by_four = (i >= kBarStEmpty && i < kBarK) || (i >= kBarV && i < kBarVEmpty) || (i >= kBarQ && i < kBarS) || (i >= kBarP && i < kBarO) || i >= kBarC;
-            const bool by_two = (i >= kBarKEmpty && i < kBarV) || (i >= kBarVEmpty && i < kBarQ);
-            mbar_init(bars + i, i >= kBarK && i < kBarKEmpty ? 8 : by_four ? 4 : by_two ? 2 : 1);      // (K: four warps, two half steps)
+            // four warps (or lanes) arrive, or two warps, or both groups' products, or one copy's bytes or product
+            const bool by_four = (i >= kBarK && i < kBarKEmpty) || (i >= kBarQ && i < kBarS) || (i >= kBarP && i < kBarO) || i >= kBarC;
+            const bool by_two = (i >= kBarStEmpty && i < kBarK) || (i >= kBarKEmpty && i < kBarQ);
+            mbar_init(bars + i, by_four ? 4 : by_two ? 2 : 1);
         }
         mbar_fence_init();
     }
@@ -943,14 +951,14 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             // ------------------------------------------------------------------------------------- softmax, a row per thread
             const int g = warp >> 2, rt = threadIdx.x & 127;
             const int tile_row = sm->at.block * kQRows + (pair ? g * 128 : 0), row = tile_row + rt;
-            const bool valid = row < a.rows;
+            const bool valid = row < a.rows, any_valid = (row & ~31) < a.rows;      // (a warp's rows: 32 from a multiple of 32)
             const int tok = row / a.G, head = row - tok * a.G;          // (head of the group)
             const int limit = valid ? sm->at.len - a.L_q + tok : sm->last_limit;
             const int n_u = pair ? n_t : (n_t - g + 1) >> 1;
             const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
             const uint32_t o_addr = tmem + (uint32_t)(g * 256) + lane_addr, s_addr = o_addr + kColS;
-            float c;
-            {
+            float c = 0.f;
+            if (any_valid) {
                 // The warp's 32 rows of Q: raw into what will be K's buffers, sixteen lanes a row, pieces of 16 bytes XOR-ed with the row
                 // number.  Each thread then scales its own row to a largest magnitude of 2^14 .. 2^15 and writes it as fp16 in the layout of
                 // a tiled copy.  (Both groups of a block of one tile load the same rows; only the first writes them.)
@@ -997,152 +1005,166 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     }
                     fence_proxy_async();
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm->q_full[g]);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm->q_full[g]);
             float m = -INFINITY, l = 0.f;
-            for (int u = 0; u < n_u; ++u) {
-                const int t = pair ? u : 2 * u + g, c0 = (2 * t) % kQConsts;
-                ok = wait_phase(sm, odd, &sm->c_full[c0], (uint32_t)((2 * t / kQConsts) & 1), abort, 271);
-                if (ok) ok = wait_phase(sm, odd, &sm->c_full[c0 + 1], (uint32_t)((2 * t / kQConsts) & 1), abort, 273);
-                if (ok) ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                const float4* const chunk[2] = {sm->chunk[c0], sm->chunk[c0 + 1]};
-                auto rescale = [&](float alpha) {
-                    // The groups take turns (a scheduler's two warps, one of each): left to themselves they fall into step, wait for the
-                    // exponentials together (16 a clock) and then for their products together.
-                    if (ok && pair && (g == 1 || u > 0)) ok = wait_phase(sm, odd, &sm->turn[g][warp & 3], (uint32_t)((g == 1 ? u : u - 1) & 1), abort, 279);
-                    // (the logits came behind the product before, so O is quiet)
-                    if (u == 0 || !__any_sync(0xFFFFFFFFu, alpha != 1.f)) return;
+            int u = 0;
+            auto take_turn = [&]() {
+                // The groups take turns (a scheduler's two warps, one of each): left to themselves they fall into step, wait for the
+                // exponentials together (16 a clock) and then for their products together.
+                if (ok && pair && (g == 1 || u > 0)) ok = wait_phase(sm, odd, &sm->turn[g][warp & 3], (uint32_t)((g == 1 ? u : u - 1) & 1), abort, 279);
+            };
+            auto half_done = [&](int half) {
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm->p_full[g][half]);
+            };
+            if (any_valid) {
+                for (; u < n_u; ++u) {
+                    const int t = pair ? u : 2 * u + g, c0 = (2 * t) % kQConsts;
+                    ok = wait_phase(sm, odd, &sm->c_full[c0], (uint32_t)((2 * t / kQConsts) & 1), abort, 271);
+                    if (ok) ok = wait_phase(sm, odd, &sm->c_full[c0 + 1], (uint32_t)((2 * t / kQConsts) & 1), abort, 273);
+                    if (ok) ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const float4* const chunk[2] = {sm->chunk[c0], sm->chunk[c0 + 1]};
+                    auto rescale = [&](float alpha) {
+                        take_turn();
+                        // (the logits came behind the product before, so O is quiet)
+                        if (u == 0 || !__any_sync(0xFFFFFFFFu, alpha != 1.f)) return;
 #pragma unroll 1
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t r[16];
-                        tmem_ld16(o_addr + (uint32_t)(16 * i), r);
-                        tc_wait_ld();
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t r[16];
+                            tmem_ld16(o_addr + (uint32_t)(16 * i), r);
+                            tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
-                        tmem_st16(o_addr + (uint32_t)(16 * i), r);
-                    }
-                };
-                auto half_done = [&](int half) {
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm->p_full[g][half]);
-                };
-                question_softmax(s_addr, chunk, (sm->missing[c0] | sm->missing[c0 + 1]) != 0, (step0 + t) * kQStep, limit, c, m, l, rescale, half_done);
-                if (pair && lane == 0) mbar_arrive(&sm->turn[1 - g][warp & 3]);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
+                            for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
+                            tmem_st16(o_addr + (uint32_t)(16 * i), r);
+                        }
+                    };
+                    question_softmax(s_addr, chunk, (sm->missing[c0] | sm->missing[c0 + 1]) != 0, (step0 + t) * kQStep, limit, c, m, l, rescale, half_done);
+                    if (pair && lane == 0) mbar_arrive(&sm->turn[1 - g][warp & 3]);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                }
+            } else {
+                // no rows of this warp's: whatever lies in its lanes of tensor memory stays among them
+                for (; u < n_u; ++u) {
+                    ok = wait_phase(sm, odd, &sm->s_full[g], (uint32_t)(u & 1), abort, 272);
+                    take_turn();
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    half_done(0);
+                    half_done(1);
+                    if (pair && lane == 0) mbar_arrive(&sm->turn[1 - g][warp & 3]);
+                }
             }
             if (ok && n_u > 0) ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->o_full[g], 0, abort, 274));
             tc_fence_after();
-            // ---- epilogue, through Q's tiles and K's buffers once both groups are done with them.  A block of one tile: the second group hands its rows to
-            // the first.
-            float w0 = 1.f, w1 = 0.f;
-            float* const other = reinterpret_cast<float*>(smem) + rt * kD;
-            static_assert(2 * kQTile >= 128 * kD * (int)sizeof(float) && 2 * kQTile >= 8 * 8192, "a tile of fp32 rows, and 8 KB a warp");
+            // ---- epilogue: rows leave through shared memory, once both groups are done with all in front of the stages, and one bulk copy a
+            // row.  A block of one tile: each group merges half of the channels, and hands the other half of its own to the other.
+            float w_own = 1.f, w_other = 0.f;
+            float* const given = reinterpret_cast<float*>(smem) + (1 - g) * (128 * 64) + rt * 64;      // to the other group: [128 rows][64 channels]
+            const float* const taken = reinterpret_cast<const float*>(smem) + g * (128 * 64) + rt * 64;
             asm volatile("bar.sync 1, 256;" ::: "memory");
             if (!pair) {
-                if (g == 1 && ok) {
+                if (ok && any_valid) {
 #pragma unroll 1
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t r[16];
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t r[32];
                         if (n_u > 0) {
-                            tmem_ld16(o_addr + (uint32_t)(16 * i), r);
+                            tmem_ld32(o_addr + (uint32_t)(64 * (1 - g) + 32 * i), r);
                             tc_wait_ld();
                         }
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4)
-                            *reinterpret_cast<float4*>(other + (((4 * i + j / 4) ^ lane) << 2)) =
+                        for (int j = 0; j < 32; j += 4)
+                            *reinterpret_cast<float4*>(given + (((8 * i + j / 4) ^ (lane & 15)) << 2)) =
                                 n_u > 0 ? make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]))
                                         : make_float4(0.f, 0.f, 0.f, 0.f);
                     }
-                    sm->ml[rt] = make_float2(m, l);
+                    sm->ml[g][rt] = make_float2(m, l);
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (g == 0) {
-                    const float2 ml = sm->ml[rt];
+                if (any_valid) {
+                    const float2 ml = sm->ml[1 - g][rt];
                     const float mx = fmaxf(m, ml.x);
-                    w0 = partial_weight(make_float2(m, l), mx);
-                    w1 = partial_weight(ml, mx);
+                    w_own = partial_weight(make_float2(m, l), mx);
+                    w_other = partial_weight(ml, mx);
                     m = mx;
-                    l = w0 * l + w1 * ml.y;
+                    l = w_own * l + w_other * ml.y;
                 }
             }
-            if (ok && (pair || g == 0)) {      // (whole warps: the reads of tensor memory are theirs)
+            if (ok && any_valid) {      // (whole warps: the reads of tensor memory are theirs)
                 const Place at = sm->at;
                 const bool begins = step0 == 0, whole = begins && sm->step1 == at.n_steps;
                 const float inv = row_inverse(l);
-                // 256 bytes of each of the warp's 32 rows at a time (a whole bf16 row, or half of an fp32 one), 16-byte pieces XOR-ed with the
-                // row number, and out again with sixteen lanes a row.
-                unsigned char* const stage = k_smem + warp * 8192;
-                const size_t out_row = ((size_t)at.b * a.L_q + tok) * a.Hq + at.h * a.G + head;
-                const size_t set_row = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
-                const unsigned long long dst = reinterpret_cast<unsigned long long>(whole ? reinterpret_cast<char*>(a.out) + out_row * (kD * 2)
-                                                                                          : reinterpret_cast<char*>(a.part_o) + set_row * (kD * 4));
-                const unsigned rows_there = __ballot_sync(0xFFFFFFFFu, valid);
-                const bool poisoned = sm->poison != 0;
-                for (int pass = 0; pass < (whole ? 1 : 2); ++pass) {
+                const int c0 = pair ? 0 : 64 * g, width = pair ? kD : 64;          // this thread's channels
+                // a row's bytes lie together, rows an odd number of 16 bytes apart
+                unsigned char* const mine = pair ? smem + (g * 128 + rt) * (kD * 4 + 16) : smem + 2 * kQTile + (g * 128 + rt) * (64 * 4 + 16);
+                static_assert(256 * (kD * 4 + 16) <= kQOffStage && 2 * kQTile + 256 * (64 * 4 + 16) <= kQOffStage, "the rows fit in front of the stages");
 #pragma unroll 1
-                    for (int i = 0; i < (whole ? 8 : 4); ++i) {
-                        const int c16 = pass * 4 + i;      // 16 channels
-                        uint32_t r[16];
-                        float o[16];
-                        if (n_u > 0) {
-                            tmem_ld16(o_addr + (uint32_t)(16 * c16), r);
-                            tc_wait_ld();
-                        }
+                for (int i = 0; i < width / 32; ++i) {
+                    uint32_t r[32];
+                    if (n_u > 0) {
+                        tmem_ld32(o_addr + (uint32_t)(c0 + 32 * i), r);
+                        tc_wait_ld();
+                    } else {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) o[j] = n_u > 0 ? __uint_as_float(r[j]) : 0.f;
-                        if (!pair) {
+                        for (int j = 0; j < 32; ++j) r[j] = 0u;
+                    }
+                    if (!pair) {
 #pragma unroll
-                            for (int j = 0; j < 16; j += 4) {
-                                const float4 y = *reinterpret_cast<const float4*>(other + (((4 * c16 + j / 4) ^ lane) << 2));
-                                o[j] = w0 * o[j] + w1 * y.x; o[j + 1] = w0 * o[j + 1] + w1 * y.y;
-                                o[j + 2] = w0 * o[j + 2] + w1 * y.z; o[j + 3] = w0 * o[j + 3] + w1 * y.w;
-                            }
-                        }
-                        if (poisoned && valid) {
-                            // values that were NaN, in keys that this row sees and the block's first does not
-                            const int from = max(sm->first_limit + 1, step0 * kQStep), to = min(min(limit, at.len - 1), (step0 + n_t) * kQStep - 1);
-                            for (int key = from; key <= to; ++key) {
-                                const int id = __ldg(a.table + (size_t)at.seq * a.p.max_pages + key / T);
-                                if ((unsigned)id >= (unsigned)a.p.n_pages) continue;
-                                const uint8_t* const v = a.p.v8 + (((size_t)id * Hkv + at.h) * T + key % T) * kD + 16 * c16;
-#pragma unroll
-                                for (int j = 0; j < 16; ++j)
-                                    if ((__ldg(v + j) & 0x7F) == 0x7F) o[j] = __int_as_float(0x7FC00000);
-                            }
-                        }
-                        unsigned char* const mine = stage + lane * 256;
-                        if (whole) {
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                *reinterpret_cast<uint4*>(mine + (((2 * i + j) ^ (lane & 15)) << 4)) =
-                                    make_uint4(pack_bf16(o[8 * j] * inv, o[8 * j + 1] * inv), pack_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
-                                               pack_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv), pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                *reinterpret_cast<float4*>(mine + (((4 * i + j) ^ (lane & 15)) << 4)) = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 y = *reinterpret_cast<const float4*>(taken + (((8 * i + j / 4) ^ (lane & 15)) << 2));
+                            r[j] = __float_as_uint(w_own * __uint_as_float(r[j]) + w_other * y.x);
+                            r[j + 1] = __float_as_uint(w_own * __uint_as_float(r[j + 1]) + w_other * y.y);
+                            r[j + 2] = __float_as_uint(w_own * __uint_as_float(r[j + 2]) + w_other * y.z);
+                            r[j + 3] = __float_as_uint(w_own * __uint_as_float(r[j + 3]) + w_other * y.w);
                         }
                     }
-                    __syncwarp();
-#pragma unroll 4
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = 2 * i + (lane >> 4), p = lane & 15;
-                        const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 256 + ((p ^ (r & 15)) << 4));
-                        char* const to = reinterpret_cast<char*>(__shfl_sync(0xFFFFFFFFu, dst, r)) + pass * 256 + p * 16;
-                        if ((rows_there >> r) & 1u) *reinterpret_cast<uint4*>(to) = v;
+                    if (whole) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) y[k] = pack_bf16(__uint_as_float(r[j + 2 * k]) * inv, __uint_as_float(r[j + 2 * k + 1]) * inv);
+                            *reinterpret_cast<uint4*>(mine + i * 64 + j * 2) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) *reinterpret_cast<uint4*>(mine + i * 128 + j * 4) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
                     }
-                    __syncwarp();
                 }
                 if (valid) {
-                    if (!whole) a.part_ml[set_row] = make_float2(m, l);
-                    else if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + at.h * a.G + head) * a.L_q + tok] = row_lse(m, l);
+                    if (sm->poison != 0) {
+                        // values that were NaN, in keys that this row sees and the block's first does not
+                        const int from = max(sm->first_limit + 1, step0 * kQStep), to = min(min(limit, at.len - 1), (step0 + n_t) * kQStep - 1);
+#pragma unroll 1
+                        for (int key = from; key <= to; ++key) {
+                            const int id = __ldg(a.table + (size_t)at.seq * a.p.max_pages + key / T);
+                            if ((unsigned)id >= (unsigned)a.p.n_pages) continue;
+                            const uint8_t* const v = a.p.v8 + (((size_t)id * Hkv + at.h) * T + key % T) * kD + c0;
+#pragma unroll 1
+                            for (int j = 0; j < width; ++j) {
+                                if ((__ldg(v + j) & 0x7F) != 0x7F) continue;
+                                if (whole) reinterpret_cast<uint16_t*>(mine)[j] = 0x7FC0;
+                                else reinterpret_cast<float*>(mine)[j] = __int_as_float(0x7FC00000);
+                            }
+                        }
+                    }
+                    const size_t out_row = ((size_t)at.b * a.L_q + tok) * a.Hq + at.h * a.G + head;
+                    const size_t set_row = ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * kQRows + (row - at.block * kQRows);
+                    fence_proxy_async();
+                    if (whole) bulk_store(a.out + out_row * kD + c0, mine, (uint32_t)width * 2);
+                    else bulk_store(a.part_o + set_row * kD + c0, mine, (uint32_t)width * 4);
+                    if (pair || g == 0) {
+                        if (!whole) a.part_ml[set_row] = make_float2(m, l);
+                        else if (a.lse != nullptr) a.lse[((size_t)at.b * a.Hq + at.h * a.G + head) * a.L_q + tok] = row_lse(m, l);
+                    }
+                    tma_store_wait_read();
                 }
             }
             tc_fence_before();
@@ -1150,6 +1172,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             tc_fence_after();
             if (sm->abort_flag != 0) break;
         }
+        bulk_store_wait();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         for (;;) {
@@ -1217,44 +1240,48 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[kv][i], 0) && !mbar_try_wait(&sm->st_full[kv][i], 1); ++k) {}
             } else if (warp >= 12) {
                 // --------------------------------------------------------------------------------------------------- widening
-                // A lane takes 16 bytes of a row at a time.  Eight lanes take four neighbouring pieces of each of two rows r and r ^ 5:
-                // with the swizzle of either side their reads and their writes all fall into different banks.
-                const int cw = warp & 3;
+                // Two warps take a half step, the other two the next one: each half step is a chain of waits, reads, conversions, writes and
+                // a fence of some 2500 clocks, most of it latency, and so two are under way.  A lane takes 16 bytes of a row at a time.
+                // Eight lanes take four neighbouring pieces of each of two rows r and r ^ 5: with the swizzle of either side their reads and
+                // their writes all fall into different banks.
+                const int turn = (warp >> 1) & 1, row0 = (warp & 1) * 32;
                 const int first_limit = sm->first_limit, len = sm->at.len;
                 const int r8 = (lane >> 3) ^ ((lane >> 2) & 1 ? 5 : 0), piece = lane & 3;
                 const int kv = warp >= 16;
-                for (int t = 0; t < 2 * n_t; ++t) {      // (t counts half steps here)
+                for (int t = turn; t < 2 * n_t; t += 2) {      // (t counts half steps here)
                     // K: half of the buffer of its step; V: a slot
                     const int step = t >> 1, slot = kv == 0 ? step & 1 : pair ? t & 1 : t & 3, uses = kv == 0 || !pair ? step >> 1 : step;
-                    // one of the four warps polls, the others sleep at a barrier (twelve polling warps took half of the issue slots)
-                    if (cw == 0) {
+                    // one of the two warps polls, the other sleeps at a barrier (twelve polling warps took half of the issue slots)
+                    if ((warp & 1) == 0) {
                         bool there = wait_phase(sm, odd, &sm->st_full[kv][t % kQStages], (uint32_t)((t / kQStages) & 1), abort, 262);
                         if (kv == 1 && there) there = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 275);
-                        if (there && t == 0 && (kv == 0 || !pair)) {      // the raw rows of Q are out of K's buffers, the second tile is idle
+                        if (there && step == 0 && (kv == 0 || !pair)) {      // the raw rows of Q are out of K's buffers, the second tile is idle
                             there = wait_phase(sm, odd, &sm->q_full[0], 0, abort, 276);
                             if (there) there = wait_phase(sm, odd, &sm->q_full[1], 0, abort, 277);
                         }
                         if (there && uses > 0) there = wait_phase(sm, odd, kv == 0 ? &sm->k_empty[slot] : &sm->v_empty[slot], (uint32_t)((uses - 1) & 1), abort, 263);
                         there = __all_sync(0xFFFFFFFFu, there);
-                        if (lane == 0) sm->go[kv][t & 1] = there;
+                        if (lane == 0) sm->go[kv][turn][step & 1] = there;
                     }
-                    asm volatile("bar.sync %0, 128;" ::"r"(2 + kv) : "memory");
-                    if (!sm->go[kv][t & 1]) break;
-                    unsigned char* const src = stage_smem + (kv * kQStages + t % kQStages) * kQStage + (16 * cw + r8) * kD;
-                    float vm = 1.f;
+                    asm volatile("bar.sync %0, 64;" ::"r"(2 + 2 * kv + turn) : "memory");
+                    if (!sm->go[kv][turn][step & 1]) break;
+                    unsigned char* const src = stage_smem + (kv * kQStages + t % kQStages) * kQStage + (row0 + r8) * kD;
+                    const int half_at = kv == 0 ? kQHalf : kQSlotHalf;          // between the two 64-column halves
+                    unsigned char* const dst = smem + (kv == 0 ? kQOffK + slot * kQTile + (t & 1) * (kQSub * 128) : v_slot(slot)) + (row0 + r8) * 128;
+                    float vm[2] = {1.f, 1.f};
                     if (kv == 1) {
-                        const float4 sc = sm->chunk[t % kQConsts][cw];
                         const int key0 = step0 * kQStep + t * kQSub;
-                        vm = sc.w;
-                        if (key0 + kQSub - 1 > first_limit || sc.x < 0.f) {
+                        const float4 sc0 = sm->chunk[t % kQConsts][row0 / 16], sc1 = sm->chunk[t % kQConsts][row0 / 16 + 1];
+                        vm[0] = sc0.w; vm[1] = sc1.w;
+                        if (key0 + kQSub - 1 > first_limit || sc0.x < 0.f || sc1.x < 0.f) {
                             // As in the kernel above: keys that no row of the sequence sees, or of no page, count as zero; a NaN in
                             // a key that only some rows see is taken out, and put into the rows that see it at the end.
 #pragma unroll 1
-                            for (int i = 0; i < 4; ++i) {
-                                const int key = key0 + 16 * cw + 8 * (i >> 1) + r8;
+                            for (int i = 0; i < 8; ++i) {
+                                const int key = key0 + row0 + 8 * (i >> 1) + r8;
                                 uint4* const at = reinterpret_cast<uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
                                 uint4 w = *at;
-                                if (key >= len || sc.x < 0.f) w = make_uint4(0u, 0u, 0u, 0u);
+                                if (key >= len || (i < 4 ? sc0.x : sc1.x) < 0.f) w = make_uint4(0u, 0u, 0u, 0u);
                                 else if (key > first_limit) {
                                     const uint4 nan = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
                                     if ((nan.x | nan.y | nan.z | nan.w) != 0u) sm->poison = 1;
@@ -1264,23 +1291,21 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                             }
                         }
                     }
-                    const int half_at = kv == 0 ? kQHalf : kQSlotHalf;          // between the two 64-column halves
-                    unsigned char* const dst = smem + (kv == 0 ? kQOffK + slot * kQTile + (t & 1) * (kQSub * 128) : v_slot(slot)) + (16 * cw + r8) * 128;
-                    uint4 w[4];
+                    uint4 w[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)      // pieces (i & 1) * 4 .. of rows 16 cw + 8 (i >> 1) ..
+                    for (int i = 0; i < 8; ++i)      // pieces (i & 1) * 4 .. of rows row0 + 8 (i >> 1) ..
                         w[i] = *reinterpret_cast<const uint4*>(src + 8 * (i >> 1) * kD + (((4 * (i & 1) + piece) ^ r8) << 4));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 8; ++i) {
                         unsigned char* const row = dst + (i & 1) * half_at + 8 * (i >> 1) * 128;
                         *reinterpret_cast<uint4*>(row + (((2 * piece) ^ r8) << 4)) = make_uint4(widen2(w[i].x), widen2(w[i].x >> 16), widen2(w[i].y), widen2(w[i].y >> 16));
                         *reinterpret_cast<uint4*>(row + (((2 * piece + 1) ^ r8) << 4)) = make_uint4(widen2(w[i].z), widen2(w[i].z >> 16), widen2(w[i].w), widen2(w[i].w >> 16));
                     }
-                    if (vm != 1.f) {       // what V's scale is beside a power of two (nothing, as daf_page_write leaves them): each lane its own pieces
-                        const __half2 f = __float2half2_rn(vm);
+                    if (vm[0] != 1.f || vm[1] != 1.f) {       // what V's scale is beside a power of two (nothing, as daf_page_write leaves them): each lane its own pieces
 #pragma unroll 1
-                        for (int i = 0; i < 8; ++i) {
-                            __half2* const h = reinterpret_cast<__half2*>(dst + (i & 1) * kQSlotHalf + 8 * ((i >> 1) & 1) * 128 + (((2 * piece + (i >> 2)) ^ r8) << 4));
+                        for (int i = 0; i < 16; ++i) {
+                            const __half2 f = __float2half2_rn(i < 8 ? vm[0] : vm[1]);
+                            __half2* const h = reinterpret_cast<__half2*>(dst + (i & 1) * kQSlotHalf + 8 * (2 * (i >> 3) + ((i >> 1) & 1)) * 128 + (((2 * piece + ((i >> 2) & 1)) ^ r8) << 4));
 #pragma unroll
                             for (int j = 0; j < 4; ++j) h[j] = __hmul2(h[j], f);
                         }
