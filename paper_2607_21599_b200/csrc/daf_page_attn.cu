@@ -1408,16 +1408,19 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
     constexpr int kRows = 8 / kWarps, kAtOnce = kWarps == 1 ? 8 : 5;
     __shared__ float4 acc_s[8][32];
     __shared__ float sum_s[8];
-    __shared__ int begin_cta[256], counts[8];
+    __shared__ int begin_cta[kWarps == 1 ? 256 : 1], counts[8];
+    __shared__ ChainEntry begin_chain[kWarps == 1 ? 256 : 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
     pdl_wait();
     pdl_launch_dependents();
     // Few rows: a block per CTA and row.  Many: the CTAs that begin such a segment, in order, so that every block numbers them alike
     // (at most 256, a thread each), since most blocks of a full grid would only find that there is nothing to do.
-    const int groups = (block_rows + kRows - 1) / kRows;
+    const int groups = (min(block_rows, a.rows) + kRows - 1) / kRows;
     int n_begin = 1;
     if (kWarps == 1) {
-        const bool begins = (int)threadIdx.x < ctas && a.chains[threadIdx.x].last_cta >= 0;
+        ChainEntry mine = {-1, 0, 0, 0};
+        if ((int)threadIdx.x < ctas) mine = a.chains[threadIdx.x];
+        const bool begins = mine.last_cta >= 0;
         const unsigned some = __ballot_sync(0xFFFFFFFFu, begins);
         if (lane == 0) counts[warp] = __popc(some);
         __syncthreads();
@@ -1428,12 +1431,15 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
             if (w < warp) before += counts[w];
             n_begin += counts[w];
         }
-        if (begins) begin_cta[before] = (int)threadIdx.x;
+        if (begins) {
+            begin_cta[before] = (int)threadIdx.x;
+            begin_chain[before] = mine;
+        }
         __syncthreads();
     }
     for (int item = kWarps == 1 ? blockIdx.x : blockIdx.y; item < n_begin * groups; item += kWarps == 1 ? gridDim.x : gridDim.y) {
         const int first = kWarps == 1 ? begin_cta[item / groups] : blockIdx.x, r = (item % groups) * kRows + warp / kWarps;
-        const ChainEntry e = a.chains[first];
+        const ChainEntry e = kWarps == 1 ? begin_chain[item / groups] : a.chains[first];
         if (kWarps > 1 && e.last_cta < 0) return;
         const int row = e.block * block_rows + r;
         const bool there = r < block_rows && row < a.rows;
