@@ -1400,24 +1400,24 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     }
 }
 
-// Merge of the segments that lie in several CTAs: kWarps warps per row of a segment that CTA blockIdx.x begins.  Bound by the trips
-// to L2, so a warp asks for its first kAtOnce partials together with the row's maxima: few rows with many partials (one answer over a
-// long context: 37) take eight warps a row, many rows with few partials one.
-template <int kWarps>
+// Merge of the segments that lie in several CTAs: kWarps warps per row of such a segment.  Bound by the trips to L2, so a warp asks for
+// its first kAtOnce partials together with the row's maxima.  kMany: the blocks share the rows of all such segments; otherwise (few rows
+// a segment) blockIdx is the CTA that begins it and a row.
+template <int kWarps, bool kMany>
 __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, int block_rows, int ctas) {
-    constexpr int kRows = 8 / kWarps, kAtOnce = kWarps == 1 ? 8 : 5;
+    constexpr int kRows = 8 / kWarps, kAtOnce = kWarps == 1 ? 8 : kWarps == 4 ? 10 : 5;
     __shared__ float4 acc_s[8][32];
     __shared__ float sum_s[8];
-    __shared__ int begin_cta[kWarps == 1 ? 256 : 1], counts[8];
-    __shared__ ChainEntry begin_chain[kWarps == 1 ? 256 : 1];
+    __shared__ int begin_cta[kMany ? 256 : 1], counts[8];
+    __shared__ ChainEntry begin_chain[kMany ? 256 : 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
     pdl_wait();
     pdl_launch_dependents();
-    // Few rows: a block per CTA and row.  Many: the CTAs that begin such a segment, in order, so that every block numbers them alike
-    // (at most 256, a thread each), since most blocks of a full grid would only find that there is nothing to do.
+    // kMany: the CTAs that begin such a segment, in order, so that every block numbers them alike (at most 256, a thread each), since
+    // most blocks of a full grid would only find that there is nothing to do.
     const int groups = (min(block_rows, a.rows) + kRows - 1) / kRows;
     int n_begin = 1;
-    if (kWarps == 1) {
+    if (kMany) {
         ChainEntry mine = {-1, 0, 0, 0};
         if ((int)threadIdx.x < ctas) mine = a.chains[threadIdx.x];
         const bool begins = mine.last_cta >= 0;
@@ -1437,10 +1437,10 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
         }
         __syncthreads();
     }
-    for (int item = kWarps == 1 ? blockIdx.x : blockIdx.y; item < n_begin * groups; item += kWarps == 1 ? gridDim.x : gridDim.y) {
-        const int first = kWarps == 1 ? begin_cta[item / groups] : blockIdx.x, r = (item % groups) * kRows + warp / kWarps;
-        const ChainEntry e = kWarps == 1 ? begin_chain[item / groups] : a.chains[first];
-        if (kWarps > 1 && e.last_cta < 0) return;
+    for (int item = kMany ? blockIdx.x : blockIdx.y; item < n_begin * groups; item += kMany ? gridDim.x : gridDim.y) {
+        const int first = kMany ? begin_cta[item / groups] : blockIdx.x, r = (item % groups) * kRows + warp / kWarps;
+        const ChainEntry e = kMany ? begin_chain[item / groups] : a.chains[first];
+        if (!kMany && e.last_cta < 0) return;
         const int row = e.block * block_rows + r;
         const bool there = r < block_rows && row < a.rows;
         // partial i of the row: the first CTA's second set, then the following CTAs' first sets
@@ -1599,8 +1599,14 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     }
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
-    e = few ? launch_kernel(page_merge_kernel<8>, dim3(ctas, 8 * blocks), dim3(256), 0, stream, a, 8 * blocks, ctas)
-            : launch_kernel(page_merge_kernel<1>, dim3(3 * ctas), dim3(256), 0, stream, a, (int)kQRows, ctas);
+    // Few long segments leave many partials of a row: with four warps a row instead of one, 28 rows of 4 heads over 8k keys (37 partials)
+    // take 19.2 us instead of 31.5 with the attention itself, 132 rows of 8 heads over 16k (18) 38.2 instead of 41.8.  Where there are
+    // more rows than warps one is as good: 448 rows of 4 heads over 6k, 31.0 us against 32.3.
+    const long long heads = (long long)n * pool.Hkv, segments = heads * ((a.rows + kQRows - 1) / kQRows);
+    const bool four = ctas > 10 * segments && heads * a.rows <= 10 * ctas;
+    e = few ? launch_kernel(page_merge_kernel<8, false>, dim3(ctas, a.rows), dim3(256), 0, stream, a, 8 * blocks, ctas)
+      : four ? launch_kernel(page_merge_kernel<4, true>, dim3(3 * ctas), dim3(256), 0, stream, a, (int)kQRows, ctas)
+             : launch_kernel(page_merge_kernel<1, true>, dim3(3 * ctas), dim3(256), 0, stream, a, (int)kQRows, ctas);
     count_launch();
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
     return check_launch();
