@@ -47,6 +47,11 @@ struct ChainEntry {
 // copies into a ring of its own, whose 16-byte pieces are XOR-ed with the row number so that eight rows of a column lie in
 // different banks), multiplies, keeps the running maximum and sum, and multiplies again.  (Tiled copies were slower here: a warp has
 // to issue them one by one, with everything in uniform registers, and at pages of 16 tokens a step takes four: 1160 clocks a step.)
+//   Measured: one token of 64 sequences of 0.5k to 12k tokens, 32 / 8 heads, 145 us: 5.6 TB/s, 85 % of a copy's rate.  One token of 28 / 4
+// heads over 32k 14.8 us (5.2 at that rate) and over 1k 11.0: two launches and the chain lengths -> table -> bytes -> products -> merge,
+// of which every part runs once.  Two tokens (14 rows) of 16 sequences of 4k 27.8, three (21 rows) 37.9, one 20.5: each eight rows more
+// cost some 8 us of conversions and products in warps that are too few (two a scheduler) to cover their latencies; with 12 warps of
+// two column blocks 31.3, with 10 of three 53.7 (spills).
 //   8-bit values are exact in fp16, and so are the query rows once each is scaled by a power of two to a largest magnitude of
 //   2^14 .. 2^15 (elements 2^-31 of that and below are rounded), so the logits are products of the given numbers with fp32 sums.
 //   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
@@ -655,13 +660,19 @@ page_decode_kernel(const PageAttnArgs a) {
 //   0-3, 4-7  a tile group's softmax, a row per thread, and its epilogue.
 // A block of two tiles shares every widened K and V.  A block of one tile gives its even steps to one group and its odd ones to the
 // other, and the two halves of the result are merged in shared memory.  A group's 256 columns of tensor memory are O and S, 128
-// each.  One S is enough because the groups take turns: while one's products run, the other's softmax does.  (Steps of 64 keys with
-// two S a group: 114 us for 128 tokens of 28 / 4 heads over 32k keys, the products of both groups and the widening bound by shared
-// memory; with Q in tensor memory and one S: 110, the products' latency as long as a softmax step.)
+// each.  One S is enough because the groups take turns: while one's products run, the other's softmax does.
+//   Measured: 128 tokens of 28 / 4 heads over 32k keys 86.7 us, 694 TFLOP/s, 42 % of the measured bf16 rate; 4 tokens of 16 sequences of
+// 4k 40.4 (28 rows of a tile's 128), 64 tokens over 6k 31.0.  A step of both tiles takes some 5800 clocks, of which the tensor cores
+// are busy for 2050; the rest is each group's chain: exponentials 2000 (the unit needs 1024 of them), maximum 550, P on its way 350,
+// products 1500 to 1800.  Leaving the exponentials or three quarters of Q K^T out of the kernel changed nothing, leaving the widening out
+// a tenth.  A piece of work costs some 15,000 clocks beside its steps.  What was measured on the way, same case: steps of 64 keys
+// with two S a group 114 us; with Q in tensor memory and one S 110; without turns 104.
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 128, kQSub = 64;
 constexpr int kQStages = 3;        // half steps
-constexpr int kQPad = 12;          // places (a step of two tiles takes three) that a piece of work costs: rows of Q in, results out, some 18,000 clocks
+// Places (a step of two tiles takes three) that a piece of work costs: rows of Q in, results out.  128 tokens of 28 / 4 heads over 32k
+// keys with 6: 92 us, 8 and 10: 89, 12: 87.
+constexpr int kQPad = 12;
 constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
 constexpr int kQThreads = 640;
@@ -673,7 +684,7 @@ constexpr int kQStage = kQSub * kD;                   // 8 KB: the bytes of K or
 constexpr uint32_t kColS = 128;                       // columns of a group, behind O
 constexpr float kLazy = 6.f;                          // log2: a row's maximum may be this stale, P then reaches 2^(kPExp + kLazy)
 // Shared memory: Q's two tiles; V's two slots; K's two buffers.  A block of one tile has four slots of V, the last two in the second
-// tile of Q.  When a piece begins K's buffers hold the raw rows of Q, at its end they and Q's tiles what leaves the CTA.
+// tile of Q.  When a piece begins K's buffers hold the raw rows of Q, at its end all of this what leaves the CTA.
 constexpr int kQOffV = 2 * kQTile, kQOffK = kQOffV + 2 * kQSlot, kQOffStage = kQOffK + 2 * kQTile;
 
 struct QuestionSmem {
