@@ -508,6 +508,43 @@ def test_long_sequences(L, L_q, Hq, Hkv, T):
     assert (np.abs(got[0] - want) <= tol).all(), np.abs(got[0] - want).max()
 
 
+@pytest.mark.parametrize("L_q,Hq,Hkv", [(1, 256, 256), (26, 256, 256), (1, 256, 1), (3, 256, 1), (1, 200, 8), (2, 39, 3)])
+def test_head_counts_at_the_limits(L_q, Hq, Hkv):
+    lens = [70, 1, 200] if Hkv < 256 else [70, 33]
+    c = _cache_for(lens, 32, Hkv, seed=Hq + L_q, junk=False)
+    _attend(c, lens, L_q, Hq)
+
+
+def test_a_question_of_every_sequence_of_a_full_call():
+    n, L_q = 2048, 30
+    rng = random.Random(3)
+    lens = [rng.randint(0, 90) for _ in range(n)]
+    c = _cache_for(lens, 16, 1, seed=31, junk=False, scale_exps=(-8, -6))
+    q = torch.randn(n, L_q, 1, 128, generator=torch.Generator().manual_seed(9)).to(torch.bfloat16)
+    got, _ = _attend(c, lens, L_q, 1, q=q, check=False)
+    for b in range(0, n, 61):
+        sees = max(0, L_q - lens[b])                 # rows in front of the first that sees a key
+        assert not got[b, :sees].any()
+        if lens[b] == 0:
+            continue
+        want, mag, dots = (x.cpu().numpy()[sees:] for x in _torch_attend(c, lens[b], L_q, 1, q[b], seq=b))
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -16 * dots[..., None] + 2.0 ** -19) * mag * 1.01 + 2.0 ** -34 * 90 * 448 * 2.0 ** -6
+        assert (np.abs(got[b, sees:] - want) <= tol).all(), b
+
+
+@pytest.mark.parametrize("L_q", [1, 30])
+def test_a_sequence_of_millions_of_tokens(L_q):
+    L, T = 2_000_003, 128
+    c = _cache_for([L], T, 1, seed=7, junk=False, scale_exps=(-8, -6))
+    q = torch.randn(1, L_q, 1, 128, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    got, _ = _attend(c, [L], L_q, 1, q=q, check=False)
+    want, mag, dots = (x.cpu().numpy() for x in _torch_attend(c, L, L_q, 1, q[0]))
+    # fp32 sums: L / 148 keys, 16 at a time, one behind the other, and 148 partial ones (2^-24 of the running sum each)
+    sums = (L / 148 / 16 + 148) * 2.0 ** -24
+    tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -16 * dots[..., None] + 2.0 ** -19 + sums) * mag * 1.01 + 2.0 ** -34 * L * 448 * 2.0 ** -6
+    assert (np.abs(got[0] - want) <= tol).all(), np.abs(got[0] - want).max()
+
+
 @pytest.mark.parametrize("L_q", [1, 40])
 def test_pages_beyond_4_gb(L_q):
     """A layer of more than 2^32 bytes: the sequence's pages are the last ones."""
@@ -649,6 +686,15 @@ def test_large_pool_and_many_items():
     src = [rng.choice(full) for _ in empty]
     keep = [rng.randint(0, int((c.np["table"][s] >= 0).sum()) * 16) for s in src]
     assert _fork(c, src, empty, keep, [min(640, k + 40) for k in keep], True) == ""
+    _compact(c, in_place=False)
+
+
+@pytest.mark.parametrize("used", [0, 1, 4])
+def test_compact_of_an_empty_and_a_full_pool(used):
+    c = Cache(4, 16, 2, 2, 4, n_layers=2, seed=3, junk=False)
+    if used:
+        c.give(1, 16 * used)
+    _compact(c)
     _compact(c, in_place=False)
 
 
