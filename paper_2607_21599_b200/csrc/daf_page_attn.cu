@@ -129,9 +129,9 @@ __device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, int* 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int run = 0;
     for (int b0 = 0; b0 < a.n; b0 += kThreads) {
-        const int b = b0 + tid;
+        const int b = a.n <= 32 ? lane : b0 + tid;
         int x = b < a.n ? steps_of(seq_len(a, b), step) : 0;
-        if (blockIdx.x == 0 && b < a.n) {
+        if (blockIdx.x == 0 && b < a.n && b == b0 + tid) {
             const int len = __ldg(a.lens + b), seq = a.seqs != nullptr ? __ldg(a.seqs + b) : b;
             if ((unsigned)seq >= (unsigned)a.p.n_seqs || len != seq_len(a, b)) report_status(a.status, DAF_ERR_BOUNDS, 252, b);
         }
@@ -139,6 +139,10 @@ __device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, int* 
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
             if (lane >= o) x += y;
+        }
+        if (a.n <= 32) {                             // every warp knows all of it
+            if (warp == 0 && b < a.n) pre[b + 1] = x;
+            break;
         }
         if (lane == 31) warp_sums[warp] = x;
         __syncthreads();
@@ -175,10 +179,12 @@ __device__ __forceinline__ int cta_of(const Shares& s, long long at) {
 template <int kW>
 __device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* pre, Place& x) {
     x.step = 0;
-    x.width = min(kW, a.units - kW * ++x.block);
-    if (x.width > 0) return;
-    x.block = 0;
-    x.width = min(kW, a.units);
+    if (kW > 1) {
+        x.width = min(kW, a.units - kW * ++x.block);
+        if (x.width > 0) return;
+        x.block = 0;
+        x.width = min(kW, a.units);
+    }
     if (++x.h < a.p.Hkv) return;
     x.h = 0;
     ++x.b;
@@ -190,13 +196,15 @@ __device__ __forceinline__ void next_segment(const PageAttnArgs& a, const int* p
 // What a step costs: in blocks of up to two tiles (many rows), one tile takes 0.68 of the time of two.
 template <int kW>
 __device__ __forceinline__ int weight(int width) { return kW == 1 ? 1 : width + 1; }
-// Places that one (sequence, KV head) takes, and that sequences 0 .. b - 1 take.
+// Places that one (sequence, KV head) takes, and that sequences 0 .. b - 1 take.  (kW == 1, few rows: one tile, no pad.)
 template <int kW>
 __device__ __forceinline__ long long head_places(const PageAttnArgs& a, int n_steps) {
+    if (kW == 1) return n_steps;
     return (long long)n_steps * (a.units / kW * weight<kW>(kW) + (a.units % kW != 0 ? weight<kW>(1) : 0)) + (long long)a.pad * ((a.units + kW - 1) / kW);
 }
 template <int kW>
 __device__ __forceinline__ long long places_before(const PageAttnArgs& a, const int* pre, int b) {
+    if (kW == 1) return (long long)a.p.Hkv * pre[b];
     return a.p.Hkv * (head_places<kW>(a, pre[b]) + (long long)(b - 1) * a.pad * ((a.units + kW - 1) / kW));
 }
 // The first step that begins at or behind `at` (which is less than the total); a place in front of a segment's first step stands for it.
@@ -216,16 +224,23 @@ __device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre,
     const long long head = head_places<kW>(a, x.n_steps), block = (long long)weight<kW>(kW) * x.n_steps + a.pad;
     x.h = (int)axis_div(rest, head);
     rest -= x.h * head;
-    x.block = kW == 1 && a.units == 1 ? 0 : (int)axis_div(rest, block);
+    if (kW == 1) {
+        x.block = 0;
+        x.width = 1;
+        x.step = (int)rest;
+        return x;
+    }
+    x.block = (int)axis_div(rest, block);
     x.width = min(kW, a.units - kW * x.block);
     rest = max(rest - x.block * block - a.pad, 0ll);
-    x.step = kW == 1 ? (int)rest : (int)axis_div(rest + weight<kW>(x.width) - 1, weight<kW>(x.width));
+    x.step = (int)axis_div(rest + weight<kW>(x.width) - 1, weight<kW>(x.width));
     if (x.step == x.n_steps) next_segment<kW>(a, pre, x);
     return x;
 }
 // The last place that stands for a place's step.
 template <int kW>
 __device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* pre, const Place& x) {
+    if (kW == 1) return places_before<kW>(a, pre, x.b) + (long long)x.h * x.n_steps + x.step;
     return places_before<kW>(a, pre, x.b) + x.h * head_places<kW>(a, x.n_steps) + x.block * ((long long)weight<kW>(kW) * x.n_steps + a.pad) + a.pad + (long long)x.step * weight<kW>(x.width);
 }
 
@@ -614,18 +629,23 @@ page_decode_kernel(const PageAttnArgs a) {
             float sum = mine * ml.y;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-            auto add = [&](int i, const float4* src) {
+            auto add = [&](int i, float4 v) {
                 const float w = __shfl_sync(0xFFFFFFFFu, mine, i);
                 if (w != 0.f) {                        // (the others' memory holds anything)
-                    const float4 v = src[lane];
                     acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
                 }
             };
 #pragma unroll
-            for (int i = 0; i < kDecodeWarps; ++i) add(2 * i + 1, reinterpret_cast<const float4*>(pieces + i * kPiece + r * kD));
+            for (int i0 = 0; i0 < kDecodeWarps; i0 += 4) {
+                float4 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const float4*>(pieces + (i0 + i) * kPiece + r * kD)[lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) add(2 * (i0 + i) + 1, v[i]);
+            }
             for (unsigned rest = group & 0x55555555u; rest != 0; rest &= rest - 1) {
                 const int i = __ffs(rest) - 1;
-                add(i, reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kRows + r) * kD));
+                add(i, reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kRows + r) * kD)[lane]);
             }
             if (begins && ends) {
                 const int tok = r / a.G, head = seg.y * a.G + r % a.G;
