@@ -415,7 +415,8 @@ int daf_page_read(const daf_page_params* p, int32_t layer, int32_t n, const int3
  * lens[b] - L_q + t (the tokens of this call are in the pages already).  L_q = 1 is a decoding step.
  *   q     bf16 [n, L_q, n_q_heads, 128];  out  the same shape;  lse  fp32 [n, n_q_heads, L_q] or NULL
  *   softmax_scale  <= 0 selects 1/sqrt(128)
- * A row that sees no key is zeros with an lse of -inf.  At most 2048 sequences a call. */
+ * A row that sees no key is zeros with an lse of -inf.  At most 2048 sequences a call, and
+ * n * n_kv_heads * max_pages * page_tokens is at most 2^35. */
 int daf_page_attn(const daf_page_params* p, int32_t layer, int32_t n, const int32_t* seqs, const int32_t* lens, int32_t L_q,
                   int32_t n_q_heads, float softmax_scale, const void* q, const int32_t* table, const void* k8, const void* v8,
                   const float* k_scale, const float* v_scale, void* out, float* lse,

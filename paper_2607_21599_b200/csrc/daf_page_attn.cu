@@ -21,6 +21,7 @@ struct PageAttnArgs {
     Pool p;
     int n, L_q, Hq, G;
     int rows;              // query rows of a KV head: L_q * G, row r is token r / G, head r % G of the group
+    int inv_G;             // 65536 / G, rounded down, + 1
     int units;             // tiles of them: what a step of keys of one (sequence, KV head) costs
     int pad;               // what a segment costs beyond its steps
     float scale_log2;      // softmax scale * log2(e)
@@ -159,20 +160,26 @@ __device__ __forceinline__ void sum_steps(const PageAttnArgs& a, int step, int* 
     __syncthreads();
 }
 
-// Quotients on the work axis: the axis is seldom longer than 32 bits, and a division of 64 bits takes some 300 cycles.
+// Positions on the work axis.  For few rows 32 bits are enough (daf_page_attn refuses calls that could need more), and every CTA begins
+// with a chain of this arithmetic; for many rows a division of 32 bits is tried first, since one of 64 takes some 300 cycles.
+template <int kW> using Axis = std::conditional_t<kW == 1, int, long long>;
+__device__ __forceinline__ int axis_div(int x, int y) { return (int)((uint32_t)x / (uint32_t)y); }
 __device__ __forceinline__ long long axis_div(long long x, long long y) {
     return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
 // `total` places shared by `ctas`: the first `more` take each + 1, the others `each`.
-struct Shares { long long each, more; };
-__device__ __forceinline__ Shares share(long long total, long long ctas) {
-    const long long each = axis_div(total, ctas);
-    return Shares{each, total - each * ctas};
+template <typename A> struct Shares { A each, more; };
+template <typename A>
+__device__ __forceinline__ Shares<A> share(A total, A ctas) {
+    const A each = axis_div(total, ctas);
+    return Shares<A>{each, total - each * ctas};
 }
-__device__ __forceinline__ long long cta_begin(const Shares& s, long long c) { return c * s.each + min(c, s.more); }
+template <typename A>
+__device__ __forceinline__ A cta_begin(const Shares<A>& s, A c) { return c * s.each + min(c, s.more); }
 // The CTA whose stretch holds place `at`.
-__device__ __forceinline__ int cta_of(const Shares& s, long long at) {
-    const long long longer = s.more * (s.each + 1);
+template <typename A>
+__device__ __forceinline__ int cta_of(const Shares<A>& s, A at) {
+    const A longer = s.more * (s.each + 1);
     return (int)(at < longer ? axis_div(at, s.each + 1) : s.more + axis_div(at - longer, s.each));
 }
 
@@ -198,18 +205,18 @@ template <int kW>
 __device__ __forceinline__ int weight(int width) { return kW == 1 ? 1 : width + 1; }
 // Places that one (sequence, KV head) takes, and that sequences 0 .. b - 1 take.  (kW == 1, few rows: one tile, no pad.)
 template <int kW>
-__device__ __forceinline__ long long head_places(const PageAttnArgs& a, int n_steps) {
+__device__ __forceinline__ Axis<kW> head_places(const PageAttnArgs& a, int n_steps) {
     if (kW == 1) return n_steps;
-    return (long long)n_steps * (a.units / kW * weight<kW>(kW) + (a.units % kW != 0 ? weight<kW>(1) : 0)) + (long long)a.pad * ((a.units + kW - 1) / kW);
+    return (Axis<kW>)n_steps * (a.units / kW * weight<kW>(kW) + (a.units % kW != 0 ? weight<kW>(1) : 0)) + (Axis<kW>)a.pad * ((a.units + kW - 1) / kW);
 }
 template <int kW>
-__device__ __forceinline__ long long places_before(const PageAttnArgs& a, const int* pre, int b) {
-    if (kW == 1) return (long long)a.p.Hkv * pre[b];
-    return a.p.Hkv * (head_places<kW>(a, pre[b]) + (long long)(b - 1) * a.pad * ((a.units + kW - 1) / kW));
+__device__ __forceinline__ Axis<kW> places_before(const PageAttnArgs& a, const int* pre, int b) {
+    if (kW == 1) return a.p.Hkv * pre[b];
+    return a.p.Hkv * (head_places<kW>(a, pre[b]) + (Axis<kW>)(b - 1) * a.pad * ((a.units + kW - 1) / kW));
 }
 // The first step that begins at or behind `at` (which is less than the total); a place in front of a segment's first step stands for it.
 template <int kW>
-__device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre, long long at) {
+__device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre, Axis<kW> at) {
     int lo = 0, hi = a.n - 1;                    // last b whose places begin at or in front of `at`
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
@@ -220,8 +227,8 @@ __device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre,
     x.len = seq_len(a, lo);
     x.seq = a.seqs != nullptr ? __ldg(a.seqs + lo) : lo;
     x.n_steps = pre[lo + 1] - pre[lo];
-    long long rest = at - places_before<kW>(a, pre, lo);
-    const long long head = head_places<kW>(a, x.n_steps), block = (long long)weight<kW>(kW) * x.n_steps + a.pad;
+    Axis<kW> rest = at - places_before<kW>(a, pre, lo);
+    const Axis<kW> head = head_places<kW>(a, x.n_steps), block = (Axis<kW>)weight<kW>(kW) * x.n_steps + a.pad;
     x.h = (int)axis_div(rest, head);
     rest -= x.h * head;
     if (kW == 1) {
@@ -232,16 +239,16 @@ __device__ __forceinline__ Place place_at(const PageAttnArgs& a, const int* pre,
     }
     x.block = (int)axis_div(rest, block);
     x.width = min(kW, a.units - kW * x.block);
-    rest = max(rest - x.block * block - a.pad, 0ll);
-    x.step = (int)axis_div(rest + weight<kW>(x.width) - 1, weight<kW>(x.width));
+    rest = max(rest - x.block * block - a.pad, (Axis<kW>)0);
+    x.step = (int)axis_div(rest + weight<kW>(x.width) - 1, (Axis<kW>)weight<kW>(x.width));
     if (x.step == x.n_steps) next_segment<kW>(a, pre, x);
     return x;
 }
 // The last place that stands for a place's step.
 template <int kW>
-__device__ __forceinline__ long long axis_at(const PageAttnArgs& a, const int* pre, const Place& x) {
-    if (kW == 1) return places_before<kW>(a, pre, x.b) + (long long)x.h * x.n_steps + x.step;
-    return places_before<kW>(a, pre, x.b) + x.h * head_places<kW>(a, x.n_steps) + x.block * ((long long)weight<kW>(kW) * x.n_steps + a.pad) + a.pad + (long long)x.step * weight<kW>(x.width);
+__device__ __forceinline__ Axis<kW> axis_at(const PageAttnArgs& a, const int* pre, const Place& x) {
+    if (kW == 1) return places_before<kW>(a, pre, x.b) + x.h * x.n_steps + x.step;
+    return places_before<kW>(a, pre, x.b) + x.h * head_places<kW>(a, x.n_steps) + x.block * ((Axis<kW>)weight<kW>(kW) * x.n_steps + a.pad) + a.pad + (Axis<kW>)x.step * weight<kW>(x.width);
 }
 
 // A row's factor 1 / sum (a row that saw nothing: 0), its log-sum-exp, and the weight of a partial with (maximum, sum) in a merge
@@ -253,6 +260,10 @@ __device__ __forceinline__ float row_lse(float m, float l) {
 __device__ __forceinline__ float partial_weight(float2 ml, float mx) {
     return ml.y == 0.f ? 0.f : (ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - mx));
 }
+
+// Token of one of the few rows: row / G by the reciprocal in 16 bits (row < 24, G <= 24: what is added to it stays below 24 / 65536,
+// less than what row / G lacks of the next whole number).
+__device__ __forceinline__ int token_of(const PageAttnArgs& a, int row) { return (row * a.inv_G) >> 16; }
 
 template <int kN>
 __global__ void __launch_bounds__(decode_warps(kN) * 32, 1)
@@ -273,20 +284,21 @@ page_decode_kernel(const PageAttnArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     sum_steps<kDecodeWarps * 32>(a, kStep, pre, warp_sums);
-    const long long total = places_before<1>(a, pre, a.n);
+    const int total = places_before<1>(a, pre, a.n);
     // CTAs that take part: no more than give each of its warps a step
-    const long long ctas = min((long long)gridDim.x, (total + kDecodeWarps - 1) / kDecodeWarps);
-    const Shares shares = share(total, ctas);
-    const long long cta_lo = cta_begin(shares, min((long long)blockIdx.x, ctas));
-    const long long span = cta_begin(shares, min((long long)blockIdx.x + 1, ctas)) - cta_lo;
-    const long long lo = cta_lo + axis_div(warp * span, kDecodeWarps), hi = cta_lo + axis_div((warp + 1) * span, kDecodeWarps);
+    const int ctas = min((int)gridDim.x, (int)((unsigned)(total + kDecodeWarps - 1) / kDecodeWarps));
+    const Shares<int> shares = share(total, ctas);
+    const int cta_lo = cta_begin(shares, min((int)blockIdx.x, ctas)), span = cta_begin(shares, min((int)blockIdx.x + 1, ctas)) - cta_lo;
+    // a warp's stretch: the first ones take one more
+    const unsigned warp_each = (unsigned)span / kDecodeWarps, warp_more = (unsigned)span % kDecodeWarps;
+    const int lo = cta_lo + (int)(warp * warp_each + min((unsigned)warp, warp_more)), hi = lo + (int)(warp_each + ((unsigned)warp < warp_more ? 1u : 0u));
 
     const int T = a.p.T, Hkv = a.p.Hkv, page_bits = 31 - __clz(T);
     Place at = {};
     if (lo < hi) at = place_at<1>(a, pre, lo);
     // ---- the loads run ahead of the products with a place of their own
     Place ahead = at;
-    long long ahead_at = lo;
+    int ahead_at = lo;
     int ids = -1, ids_first = -64;               // page numbers of 32 pages of the place's sequence, one a lane
     const uint32_t ring_at = smem_u32(ring);
     const uint32_t dst0 = (uint32_t)((lane >> 3) * kD + (((lane & 7) ^ (lane >> 3)) << 4)), dst1 = (uint32_t)((lane >> 3) * kD + 512 + (((lane & 7) ^ (lane >> 3) ^ 4) << 4));
@@ -338,7 +350,7 @@ page_decode_kernel(const PageAttnArgs a) {
     bool tail = false;
     float o[kN][8][4];       // [column block][16 channels]: channels 16 c + 2 g and + 1 of rows 2 t (elements 0, 2) and 2 t + 1 (1, 3)
     float m[kN][2], l[kN][2];
-    for (long long x = lo; x < hi;) {
+    for (int x = lo; x < hi;) {
         // ---- a segment, or the stretch of it that is this warp's
         const int first_step = at.step;
         uint32_t qf[kN][8][2];
@@ -348,7 +360,7 @@ page_decode_kernel(const PageAttnArgs a) {
         for (int n = 0; n < kN; ++n) {
             const int row = 8 * n + g;
             const bool there = row < a.rows;
-            const uint2* const src = reinterpret_cast<const uint2*>(a.q + (((size_t)at.b * a.L_q + row / a.G) * a.Hq + at.h * a.G + row % a.G) * kD) + t;
+            const uint2* const src = reinterpret_cast<const uint2*>(a.q + (((size_t)at.b * a.L_q + token_of(a, row)) * a.Hq + at.h * a.G + row - token_of(a, row) * a.G) * kD) + t;
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
                 const uint2 v = there ? __ldg(src + kk * 4) : make_uint2(0u, 0u);
@@ -385,7 +397,7 @@ page_decode_kernel(const PageAttnArgs a) {
             for (int j = 0; j < 2; ++j) {
                 const int mine = 8 * n + 2 * t + j;
                 cs[n][j] = __shfl_sync(0xFFFFFFFFu, back, 4 * (2 * t + j));
-                limit[n][j] = mine < a.rows ? at.len - a.L_q + mine / a.G : -1;
+                limit[n][j] = mine < a.rows ? at.len - a.L_q + token_of(a, mine) : -1;
                 m[n][j] = -INFINITY;
                 l[n][j] = 0.f;
             }
@@ -549,7 +561,7 @@ page_decode_kernel(const PageAttnArgs a) {
                 for (int j = 0; j < 2; ++j) {
                     const int row = 8 * n + 2 * t + j;
                     if (row >= a.rows) continue;
-                    const int tok = row / a.G, head = at.h * a.G + row % a.G;
+                    const int tok = token_of(a, row), head = at.h * a.G + row - tok * a.G;
                     const float inv = row_inverse(l[n][j]);
                     uint32_t* const dst = reinterpret_cast<uint32_t*>(a.out + (((size_t)at.b * a.L_q + tok) * a.Hq + head) * kD) + g;
 #pragma unroll
@@ -648,7 +660,7 @@ page_decode_kernel(const PageAttnArgs a) {
                 add(i, reinterpret_cast<const float4*>(a.part_o + (((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (i >> 1)) * kRows + r) * kD)[lane]);
             }
             if (begins && ends) {
-                const int tok = r / a.G, head = seg.y * a.G + r % a.G;
+                const int tok = token_of(a, r), head = seg.y * a.G + r - tok * a.G;
                 const float inv = row_inverse(sum);
                 reinterpret_cast<uint2*>(a.out + (((size_t)seg.x * a.L_q + tok) * a.Hq + head) * kD)[lane] =
                     make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
@@ -726,7 +738,7 @@ struct QuestionSmem {
     Place at;
     int step1, n_t, first_limit, last_limit;      // steps at.step .. step1 - 1, of which the first n_t have keys that some row sees
     Place end;
-    Shares shares;
+    Shares<long long> shares;
     ChainEntry chain;
 };
 constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK = (int)(offsetof(QuestionSmem, k_full) / 8),
@@ -922,7 +934,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     if (warp == 0) {
         const long long total = places_before<2>(a, pre, a.n);
         const long long ctas = min((long long)gridDim.x, (total + 3) / 4);       // no fewer than two steps of a tile each
-        const Shares shares = share(total, ctas);
+        const Shares<long long> shares = share(total, ctas);
         // lane 0 finds the stretch's begin, lane 1 its end; both move up to the next step's begin
         const long long from = cta_begin(shares, min((long long)blockIdx.x + min(lane, 1), ctas));
         Place at = {};
@@ -1588,7 +1600,7 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     const int ctas = page_ctas();
     PageAttnArgs a;
     a.p = pool; a.n = n; a.L_q = L_q; a.Hq = Hq; a.G = Hq / pool.Hkv;
-    a.rows = L_q * a.G;
+    a.rows = L_q * a.G; a.inv_G = 65536 / a.G + 1;
     const int blocks = few_blocks(a.rows);
     const bool few = blocks > 0;
     a.units = few ? 1 : (a.rows + 127) / 128;

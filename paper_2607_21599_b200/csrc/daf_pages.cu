@@ -628,6 +628,10 @@ static int resolve_pages(const daf_page_params* p) {
     if (p->n_seqs > (1 << 20) || p->n_layers > 4096) return DAF_ERR_UNSUPPORTED;
     return DAF_OK;
 }
+// daf_page_attn counts its steps of 32 keys in 32 bits.
+static bool steps_fit(const daf_page_params* p, int n) {
+    return (long long)n * p->n_kv_heads * p->max_pages * p->page_tokens <= 1ll << 35;
+}
 static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 static size_t plan_bytes(const daf_page_params* p, int n) {
     return 256 + round256((size_t)p->n_pages * 8) + round256((size_t)p->n_pages * 4) + round256((size_t)p->n_seqs * 4) +
@@ -705,7 +709,7 @@ size_t daf_page_workspace_bytes(const daf_page_params* p, int32_t n, int32_t L_q
     if (resolve_pages(p) != DAF_OK || n < 0 || L_q < 0 || n_q_heads < 0) return 0;
     size_t need = plan_bytes(p, n);
     if (L_q > 0 && n_q_heads > 0) {
-        if (n_q_heads % p->n_kv_heads != 0 || n_q_heads > 256 || L_q > kPageMaxTokens || n > kPageMaxSeqs) return 0;
+        if (n_q_heads % p->n_kv_heads != 0 || n_q_heads > 256 || L_q > kPageMaxTokens || n > kPageMaxSeqs || !steps_fit(p, n)) return 0;
         const size_t attn = page_attn_scratch_bytes(n, L_q, n_q_heads, p->n_kv_heads);
         if (attn > need) need = attn;
     }
@@ -772,6 +776,7 @@ int daf_page_attn(const daf_page_params* p, int32_t layer, int32_t n, const int3
     if (layer < 0 || layer >= p->n_layers || n < 0 || L_q < 0 || n_q_heads <= 0) return DAF_ERR_INVALID_ARG;
     if (n_q_heads % p->n_kv_heads != 0 || n_q_heads > 256 || n > kPageMaxSeqs) return DAF_ERR_UNSUPPORTED;
     if ((long long)n * L_q > kPageMaxTokens) return DAF_ERR_UNSUPPORTED;
+    if (!steps_fit(p, n)) return DAF_ERR_UNSUPPORTED;
     if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes)) return rc;
     if (n == 0 || L_q == 0) return DAF_OK;
     if (int rc = check_workspace(workspace, workspace_bytes, kStatusBytes + page_attn_scratch_bytes(n, L_q, n_q_heads, p->n_kv_heads))) return rc;

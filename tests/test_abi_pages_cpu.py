@@ -162,6 +162,13 @@ def test_counts_layers_and_heads_are_checked():
     assert c["free"](n=-1) == api.DAF_ERR_INVALID_ARG
 
 
+def test_more_keys_than_an_attention_call_counts_are_refused():
+    p, b = _params(n_kv_heads=8, max_pages=(1 << 22) // 32), _buf()          # pages of 32 tokens: 4M tokens a sequence
+    ws = _buf(api.daf_page_workspace_bytes(p, 1024, 1, 8))
+    assert api.daf_page_workspace_bytes(p, 1025, 1, 8) == 0
+    assert _calls(p, b, ws)["attn"](n=1025, heads=8) == api.DAF_ERR_UNSUPPORTED
+
+
 def test_nothing_to_do_is_ok_and_launches_nothing():
     p, b = _params(), _buf()
     ws = _buf(api.daf_page_workspace_bytes(p, 4, 1, 4))
