@@ -66,7 +66,10 @@ constexpr float kPExp = 9.f;
 __host__ __device__ constexpr int decode_warps(int blocks) { return blocks == 1 ? 12 : 8; }
 __host__ __device__ constexpr int decode_depth(int blocks) { return blocks == 1 ? 2 : 3; }
 struct DecodeStage { float ks[2], vs[2]; };          // scales of the step's first and second 16 keys; negative: no such page
-__host__ __device__ constexpr int piece_floats(int rows) { return rows * kD + 2 * rows; }       // an unfinished segment's rows, maxima and sums
+// An unfinished segment's rows, maxima and sums in shared memory; rows 528 bytes apart, so that a warp's eight-byte stores to every second
+// row fall into different banks.
+constexpr int kPieceRow = kD + 4;
+__host__ __device__ constexpr int piece_floats(int rows) { return rows * kPieceRow + 2 * rows; }
 __host__ __device__ constexpr size_t ring_bytes(int blocks) { return (size_t)decode_warps(blocks) * decode_depth(blocks) * 2 * kTile; }
 __host__ __device__ constexpr size_t decode_smem(int blocks) {
     return 1024 + ring_bytes(blocks) + (size_t)decode_warps(blocks) * decode_depth(blocks) * sizeof(DecodeStage);
@@ -610,8 +613,8 @@ page_decode_kernel(const PageAttnArgs a) {
                 const int row = 8 * n + 2 * t + j;
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
-                    *reinterpret_cast<float2*>(dst + row * kD + 16 * c + 2 * g) = make_float2(o[n][c][j], o[n][c][2 + j]);
-                if (g == 0) reinterpret_cast<float2*>(dst + kRows * kD)[row] = make_float2(m[n][j], l[n][j]);
+                    *reinterpret_cast<float2*>(dst + row * kPieceRow + 16 * c + 2 * g) = make_float2(o[n][c][j], o[n][c][2 + j]);
+                if (g == 0) reinterpret_cast<float2*>(dst + kRows * kPieceRow)[row] = make_float2(m[n][j], l[n][j]);
             }
     }
     __syncthreads();
@@ -631,7 +634,7 @@ page_decode_kernel(const PageAttnArgs a) {
             // lane i knows piece i: odd ones lie here, even ones were parked
             float2 ml = make_float2(-INFINITY, 0.f);
             if ((group >> lane) & 1u)
-                ml = (lane & 1) ? reinterpret_cast<const float2*>(pieces + (lane >> 1) * kPiece + kRows * kD)[r]
+                ml = (lane & 1) ? reinterpret_cast<const float2*>(pieces + (lane >> 1) * kPiece + kRows * kPieceRow)[r]
                                 : __ldcg(a.part_ml + ((size_t)gridDim.x * 2 + (size_t)blockIdx.x * kDecodeWarps + (lane >> 1)) * kRows + r);
             float mx = ml.x;
 #pragma unroll
@@ -643,15 +646,15 @@ page_decode_kernel(const PageAttnArgs a) {
             for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
             auto add = [&](int i, float4 v) {
                 const float w = __shfl_sync(0xFFFFFFFFu, mine, i);
-                if (w != 0.f) {                        // (the others' memory holds anything)
-                    acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
-                }
+                const bool counts = w != 0.f;          // (the others' memory holds anything)
+                acc.x += counts ? w * v.x : 0.f; acc.y += counts ? w * v.y : 0.f;
+                acc.z += counts ? w * v.z : 0.f; acc.w += counts ? w * v.w : 0.f;
             };
 #pragma unroll
             for (int i0 = 0; i0 < kDecodeWarps; i0 += 4) {
                 float4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const float4*>(pieces + (i0 + i) * kPiece + r * kD)[lane];
+                for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const float4*>(pieces + (i0 + i) * kPiece + r * kPieceRow)[lane];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) add(2 * (i0 + i) + 1, v[i]);
             }
