@@ -114,6 +114,19 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {            // 0xFF w
     return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
 }
 
+// Largest magnitude (bf16 bits, which ascend with it) of the finite ones among words of two bf16 values: all of them at first, two at
+// a time, and only where one is not finite each by itself.
+struct FiniteMax {
+    uint32_t pairs = 0;
+    __device__ __forceinline__ void add(uint32_t w) { pairs = __vmaxu2(pairs, w & 0x7FFF7FFFu); }
+    __device__ __forceinline__ uint32_t top() const { return max(pairs & 0xFFFFu, pairs >> 16); }
+    __device__ __forceinline__ bool all_finite() const { return top() < 0x7F80u; }
+};
+__device__ __forceinline__ uint32_t finite_top(uint32_t w) {
+    const uint32_t b0 = w & 0x7FFFu, b1 = (w >> 16) & 0x7FFFu;
+    return max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u);
+}
+
 // A place on the work axis: a segment is (b, h, block), a block `width` tiles (kW, or one less in the last).  It takes a.pad places, for
 // what it costs beyond its steps, and weight<kW>(width) places for each of them.
 struct Place { int b, h, block, width, step, n_steps, seq, len; };
@@ -381,11 +394,14 @@ page_decode_kernel(const PageAttnArgs a) {
         }
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
-            uint32_t big = 0;
+            FiniteMax all;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const uint32_t bits = (qf[n][j >> 2][(j >> 1) & 1] >> (16 * (j & 1))) & 0x7FFFu;
-                big = max(big, bits < 0x7F80u ? bits : 0u);
+            for (int j = 0; j < 16; ++j) all.add(qf[n][j >> 1][j & 1]);
+            uint32_t big = all.top();
+            if (!all.all_finite()) {
+                big = 0;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) big = max(big, finite_top(qf[n][j >> 1][j & 1]));
             }
             big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
             big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
@@ -1024,14 +1040,19 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 cp_async_wait_group<0>();
                 __syncwarp();
                 const uint4* const mine = reinterpret_cast<const uint4*>(raw + rt * 256);
-                uint32_t big = 0;
-#pragma unroll 4
+                FiniteMax all;
+#pragma unroll 8
                 for (int i = 0; i < 16; ++i) {
                     const uint4 w = mine[i ^ (rt & 15)];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t x = (j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w), b0 = x & 0x7FFFu, b1 = (x >> 16) & 0x7FFFu;
-                        big = max(big, max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u));
+                    all.add(w.x); all.add(w.y); all.add(w.z); all.add(w.w);
+                }
+                uint32_t big = all.top();
+                if (!all.all_finite()) {
+                    big = 0;
+#pragma unroll 1
+                    for (int i = 0; i < 16; ++i) {
+                        const uint4 w = mine[i];
+                        big = max(max(big, max(finite_top(w.x), finite_top(w.y))), max(finite_top(w.z), finite_top(w.w)));
                     }
                 }
                 const int e = max((int)(big >> 7) - 127, -100);
