@@ -398,41 +398,46 @@ def alloc_page_workspace(p: daf_page_params, n: int, L_q: int = 0, n_q_heads: in
     return torch.zeros(size, dtype=torch.uint8, device=device)
 
 
+def _page_workspace(workspace):
+    """Address and size, once it is sure that the call's tensors can be on the current device, where its kernels run."""
+    if workspace is not None and torch.cuda.is_initialized() and workspace.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("the workspace is not on the current device")
+    return _ptr(workspace), _nbytes(workspace)
+
+
 def daf_page_write(p, layer, n, seqs, lens, row_off, idx, max_rows, k, v, table, refs, k8, v8, k_scale, v_scale, workspace,
                    stream=None) -> int:
     return lib().daf_page_write(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(lens), _ptr(row_off), _ptr(idx),
                                 int(max_rows), _ptr(k), _ptr(v), _ptr(table), _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale),
-                                _ptr(v_scale), _ptr(workspace), _nbytes(workspace), _stream(stream))
+                                _ptr(v_scale), *_page_workspace(workspace), _stream(stream))
 
 
 def daf_page_read(p, layer, n, seqs, first, row_off, max_rows, table, k8, v8, k_scale, v_scale, k_rows, v_rows, workspace,
                   stream=None) -> int:
     return lib().daf_page_read(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(first), _ptr(row_off), int(max_rows),
                                _ptr(table), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(k_rows), _ptr(v_rows),
-                               _ptr(workspace), _nbytes(workspace), _stream(stream))
+                               *_page_workspace(workspace), _stream(stream))
 
 
 def daf_page_attn(p, layer, n, seqs, lens, L_q, n_q_heads, softmax_scale, q, table, k8, v8, k_scale, v_scale, out, lse,
                   workspace, stream=None) -> int:
     return lib().daf_page_attn(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(lens), int(L_q), int(n_q_heads),
                                float(softmax_scale), _ptr(q), _ptr(table), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale),
-                               _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
+                               _ptr(out), _ptr(lse), *_page_workspace(workspace), _stream(stream))
 
 
 def daf_page_fork(p, n, src, dst, keep, want, share, table, refs, k8, v8, k_scale, v_scale, workspace, stream=None) -> int:
     return lib().daf_page_fork(ctypes.byref(p), int(n), _ptr(src), _ptr(dst), _ptr(keep), _ptr(want), int(bool(share)), _ptr(table),
-                               _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(workspace),
-                               _nbytes(workspace), _stream(stream))
+                               _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), *_page_workspace(workspace), _stream(stream))
 
 
 def daf_page_free(p, n, seqs, keep, table, refs, workspace, stream=None) -> int:
-    return lib().daf_page_free(ctypes.byref(p), int(n), _ptr(seqs), _ptr(keep), _ptr(table), _ptr(refs), _ptr(workspace),
-                               _nbytes(workspace), _stream(stream))
+    return lib().daf_page_free(ctypes.byref(p), int(n), _ptr(seqs), _ptr(keep), _ptr(table), _ptr(refs), *_page_workspace(workspace), _stream(stream))
 
 
 def daf_page_compact(p, table, refs, table_out, refs_out, live_out, k8, v8, k_scale, v_scale, workspace, stream=None) -> int:
     return lib().daf_page_compact(ctypes.byref(p), _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(live_out),
-                                  _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(workspace), _nbytes(workspace),
+                                  _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), *_page_workspace(workspace),
                                   _stream(stream))
 
 

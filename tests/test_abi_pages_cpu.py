@@ -162,6 +162,16 @@ def test_counts_layers_and_heads_are_checked():
     assert c["free"](n=-1) == api.DAF_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("call", ["write", "read", "attn", "fork", "free", "compact"])
+def test_another_device_than_the_current_one_is_refused(call, monkeypatch):
+    p, b = _params(), _buf()
+    ws = _buf(api.daf_page_workspace_bytes(p, 4, 1, 4))
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    with pytest.raises(ValueError, match="current device"):
+        _calls(p, b, ws)[call]()
+
+
 def test_more_keys_than_an_attention_call_counts_are_refused():
     p, b = _params(n_kv_heads=8, max_pages=(1 << 22) // 32), _buf()          # pages of 32 tokens: 4M tokens a sequence
     ws = _buf(api.daf_page_workspace_bytes(p, 1024, 1, 8))
