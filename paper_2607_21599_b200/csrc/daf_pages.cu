@@ -250,13 +250,15 @@ __global__ void __launch_bounds__(128) page_read_kernel(const ReadArgs a) {
 // prefix sums over items and over refs, then a grid does what was decided: table, refs and the bytes.  Copies of some 100 MB run at 5.4 to
 // 5.8 TB/s (82 to 88 % of a copy's rate); of few pages the decision is what counts: 5 to 7 us of dependent loads and scans in one CTA.
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanRefs = 16;            // refs a thread looks at per round: 16k pages a round
+constexpr int kPlanRefs = 16;            // words of 32 pages that a warp looks at per round at most: 16k pages a round
+constexpr int kPlanRound = kPlanThreads * kPlanRefs;
+constexpr int kPlanRows = 1 << 16;       // up to as many rows of the table are marked in shared memory
 
 struct PlanHead { int ok, n_new, n_copies, live; };
 struct PlanArrays {       // in the workspace behind the status word
     PlanHead* head;
     int2* copies;         // [n_pages] (from, to)
-    int32_t* fresh;       // [n_pages, to a multiple of 64] pages handed out, ascending (compact: where a page goes, by its old number, or -1)
+    int32_t* fresh;       // [n_pages] pages handed out, ascending (compact: where a page goes, by its old number, or -1)
     int32_t* marks;       // [n_seqs]
     int2* items;          // [n + 1] running counts: new pages, copies
 };
@@ -291,6 +293,43 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
 }
 __device__ __forceinline__ unsigned long long pack2(int a, int b) { return ((unsigned long long)(unsigned)a << 32) | (unsigned)b; }
 
+// Which of a round's pages from p0 on are free (or, kUsed, in use): word u of a warp holds 32 neighbouring pages from plan_page(p0, u,
+// words) on, and no warp has more words than the round's pages, shared by all warps, need.
+__device__ __forceinline__ int plan_words_of(int n_pages, int p0) { return min(kPlanRefs, (n_pages - p0 + kPlanThreads - 1) / kPlanThreads); }
+__device__ __forceinline__ int plan_page(int p0, int u, int words) { return p0 + ((int)(threadIdx.x >> 5) * words + u) * 32; }
+template <bool kUsed>
+__device__ __forceinline__ void plan_words(const int32_t* refs, int n_pages, int p0, unsigned (&m)[kPlanRefs]) {
+    const int words = plan_words_of(n_pages, p0);
+    int r[kPlanRefs];
+#pragma unroll
+    for (int u = 0; u < kPlanRefs; ++u) {
+        const int p = plan_page(p0, u, words) + (int)(threadIdx.x & 31);
+        r[u] = u < words && p < n_pages ? refs[p] : (kUsed ? 0 : 1);
+    }
+#pragma unroll
+    for (int u = 0; u < kPlanRefs; ++u) {
+        m[u] = 0;
+        if (u < words) m[u] = __ballot_sync(0xFFFFFFFFu, kUsed ? r[u] > 0 : r[u] == 0);
+    }
+}
+// The sums of two counts of each warp over the warps in front of this one, and over all of them.
+__device__ __forceinline__ int2 warps_before(int2 mine, int2* all) {
+    __shared__ int2 of_warp[kPlanThreads / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();
+    if (lane == 0) of_warp[warp] = mine;
+    __syncthreads();
+    const int2 c = of_warp[lane];
+    *all = make_int2(__reduce_add_sync(0xFFFFFFFFu, c.x), __reduce_add_sync(0xFFFFFFFFu, c.y));
+    return make_int2(__reduce_add_sync(0xFFFFFFFFu, lane < warp ? c.x : 0), __reduce_add_sync(0xFFFFFFFFu, lane < warp ? c.y : 0));
+}
+__device__ __forceinline__ int words_sum(const unsigned (&m)[kPlanRefs]) {
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < kPlanRefs; ++u) n += __popc(m[u]);
+    return n;
+}
+
 struct ForkArgs {
     int n_pages, T, n_seqs, max_pages, n, share;
     const int32_t* src; const int32_t* dst; const int32_t* keep; const int32_t* want;
@@ -303,11 +342,11 @@ struct ForkArgs {
 struct ForkItem {
     int src, dst, first_new, n_new, n_copies;     // columns first_new .. first_new + n_new - 1 get new pages (a replaced one included)
 };
-__device__ __forceinline__ ForkItem fork_item(const ForkArgs& a, int i, bool* bad) {
+__device__ __forceinline__ ForkItem fork_item(const ForkArgs& a, int4 given, bool* bad) {
     ForkItem f;
-    f.src = __ldg(a.src + i); f.dst = __ldg(a.dst + i);
+    f.src = given.x; f.dst = given.y;
     f.first_new = f.n_new = f.n_copies = 0;
-    const int want = __ldg(a.want + i), keep = f.src >= 0 ? __ldg(a.keep + i) : 0;
+    const int want = given.w, keep = f.src >= 0 ? given.z : 0;
     const long long room = (long long)a.max_pages * a.T;
     if ((unsigned)f.dst >= (unsigned)a.n_seqs || f.src >= a.n_seqs || want < 0 || want > room || keep < 0 || keep > room) {
         *bad = true;
@@ -339,25 +378,35 @@ __device__ __forceinline__ ForkItem fork_item(const ForkArgs& a, int i, bool* ba
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const ForkArgs a) {
     pdl_wait();
     pdl_launch_dependents();
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31;
     __shared__ int any_bad;
+    __shared__ unsigned named[kPlanRows / 32];
+    // what the first round of everything needs is asked for at once
+    unsigned free_words[kPlanRefs];
+    plan_words<false>(a.refs, a.n_pages, 0, free_words);
+    auto given = [&](int i) { return i < a.n ? make_int4(__ldg(a.src + i), __ldg(a.dst + i), __ldg(a.keep + i), __ldg(a.want + i)) : make_int4(-1, -1, 0, 0); };
+    const int4 first = given(tid);
     if (tid == 0) any_bad = 0;
-    for (int i = tid; i < a.n_seqs; i += kPlanThreads) a.w.marks[i] = 0;
+    const bool in_smem = a.n_seqs <= kPlanRows;
+    if (in_smem) for (int i = tid; i < (a.n_seqs + 31) / 32; i += kPlanThreads) named[i] = 0;
+    else for (int i = tid; i < a.n_seqs; i += kPlanThreads) a.w.marks[i] = 0;
     __syncthreads();
     // every row at most once as a target, and no target as another item's source
     for (int i = tid; i < a.n; i += kPlanThreads) {
-        const int d = __ldg(a.dst + i);
-        if ((unsigned)d < (unsigned)a.n_seqs && atomicAdd(&a.w.marks[d], 1) != 0) any_bad = 1;
+        const int d = i == tid ? first.y : __ldg(a.dst + i);
+        if ((unsigned)d >= (unsigned)a.n_seqs) continue;
+        if (in_smem ? (atomicOr(&named[d >> 5], 1u << (d & 31)) >> (d & 31)) & 1u : (unsigned)(atomicAdd(&a.w.marks[d], 1) != 0)) any_bad = 1;
     }
     __syncthreads();
+    auto is_named = [&](int d) { return in_smem ? ((named[d >> 5] >> (d & 31)) & 1u) != 0u : __ldcg(&a.w.marks[d]) != 0; };
     unsigned long long run = 0;
     for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
         const int i = i0 + tid;
         bool bad = false;
         ForkItem f = {};
         if (i < a.n) {
-            f = fork_item(a, i, &bad);
-            if (f.src >= 0 && f.src < a.n_seqs && f.src != f.dst && __ldcg(&a.w.marks[f.src]) != 0) bad = true;
+            f = fork_item(a, i == tid ? first : given(i), &bad);
+            if (f.src >= 0 && f.src < a.n_seqs && f.src != f.dst && is_named(f.src)) bad = true;
             if (bad) any_bad = 1;
         }
         unsigned long long sum;
@@ -378,16 +427,19 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const ForkArgs 
     }
     // the n_new free pages of lowest number
     int found = 0;
-    for (int p0 = 0; p0 < a.n_pages && found < n_new; p0 += kPlanThreads * kPlanRefs) {
-        const int p = p0 + tid * kPlanRefs;
-        unsigned free_bits = 0;
+    for (int p0 = 0; p0 < a.n_pages && found < n_new; p0 += kPlanRound) {
+        if (p0 > 0) plan_words<false>(a.refs, a.n_pages, p0, free_words);
+        int2 all;
+        int at = found + warps_before(make_int2(words_sum(free_words), 0), &all).x;
+        const int words = plan_words_of(a.n_pages, p0);
 #pragma unroll
-        for (int u = 0; u < kPlanRefs; ++u)
-            if (p + u < a.n_pages && a.refs[p + u] == 0) free_bits |= 1u << u;
-        unsigned long long sum;
-        int at = found + (int)block_scan((unsigned long long)__popc(free_bits), &sum);
-        for (unsigned m = free_bits; m != 0 && at < n_new; m &= m - 1) a.w.fresh[at++] = p + __ffs(m) - 1;
-        found += (int)sum;
+        for (int u = 0; u < kPlanRefs; ++u) {
+            if (u >= words) break;
+            const int rank = at + __popc(free_words[u] & ((1u << lane) - 1u));
+            if (((free_words[u] >> lane) & 1u) && rank < n_new) a.w.fresh[rank] = plan_page(p0, u, words) + lane;
+            at += __popc(free_words[u]);
+        }
+        found += all.x;
     }
     const bool ok = found >= n_new;
     if (tid == 0) {
@@ -543,56 +595,64 @@ struct CompactArgs {
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CompactArgs a) {
     pdl_wait();
     pdl_launch_dependents();
-    const int tid = threadIdx.x;
-    auto used_bits = [&](int p) {
-        unsigned m = 0;
-#pragma unroll
-        for (int u = 0; u < kPlanRefs; ++u)
-            if (p + u < a.n_pages && a.refs[p + u] > 0) m |= 1u << u;
-        return m;
-    };
-    unsigned long long sum;
+    const int tid = threadIdx.x, lane = tid & 31;
+    unsigned used[kPlanRefs];
+    int2 all;
     int live = 0;
-    for (int p0 = 0; p0 < a.n_pages; p0 += kPlanThreads * kPlanRefs) {
-        block_scan((unsigned long long)__popc(used_bits(p0 + tid * kPlanRefs)), &sum);
-        live += (int)sum;
+    for (int p0 = 0; p0 < a.n_pages; p0 += kPlanRound) {
+        plan_words<true>(a.refs, a.n_pages, p0, used);
+        warps_before(make_int2(words_sum(used), 0), &all);
+        live += all.x;
     }
     // the r-th page in use at or above `live` goes to the r-th free one below it
     int holes = 0, movers = 0;
-    for (int p0 = 0; p0 < a.n_pages; p0 += kPlanThreads * kPlanRefs) {
-        const int p = p0 + tid * kPlanRefs;
-        const unsigned used = used_bits(p);
-        const unsigned below = p >= live ? 0u : (live - p >= kPlanRefs ? (1u << kPlanRefs) - 1u : (1u << (live - p)) - 1u);
-        unsigned hole = ~used & below, mover = used & ~below;
-        if (p + kPlanRefs > live && p < a.n_pages) {      // where no page goes to: an entry of the table must not name it (movers follow below)
+    for (int p0 = 0; p0 < a.n_pages; p0 += kPlanRound) {
+        if (a.n_pages > kPlanRound) plan_words<true>(a.refs, a.n_pages, p0, used);
+        const int words = plan_words_of(a.n_pages, p0);
+        auto below = [&](int u) {            // pages of word u in front of `live`
+            const int n = live - plan_page(p0, u, words);
+            return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+        };
+        int2 mine = make_int2(0, 0);
 #pragma unroll
-            for (int u = 0; u < kPlanRefs; u += 4) *reinterpret_cast<int4*>(a.w.fresh + p + u) = make_int4(-1, -1, -1, -1);
+        for (int u = 0; u < kPlanRefs; ++u) {
+            if (u >= words) break;
+            mine.x += __popc(~used[u] & below(u));
+            mine.y += __popc(used[u] & ~below(u));
         }
-        const unsigned long long at = block_scan(pack2(__popc(hole), __popc(mover)), &sum);
-        int h = holes + (int)(at >> 32), v = movers + (int)(at & 0xFFFFFFFFu);
-        for (; hole != 0; hole &= hole - 1) a.w.copies[h++].y = p + __ffs(hole) - 1;
-        for (; mover != 0; mover &= mover - 1) a.w.copies[v++].x = p + __ffs(mover) - 1;
-        holes += (int)(sum >> 32);
-        movers += (int)(sum & 0xFFFFFFFFu);
+        const int2 before = warps_before(mine, &all);
+        int h = holes + before.x, v = movers + before.y;
+#pragma unroll
+        for (int u = 0; u < kPlanRefs; ++u) {
+            if (u >= words) break;
+            const unsigned hole = ~used[u] & below(u), mover = used[u] & ~below(u), lower = (1u << lane) - 1u;
+            const int p = plan_page(p0, u, words) + lane;
+            if ((hole >> lane) & 1u) a.w.copies[h + __popc(hole & lower)].y = p;
+            if ((mover >> lane) & 1u) a.w.copies[v + __popc(mover & lower)].x = p;
+            else if (p >= live && p < a.n_pages) a.w.fresh[p] = -1;      // where no page goes to: an entry of the table must not name it
+            h += __popc(hole);
+            v += __popc(mover);
+        }
+        holes += all.x;
+        movers += all.y;
     }
     __syncthreads();
+    // The counts, here because refs_out may be refs: a moved page's goes to its new place before its old one is cleared, and nothing else
+    // touches either.
     for (int r = tid; r < movers; r += kPlanThreads) {
         const int2 c = a.w.copies[r];
+        const int count = a.refs[c.x];
         a.w.fresh[c.x] = c.y;
+        a.refs_out[c.y] = count;
+        a.refs_out[c.x] = 0;
     }
-    // the counts, here because refs_out may be refs: a moved page's goes to its new place before its old one is cleared
-    __syncthreads();
-    for (int p = tid; p < live; p += kPlanThreads) {
-        const int r = a.refs[p];
-        if (r > 0) a.refs_out[p] = r;
-    }
-    __syncthreads();
-    for (int r = tid; r < movers; r += kPlanThreads) {
-        const int2 c = a.w.copies[r];
-        a.refs_out[c.y] = a.refs[c.x];
-    }
-    __syncthreads();
-    for (int p = live + tid; p < a.n_pages; p += kPlanThreads) a.refs_out[p] = 0;
+    if (a.refs_out != a.refs)
+        for (int p = tid; p < live; p += kPlanThreads) {
+            const int r = a.refs[p];
+            if (r > 0) a.refs_out[p] = r;
+        }
+    for (int p = live + tid; p < a.n_pages; p += kPlanThreads)
+        if (a.refs[p] <= 0) a.refs_out[p] = 0;
     if (tid == 0) {
         *a.w.head = PlanHead{1, 0, movers, live};
         if (a.live_out != nullptr) *a.live_out = live;

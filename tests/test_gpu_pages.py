@@ -712,6 +712,17 @@ def test_compact_reports_entries_whose_page_has_no_count():
     assert c.t["refs"].cpu().tolist() == [1, 1] + [0] * 7
 
 
+def test_a_table_of_very_many_rows():
+    n = 70000
+    c = Cache(500, 16, 1, n, 2, seed=2, junk=False)
+    assert _fork(c, [-1, -1, -1], [69999, 3, 65536], [0, 0, 0], [32, 17, 5], True) == ""
+    assert _fork(c, [69999, 69999, 3], [65537, 0, 69998], [20, 16, 17], [20, 32, 30], True) == ""
+    assert _fork(c, [69999, 69999], [65538, 65538], [20, 20], [20, 20], True) == "bounds"
+    assert _fork(c, [69999, 65539], [65539, 8], [20, 0], [20, 16], True) == "bounds"
+    _free(c, [65536, 69999])
+    _compact(c)
+
+
 def test_free_reports_rows_and_counts_that_are_wrong():
     c = Cache(6, 16, 1, 2, 3, seed=1, junk=False)
     c.give(0, 48)
