@@ -748,6 +748,7 @@ static int launched(cudaError_t e) {
 }
 // Pages that `rows` newest (or any consecutive) tokens can touch.
 static int touched_pages(const daf_page_params* p, int rows) {
+    if (rows > kPageMaxTokens) rows = kPageMaxTokens;
     const int t = (rows + p->page_tokens - 2) / p->page_tokens + 1;
     return t < p->max_pages ? t : p->max_pages;
 }

@@ -175,6 +175,24 @@ def test_many_rows_over_several_grid_rounds_and_small_max_rows():
     c.same()
 
 
+@pytest.mark.parametrize("T", [16, 32])
+def test_neighbouring_pages_are_written_apart(T):
+    # neighbouring pages whose rows differ by many powers of two, one of them missing, one shared, a first and a last kept in part
+    c = Cache(40, T, 2, 2, 9, seed=T, junk=False)
+    for s in range(2):
+        c.give(s, 9 * T)
+    c.np["table"][0, 3] = -1
+    c.np["refs"][c.np["table"][0, 5]] = 2
+    c.up()
+    L, R = 9 * T - 3, 8 * T + 1
+    x = [(_rows(R, 2, seed, 0.0).float() * torch.exp2(-4.0 * (torch.arange(R) // 5 % 7).float())[:, None, None]).to(torch.bfloat16) for seed in (1, 2)]
+    _write(c, [L], [R], k=x[0], v=x[1], status=api.DAF_ERR_BOUNDS)
+    c.same()
+    _write(c, [L, L - 4], [R, 3 * T], k=torch.cat([x[1], x[0][:3 * T]]), v=torch.cat([x[0], x[1][:3 * T]]), seqs=[1, 0], status=api.DAF_ERR_BOUNDS,
+           max_rows=2 ** 31 - 1)
+    c.same()
+
+
 def test_write_skips_and_reports_what_is_out_of_range():
     c = Cache(20, 16, 2, 4, 4, seed=6)
     for s in range(4):
