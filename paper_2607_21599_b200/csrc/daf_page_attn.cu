@@ -5,6 +5,7 @@
 // equal stretch of it.  A segment that lies in several CTAs leaves partial rows (at most two sets per CTA, whatever the shapes),
 // which a second kernel merges.
 #include <cuda_fp16.h>
+#include <float.h>
 #include <math.h>
 #include <stddef.h>
 
@@ -792,6 +793,10 @@ __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t 
 }
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
+// A row's factor for the logits of a chunk.  It stays a normal number: with rows of zeros or nearly so and keys of a small scale the product
+// would be flushed to zero, and hidden logits, which are -inf ahead of it, would become NaN.  (Visible logits are below 2^32 ahead of it: times this bound they are nothing.)
+__device__ __forceinline__ float logit_factor(float c, float ks) { return fmaxf(c * fabsf(ks), FLT_MIN); }
+
 // One softmax step of one row over 128 keys: P over the first half of the logits' columns, running maximum and sum.  `rescale` is called
 // ahead of the first P with the factor for the row of O (1 unless the maximum grew by more than kLazy), `half_done` when half of P is
 // on its way to tensor memory.  c: the row's factor for its logits; chunk: two half steps' constants.  A thread has no
@@ -832,7 +837,7 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
                 mx[0] = fmax3(mx[0], __uint_as_float(sr[q & 1][16 * i + j]), __uint_as_float(sr[q & 1][16 * i + j + 1]));
                 mx[1] = fmax3(mx[1], __uint_as_float(sr[q & 1][16 * i + j + 2]), __uint_as_float(sr[q & 1][16 * i + j + 3]));
             }
-            top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), c * fabsf(k2.x), k2.y));
+            top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), logit_factor(c, k2.x), k2.y));
         }
     }
     float now = fmaxf(m, top);
@@ -849,7 +854,7 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const float4 k4 = chunk[q >> 1][2 * (q & 1) + i];
-            const float f = c * fabsf(k4.x), d = k4.y - used;
+            const float f = logit_factor(c, k4.x), d = k4.y - used;
             const uint64_t f2 = pack_f32x2(f, f), d2 = pack_f32x2(d, d);
             uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll

@@ -878,3 +878,35 @@ def test_two_graphs_share_a_workspace():
             got, _ = _attend(c, now, L_q, 8)
             assert np.array_equal(got, out[L_q].float().cpu().numpy())
     assert api.daf_poll_status(ws) == api.DAF_OK
+
+
+@pytest.mark.parametrize("L_q", [1, 6, 7, 40, 80])          # rows of a KV head: 4, 24 | 28, 160, 320 (one tile, a pair, a pair and one)
+@pytest.mark.parametrize("exps", [(-60, -59), (-60, -3), (-14, -9)])
+def test_zero_and_tiny_rows_over_small_key_scales(L_q, exps):
+    lens = [500, 3, 0, 200]                                 # (3 and 0: rows that see nothing)
+    c = _cache_for(lens, 16, 2, seed=61, junk=False)
+    c.np["k_scale"][:] = (2.0 ** np.random.default_rng(L_q).integers(*exps, c.np["k_scale"].shape)).astype(np.float32)
+    c.up()
+    q = torch.randn(4, L_q, 8, 128, generator=torch.Generator().manual_seed(5))
+    q[:, :, ::4] = 0.0
+    q[:, :, 1::4] *= 1e-30
+    q[:, :, 2::4] *= 1e-37
+    q[3, -1] = 0.0
+    for scale in (0.0, 1e-6):
+        _attend(c, lens, L_q, 8, q=q.to(torch.bfloat16), scale=scale)
+
+
+@pytest.mark.parametrize("L_q", [1, 7, 70])
+def test_zero_keys_as_they_are_written(L_q):
+    lens = [150, 5, 64]
+    c = _cache_for(lens, 32, 1, seed=62, junk=False)
+    k = _rows(sum(lens), 1, 3)
+    k[40:150] = 0.0
+    k[155:] = 0.0
+    _write(c, lens, lens, k=k)
+    c.same()
+    assert (c.np["k_scale"] == 2.0 ** -60).any()
+    q = torch.randn(3, L_q, 4, 128, generator=torch.Generator().manual_seed(6))
+    q[:, :, 1] = 0.0
+    q[:, :, 2] *= 1e-25
+    _attend(c, lens, L_q, 4, q=q.to(torch.bfloat16))
