@@ -428,7 +428,8 @@ int daf_page_attn(const daf_page_params* p, int32_t layer, int32_t n, const int3
  *                              in every layer; a page of which only a part is kept is always copied.
  *   src[i] < 0                 row dst[i], which must hold no pages, gets pages for want[i] tokens (keep is not read)
  *   src[i] == dst[i]           the row grows to pages for want[i] tokens.  keep[i] is its length now: the page its next token
- *                              goes into is replaced by a copy if others share it.
+ *                              goes into, if the row holds it, is replaced by a copy if others share it.  (Only that one:
+ *                              pages behind it that a row set back shares with others are given back by daf_page_free first.)
  * New pages are the free ones of lowest number, in the items' order, and start with whatever they held.  A row named as dst must
  * not be named by any other item.  If an item is not as described, or the free pages are too few, nothing is changed and
  * DAF_ERR_BOUNDS or DAF_ERR_PAGES recorded. */

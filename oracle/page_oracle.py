@@ -156,7 +156,7 @@ class Pool:
             if s == d:
                 row = self.table[d].tolist()
                 have = sum(e >= 0 for e in row)
-                if whole < held and refs0[row[whole]] > 1:
+                if whole < have and refs0[row[whole]] > 1:      # the page that token `keep` goes into, with tokens of the row in it or not
                     copies.append((row[whole], whole))
                 new = [c for _, c in copies] + list(range(have, pages))
             else:

@@ -365,8 +365,9 @@ __device__ __forceinline__ ForkItem fork_item(const ForkArgs& a, int4 given, boo
         if (held > lo) { *bad = true; return f; }
         f.first_new = lo;
         f.n_new = max(pages - lo, 0);
-        // a page of which a part is kept, shared with others: replaced (fork_column says where its copy comes from)
-        if (whole < held && (unsigned)row[whole] < (unsigned)a.n_pages && a.refs[row[whole]] > 1) { f.n_copies = 1; f.n_new += 1; }
+        // the page that the next token goes into, if the row holds it and others share it: replaced by a copy.  (It holds none of the
+        // row's tokens where a row of more pages was set back to a border by its length alone.)
+        if (whole < lo && (unsigned)row[whole] < (unsigned)a.n_pages && a.refs[row[whole]] > 1) { f.n_copies = 1; f.n_new += 1; }
     } else {
         if (row[0] >= 0) { *bad = true; return f; }
         if (f.src >= 0 && held > 0 && a.table[(size_t)f.src * a.max_pages + held - 1] < 0) { *bad = true; return f; }

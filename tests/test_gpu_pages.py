@@ -910,3 +910,40 @@ def test_zero_keys_as_they_are_written(L_q):
     q[:, :, 1] = 0.0
     q[:, :, 2] *= 1e-25
     _attend(c, lens, L_q, 4, q=q.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("T", [16, 128])
+@pytest.mark.parametrize("with_refs", [True, False])
+def test_growth_replaces_the_page_of_the_next_token_at_a_border_too(T, with_refs):
+    c = Cache(8, T, 2, 3, 4, n_layers=2, seed=T, junk=False)
+    assert _fork(c, [-1], [0], [0], [2 * T], True) == ""
+    _write(c, [2 * T], [2 * T], layer=1)
+    assert _fork(c, [0], [1], [2 * T], [2 * T], True) == ""
+    assert c.t["table"].tolist() == [[0, 1, -1, -1], [0, 1, -1, -1], [-1] * 4] and c.t["refs"].tolist()[:3] == [2, 2, 0]
+    # row 0 loses its second page's tokens by its length alone; its next token must not go into what row 1 still has
+    assert _fork(c, [0], [0], [T], [2 * T], True) == ""
+    assert c.t["table"].tolist() == [[0, 2, -1, -1], [0, 1, -1, -1], [-1] * 4] and c.t["refs"].tolist()[:4] == [2, 1, 1, 0]
+    child = {n: c.t[n][:, 1].clone() for n in ("k8", "v8", "k_scale", "v_scale")}
+    _write(c, [T + 1], [1], layer=1, refs=with_refs)
+    c.same()
+    assert all(torch.equal(c.t[n][:, 1], x) for n, x in child.items())
+
+
+def test_growth_of_rows_set_back_further():
+    T = 16
+    c = Cache(12, T, 1, 6, 6, seed=4, junk=False)
+    assert _fork(c, [-1], [0], [0], [5 * T], True) == ""
+    assert _fork(c, [0, 0, 0], [1, 2, 3], [5 * T] * 3, [5 * T] * 3, True) == ""
+    # several rows at once: at a border, inside a page, at the begin, at the end of what the row holds
+    assert _fork(c, [0, 1, 2, 3], [0, 1, 2, 3], [2 * T, 2 * T + 5, 0, 5 * T], [2 * T + 1, 6 * T, 1, 6 * T], True) == ""
+    assert c.t["table"][:4].tolist() == [[0, 1, 5, 3, 4, -1], [0, 1, 6, 3, 4, 7], [8, 1, 2, 3, 4, -1], [0, 1, 2, 3, 4, 9]]
+    assert c.t["refs"].tolist() == [3, 4, 2, 4, 4, 1, 1, 1, 1, 1, 0, 0]
+    # pages of one's own stay; the length may stay as well
+    assert _fork(c, [0, 2], [0, 2], [2 * T, 5], [2 * T, 5], True) == ""
+    assert c.t["table"][:3:2].tolist() == [[0, 1, 5, 3, 4, -1], [8, 1, 2, 3, 4, -1]]
+    # both owners of a page at once: each gets one
+    _free(c, [1, 2])
+    assert _fork(c, [0, 3], [0, 3], [3 * T, 3 * T], [3 * T + 1] * 2, True) == ""
+    assert _fork(c, [-1], [4], [0], [4 * T], True) == ""
+    # a page more is needed than there is: nothing changes
+    assert _fork(c, [0], [0], [T], [5 * T], True) == "pages"

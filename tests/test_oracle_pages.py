@@ -60,3 +60,16 @@ def test_fork_free_compact_by_hand():
     assert p.fork([2], [2], [20], [48], True) == ""          # page 1 is shared and only part of it kept
     assert table[2].tolist() == [0, 2, 5, -1] and refs.tolist() == [2, 1, 1, 0, 0, 1, 0, 0] and data[0, 2] == 1.0
     assert p.compact() == 4 and table[2].tolist() == [0, 2, 3, -1] and refs.tolist() == [2, 1, 1, 1, 0, 0, 0, 0] and data[0, 3] == 5.0
+
+
+def test_growth_replaces_the_page_of_the_next_token_by_hand():
+    table, refs = np.full((3, 3), -1, np.int32), np.zeros(4, np.int32)
+    data = np.arange(4.0).reshape(1, 4)
+    p = O.Pool(table, refs, 16, [data])
+    assert p.fork([-1], [0], [0], [32], True) == "" and p.fork([0], [1], [32], [32], True) == ""
+    assert p.fork([0], [0], [32], [32], True) == "" and table[0].tolist() == [0, 1, -1]       # its next token has no page yet
+    assert p.fork([0], [0], [16], [32], True) == ""          # set back to a border: token 16 would go into row 1's page
+    assert table.tolist() == [[0, 2, -1], [0, 1, -1], [-1] * 3] and refs.tolist() == [2, 1, 1, 0] and data[0, 2] == 1.0
+    assert p.fork([0], [0], [16], [32], True) == "" and table[0].tolist() == [0, 2, -1]       # its own now
+    assert p.fork([1], [1], [0], [1], True) == ""
+    assert table[1].tolist() == [3, 1, -1] and refs.tolist() == [1, 1, 1, 1]
