@@ -423,8 +423,8 @@ int daf_page_attn(const daf_page_params* p, int32_t layer, int32_t n, const int3
                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* Gives sequences pages.  Item i (int32 device arrays of n):
- *   src[i] >= 0, another row   row dst[i], which must hold no pages, becomes a copy of the first keep[i] tokens of row src[i], with
- *                              pages for want[i] tokens.  Pages held whole are shared (share != 0: same page, refs + 1) or copied
+ *   src[i] >= 0, another row   row dst[i], which must hold no pages, becomes a copy of the first keep[i] tokens of row src[i], which
+ *                              must have pages of the pool for all of them, with pages for want[i] tokens.  Pages held whole are shared (share != 0: same page, refs + 1) or copied
  *                              in every layer; a page of which only a part is kept is always copied.
  *   src[i] < 0                 row dst[i], which must hold no pages, gets pages for want[i] tokens (keep is not read)
  *   src[i] == dst[i]           the row grows to pages for want[i] tokens.  keep[i] is its length now: the page its next token

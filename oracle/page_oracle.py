@@ -144,7 +144,9 @@ class Pool:
                 return "bounds"
             held = -(-kp // T)
             have = int((self.table[d] >= 0).sum())
-            if (s == d and held > have) or (s != d and have > 0) or (s >= 0 and s != d and held and self.table[s, held - 1] < 0):
+            if (s == d and held > have) or (s != d and have > 0) or (s >= 0 and s != d and not all(0 <= e < P for e in self.table[s, :held])):
+                return "bounds"
+            if s == d and kp // T < have and not 0 <= self.table[d, kp // T] < P:
                 return "bounds"
         free = [p for p in range(P) if self.refs[p] == 0]
         refs0 = self.refs.copy()

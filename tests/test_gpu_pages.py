@@ -947,3 +947,45 @@ def test_growth_of_rows_set_back_further():
     assert _fork(c, [-1], [4], [0], [4 * T], True) == ""
     # a page more is needed than there is: nothing changes
     assert _fork(c, [0], [0], [T], [5 * T], True) == "pages"
+
+
+@pytest.mark.parametrize("share", [True, False])
+@pytest.mark.parametrize("hole", [-1, -7, 40, 10 ** 9])
+def test_a_source_row_with_a_hole_changes_nothing(hole, share):
+    c = Cache(40, 16, 2, 8, 12, n_layers=2, seed=6, junk=False)
+    for s in (0, 1):
+        c.give(s, 150, up=False)
+    c.np["table"][0, 4] = hole
+    c.up()
+    for src, dst, keep, want in (([0], [2], [150], [160]), ([0], [2], [80], [80]), ([0], [2], [65], [65]), ([1, 0, 1], [2, 3, 4], [20, 130, 3], [40, 130, 3])):
+        assert _fork(c, src, dst, keep, want, share) == "bounds", (src, keep)
+    # what lies behind the kept tokens does not count
+    assert _fork(c, [0, 1], [2, 3], [64, 150], [70, 160], share) == ""
+    # a row that grows: the page its next token goes into counts
+    if hole > 0:
+        assert _fork(c, [0], [0], [66], [70], True) == "bounds"
+        assert _fork(c, [0], [0], [64], [70], True) == "bounds"
+
+
+@pytest.mark.parametrize("at", [0, 31, 255, 256, 300, 698])
+def test_a_hole_anywhere_in_long_rows_of_many_items(at):
+    c = Cache(1500, 16, 1, 60, 700, seed=7, junk=False)
+    c.give(0, 699 * 16, up=False)
+    c.give(1, 699 * 16, up=False)
+    c.np["table"][1, at] = -1 if at < 300 else 1500
+    c.up()
+    n = 50
+    assert _fork(c, [0] * (n - 1) + [1], list(range(2, n + 2)), [699 * 16] * n, [699 * 16] * n, True) == "bounds"
+    assert _fork(c, [0] * n, list(range(2, n + 2)), [699 * 16] * n, [699 * 16 + 1] * n, True) == ""
+
+
+def test_a_hole_that_only_some_of_a_rows_items_keep():
+    c = Cache(60, 16, 1, 12, 10, seed=8, junk=False)
+    c.give(0, 150, up=False)
+    c.np["table"][0, 7] = -1
+    c.up()
+    for keep in ([60, 40, 130, 20], [130, 20, 20, 20], [20, 20, 20, 113], [20, 130, 140, 150]):
+        assert _fork(c, [0] * 4, [2, 3, 4, 5], keep, keep, True) == "bounds", keep
+    # an item before that keeps more, but is none of a row's sources, covers nothing
+    assert _fork(c, [-1, 0], [2, 3], [150, 120], [10, 120], True) == "bounds"
+    assert _fork(c, [0] * 4, [2, 3, 4, 5], [112, 40, 112, 20], [112, 112, 112, 112], True) == ""
