@@ -398,47 +398,78 @@ def alloc_page_workspace(p: daf_page_params, n: int, L_q: int = 0, n_q_heads: in
     return torch.zeros(size, dtype=torch.uint8, device=device)
 
 
-def _page_workspace(workspace):
-    """Address and size, once it is sure that the call's tensors can be on the current device, where its kernels run."""
-    if workspace is not None and torch.cuda.is_initialized() and workspace.get_device() != torch._C._cuda_getDevice():
+# What the daf_page_* calls read a tensor as: one element type, or raw bytes.
+_INT, _ROW, _BYTE, _SCALE, _RAW = torch.int32, torch.bfloat16, torch.float8_e4m3fn, torch.float32, torch.uint8
+_POOL = (_BYTE, _BYTE, _SCALE, _SCALE)
+
+
+_data_ptr, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.get_device, torch.Tensor.is_contiguous
+
+
+def _page_ptrs(kinds, tensors, workspace, stream):
+    """The tensors' addresses, then the workspace's address and size and the stream.  An int64 tensor, say, would be read as twice as
+    many int32 numbers, and another device's memory or pageable host memory would fault in the kernels, which run on the current
+    device.  (The checks cost 0.1 us of host time a tensor: a token of 64 sequences written call by call
+    9.7 -> 10.8 us.)"""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1      # (-1: there are CPU tensors only)
+    out = [None if t is None else
+           _data_ptr(t) if ((dtype := t.dtype) is kind or dtype is _RAW) and _get_device(t) == dev and _is_contiguous(t) else
+           _page_ptr(kind, t, dev) for kind, t in zip(kinds, tensors)]
+    if workspace is not None and _get_device(workspace) != dev:
         raise ValueError("the workspace is not on the current device")
-    return _ptr(workspace), _nbytes(workspace)
+    out += (_ptr(workspace), _nbytes(workspace),
+            _raw_stream(dev) or None if stream is None and dev >= 0 and _raw_stream is not None else _stream(stream))
+    return out
+
+
+def _page_ptr(kind, t, dev) -> int:
+    """Says what is wrong with a tensor, or takes it after all: pinned host memory can be read where it is."""
+    if t.dtype is not kind and t.dtype is not _RAW:
+        raise ValueError(f"a tensor of {t.dtype} where the call reads {kind} elements")
+    if _get_device(t) != dev and not (t.device.type == "cpu" and t.is_pinned()):
+        raise ValueError("a tensor is not on the current device")
+    return _ptr(t)
+
+
+_WRITE = (_INT, _INT, _INT, _INT, _ROW, _ROW, _INT, _INT, *_POOL)
+_READ = (_INT, _INT, _INT, _INT, *_POOL, _ROW, _ROW)
+_ATTN = (_INT, _INT, _ROW, _INT, *_POOL, _ROW, _SCALE)
+_FORK = (_INT, _INT, _INT, _INT, _INT, _INT, *_POOL)
+_FREE = (_INT, _INT, _INT, _INT)
+_COMPACT = (_INT, _INT, _INT, _INT, _INT, *_POOL)
 
 
 def daf_page_write(p, layer, n, seqs, lens, row_off, idx, max_rows, k, v, table, refs, k8, v8, k_scale, v_scale, workspace,
                    stream=None) -> int:
-    return lib().daf_page_write(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(lens), _ptr(row_off), _ptr(idx),
-                                int(max_rows), _ptr(k), _ptr(v), _ptr(table), _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale),
-                                _ptr(v_scale), *_page_workspace(workspace), _stream(stream))
+    a = _page_ptrs(_WRITE, (seqs, lens, row_off, idx, k, v, table, refs, k8, v8, k_scale, v_scale), workspace, stream)
+    return lib().daf_page_write(ctypes.byref(p), int(layer), int(n), *a[:4], int(max_rows), *a[4:])
 
 
 def daf_page_read(p, layer, n, seqs, first, row_off, max_rows, table, k8, v8, k_scale, v_scale, k_rows, v_rows, workspace,
                   stream=None) -> int:
-    return lib().daf_page_read(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(first), _ptr(row_off), int(max_rows),
-                               _ptr(table), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(k_rows), _ptr(v_rows),
-                               *_page_workspace(workspace), _stream(stream))
+    a = _page_ptrs(_READ, (seqs, first, row_off, table, k8, v8, k_scale, v_scale, k_rows, v_rows), workspace, stream)
+    return lib().daf_page_read(ctypes.byref(p), int(layer), int(n), *a[:3], int(max_rows), *a[3:])
 
 
 def daf_page_attn(p, layer, n, seqs, lens, L_q, n_q_heads, softmax_scale, q, table, k8, v8, k_scale, v_scale, out, lse,
                   workspace, stream=None) -> int:
-    return lib().daf_page_attn(ctypes.byref(p), int(layer), int(n), _ptr(seqs), _ptr(lens), int(L_q), int(n_q_heads),
-                               float(softmax_scale), _ptr(q), _ptr(table), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale),
-                               _ptr(out), _ptr(lse), *_page_workspace(workspace), _stream(stream))
+    a = _page_ptrs(_ATTN, (seqs, lens, q, table, k8, v8, k_scale, v_scale, out, lse), workspace, stream)
+    return lib().daf_page_attn(ctypes.byref(p), int(layer), int(n), *a[:2], int(L_q), int(n_q_heads), float(softmax_scale), *a[2:])
 
 
 def daf_page_fork(p, n, src, dst, keep, want, share, table, refs, k8, v8, k_scale, v_scale, workspace, stream=None) -> int:
-    return lib().daf_page_fork(ctypes.byref(p), int(n), _ptr(src), _ptr(dst), _ptr(keep), _ptr(want), int(bool(share)), _ptr(table),
-                               _ptr(refs), _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), *_page_workspace(workspace), _stream(stream))
+    a = _page_ptrs(_FORK, (src, dst, keep, want, table, refs, k8, v8, k_scale, v_scale), workspace, stream)
+    return lib().daf_page_fork(ctypes.byref(p), int(n), *a[:4], int(bool(share)), *a[4:])
 
 
 def daf_page_free(p, n, seqs, keep, table, refs, workspace, stream=None) -> int:
-    return lib().daf_page_free(ctypes.byref(p), int(n), _ptr(seqs), _ptr(keep), _ptr(table), _ptr(refs), *_page_workspace(workspace), _stream(stream))
+    a = _page_ptrs(_FREE, (seqs, keep, table, refs), workspace, stream)
+    return lib().daf_page_free(ctypes.byref(p), int(n), *a)
 
 
 def daf_page_compact(p, table, refs, table_out, refs_out, live_out, k8, v8, k_scale, v_scale, workspace, stream=None) -> int:
-    return lib().daf_page_compact(ctypes.byref(p), _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(live_out),
-                                  _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), *_page_workspace(workspace),
-                                  _stream(stream))
+    a = _page_ptrs(_COMPACT, (table, refs, table_out, refs_out, live_out, k8, v8, k_scale, v_scale), workspace, stream)
+    return lib().daf_page_compact(ctypes.byref(p), *a)
 
 
 def daf_poll_status(workspace, stream=None) -> int:

@@ -192,3 +192,63 @@ def test_nothing_to_do_is_ok_and_launches_nothing():
 
 def test_status_text():
     assert "free pages" in api.daf_strerror(api.DAF_ERR_PAGES)
+
+
+INTS, ROWS, BYTES, FLOATS = "int32", "bfloat16", "float8_e4m3fn", "reads torch.float32 elements"
+READ_AS = [("write", n, t) for n, t in (("lens", INTS), ("row_off", INTS), ("table", INTS), ("k", ROWS), ("v", ROWS), ("k8", BYTES), ("v8", BYTES),
+                                        ("k_scale", FLOATS), ("v_scale", FLOATS))]
+READ_AS += [("read", n, t) for n, t in (("row_off", INTS), ("table", INTS), ("k", ROWS), ("v", ROWS), ("v8", BYTES), ("k_scale", FLOATS))]
+READ_AS += [("attn", n, t) for n, t in (("lens", INTS), ("table", INTS), ("q", ROWS), ("out", ROWS), ("k8", BYTES), ("v_scale", FLOATS))]
+READ_AS += [("fork", n, t) for n, t in (("src", INTS), ("dst", INTS), ("keep", INTS), ("want", INTS), ("table", INTS), ("refs", INTS), ("v8", BYTES), ("k_scale", FLOATS))]
+READ_AS += [("free", n, INTS) for n in ("seqs", "table", "refs")]
+READ_AS += [("compact", n, t) for n, t in (("table", INTS), ("refs", INTS), ("table_out", INTS), ("refs_out", INTS), ("k8", BYTES), ("v_scale", FLOATS))]
+WRONG = {INTS: (torch.int64, torch.float32, torch.int16), ROWS: (torch.float32, torch.float16), BYTES: (torch.bfloat16, torch.float8_e5m2),
+         FLOATS: (torch.float64, torch.bfloat16, torch.int32)}
+RIGHT = {INTS: torch.int32, ROWS: torch.bfloat16, BYTES: torch.float8_e4m3fn, FLOATS: torch.float32}
+
+
+@pytest.mark.parametrize("call,name,kind", READ_AS)
+def test_tensors_of_other_types_are_refused(call, name, kind):
+    """(n is 0 for those that are taken: nothing is launched.)"""
+    p, b = _params(), _buf(1 << 16)
+    ws = _buf(api.daf_page_workspace_bytes(p, 4, 1, 4))
+    c = _calls(p, b, ws)[call]
+    for t in WRONG[kind]:
+        with pytest.raises(ValueError, match=kind):
+            c(**{name: b[:1024].view(t)})
+    if call != "compact":
+        assert c(n=0, **{name: b[:1024].view(RIGHT[kind])}) == api.DAF_OK
+
+
+@pytest.mark.parametrize("call,name,kind", READ_AS)
+def test_each_tensor_has_to_be_on_the_current_device(call, name, kind, monkeypatch):
+    p, b = _params(), _buf(1 << 16)
+    ws = _buf(api.daf_page_workspace_bytes(p, 4, 1, 4))
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)       # (where CPU tensors say that they are)
+    elsewhere = _buf(1 << 16)
+    monkeypatch.setattr(api, "_get_device", lambda t: 1 if t is elsewhere else -1)
+    c = _calls(p, b, ws)[call]
+    if call != "compact":
+        monkeypatch.setattr(api, "_raw_stream", lambda device: 0)
+        assert c(n=0) == api.DAF_OK
+    for which in (name, "workspace"):
+        with pytest.raises(ValueError, match="current device"):
+            c(**{which: elsewhere})
+
+
+def test_tensors_that_may_be_left_out_are_checked_as_well():
+    p, b = _params(), _buf(1 << 16)
+    ws = _buf(api.daf_page_workspace_bytes(p, 4, 1, 4))
+    pool, w = (b, b, b, b), b[:64].view(torch.int64)
+    for call in (lambda: api.daf_page_write(p, 0, 0, w, b, b, None, 1, b, b, b, None, *pool, ws),
+                 lambda: api.daf_page_write(p, 0, 0, None, b, b, w, 1, b, b, b, None, *pool, ws),
+                 lambda: api.daf_page_write(p, 0, 0, None, b, b, None, 1, b, b, b, w, *pool, ws),
+                 lambda: api.daf_page_read(p, 0, 0, w, None, b, 1, b, *pool, b, b, ws),
+                 lambda: api.daf_page_read(p, 0, 0, None, w, b, 1, b, *pool, b, b, ws),
+                 lambda: api.daf_page_attn(p, 0, 0, w, b, 1, 4, 0.0, b, b, *pool, b, None, ws),
+                 lambda: api.daf_page_attn(p, 0, 0, None, b, 1, 4, 0.0, b, b, *pool, b, w, ws),
+                 lambda: api.daf_page_free(p, 0, b, w, b, b, ws),
+                 lambda: api.daf_page_compact(p, b, b, b, b, w, *pool, ws)):
+        with pytest.raises(ValueError, match="int64"):
+            call()

@@ -989,3 +989,18 @@ def test_a_hole_that_only_some_of_a_rows_items_keep():
     # an item before that keeps more, but is none of a row's sources, covers nothing
     assert _fork(c, [-1, 0], [2, 3], [150, 120], [10, 120], True) == "bounds"
     assert _fork(c, [0] * 4, [2, 3, 4, 5], [112, 40, 112, 20], [112, 112, 112, 112], True) == ""
+
+
+def test_host_memory_is_refused_unless_it_is_pinned():
+    lens = [100, 40]
+    c = _cache_for(lens, 16, 2, seed=64, junk=False)
+    want, _ = _attend(c, lens, 1, 4, check=False)
+    q = torch.randn(2, 1, 4, 128, generator=torch.Generator().manual_seed(100)).to(torch.bfloat16).to(DEV)
+    out, ws = torch.zeros_like(q), _ws(c, 2, 1, 4)
+    host = torch.tensor(lens, dtype=torch.int32)
+    with pytest.raises(ValueError, match="current device"):
+        api.daf_page_attn(c.p, 0, 2, None, host, 1, 4, 0.0, q, c.t["table"], *c.pool(), out, None, ws)
+    with pytest.raises(ValueError, match="int64"):
+        api.daf_page_attn(c.p, 0, 2, None, _i32(lens).long(), 1, 4, 0.0, q, c.t["table"], *c.pool(), out, None, ws)
+    api.check(api.daf_page_attn(c.p, 0, 2, None, host.pin_memory(), 1, 4, 0.0, q, c.t["table"], *c.pool(), out, None, ws))
+    assert api.daf_poll_status(ws) == api.DAF_OK and np.array_equal(out.float().cpu().numpy(), want)
