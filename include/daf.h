@@ -363,7 +363,9 @@ int64_t daf_launch_count(void);
  *   k8, v8            bytes [n_layers, n_pages, n_kv_heads, page_tokens, 128], the 8-bit format of daf_expand_fp8_cache
  *                     (1 sign, 4 exponent, 3 mantissa bits, no infinities, 0x7f and 0xff are NaN)
  *   k_scale, v_scale  fp32 [n_layers, n_pages, n_kv_heads]: an element is worth scale * value.  daf_page_write leaves powers of
- *                     two of at least 2^-60 here; the calls that read take any positive normal number.
+ *                     two of at least 2^-60 here; the calls that read take any positive normal number, but daf_page_attn wants
+ *                     V's between 2^-60 and 2^30 (elements of up to 4.8e11) and records others (DAF_ERR_BOUNDS): further
+ *                     apart, sums lose the tokens of small scales
  *   table             int32 [n_seqs, max_pages]: page j of a sequence holds its tokens j * page_tokens and on.  Behind a
  *                     sequence's last page: -1.
  *   refs              int32 [n_pages]: how many entries of `table` name the page; 0: the page is free

@@ -58,6 +58,8 @@ struct ChainEntry {
 //   2^14 .. 2^15 (elements 2^-31 of that and below are rounded), so the logits are products of the given numbers with fp32 sums.
 //   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
 //   largest and some bits down to 2^-34 (as bf16 it would have 8), while sums of p stay in fp32.
+//   Maxima are those of p * 2^floor(log2 vs), and what is 2^-126 of one is flushed, from the sum of p too.  With V's scales at most
+//   2^90 apart, as the header asks, such a token's p is below 2^-36 of another's: four million of them are 2^-14 of a sum.
 constexpr int kStep = 32;
 constexpr int kMostBlocks = 3;                       // column blocks of eight rows
 constexpr int kTile = kStep * kD;                    // 4 KB: K or V of one step
@@ -127,6 +129,9 @@ __device__ __forceinline__ uint32_t finite_top(uint32_t w) {
     const uint32_t b0 = w & 0x7FFFu, b1 = (w >> 16) & 0x7FFFu;
     return max(b0 < 0x7F80u ? b0 : 0u, b1 < 0x7F80u ? b1 : 0u);
 }
+
+// Whether a page's V scale is one that the sums of p can take (see above); -1 stands for no page.
+__device__ __forceinline__ bool sums_take(float vs) { return (vs >= 0x1p-60f && vs <= 0x1p30f) || vs == -1.f; }
 
 // A place on the work axis: a segment is (b, h, block), a block `width` tiles (kW, or one less in the last).  It takes a.pad places, for
 // what it costs beyond its steps, and weight<kW>(width) places for each of them.
@@ -560,6 +565,7 @@ page_decode_kernel(const PageAttnArgs a) {
             __syncwarp();
             const DecodeStage sc = sc_ring[slot];
             const int key0 = at.step * kStep;
+            if (!(sums_take(sc.vs[0]) && sums_take(sc.vs[1])) && lane == 0) report_status(a.status, DAF_ERR_BOUNDS, 253, at.b);
             if (key0 + kStep - 1 > first_limit || sc.ks[0] < 0.f || sc.ks[1] < 0.f) step(std::integral_constant<bool, true>{}, key0, sc);
             else step(std::integral_constant<bool, false>{}, key0, sc);
             __syncwarp();          // every lane is done with the slot
@@ -794,7 +800,8 @@ __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t 
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // A row's factor for the logits of a chunk.  It stays a normal number: with rows of zeros or nearly so and keys of a small scale the product
-// would be flushed to zero, and hidden logits, which are -inf ahead of it, would become NaN.  (Visible logits are below 2^32 ahead of it: times this bound they are nothing.)
+// would be flushed to zero, and hidden logits, which are -inf ahead of it, would become NaN.  (Visible logits are below 2^32 ahead of
+// it: times this bound they are nothing.)
 __device__ __forceinline__ float logit_factor(float c, float ks) { return fmaxf(c * fabsf(ks), FLT_MIN); }
 
 // One softmax step of one row over 128 keys: P over the first half of the logits' columns, running maximum and sum.  `rescale` is called
@@ -1283,6 +1290,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                         if (kv == 0) {
                             ks = ids >= 0 ? __ldg(a.p.k_scale + (size_t)ids * Hkv + h) : -1.f;
                             vs = ids >= 0 ? __ldg(a.p.v_scale + (size_t)ids * Hkv + h) : -1.f;
+                            if (!sums_take(vs)) report_status(a.status, DAF_ERR_BOUNDS, 253, sm->at.b);
                         }
                     }
                     const int at0 = page0 - (ids_end - 32);

@@ -1004,3 +1004,34 @@ def test_host_memory_is_refused_unless_it_is_pinned():
         api.daf_page_attn(c.p, 0, 2, None, _i32(lens).long(), 1, 4, 0.0, q, c.t["table"], *c.pool(), out, None, ws)
     api.check(api.daf_page_attn(c.p, 0, 2, None, host.pin_memory(), 1, 4, 0.0, q, c.t["table"], *c.pool(), out, None, ws))
     assert api.daf_poll_status(ws) == api.DAF_OK and np.array_equal(out.float().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("L_q", [1, 6, 7, 70])
+@pytest.mark.parametrize("q_scale", [1.0, 25.0])
+def test_value_scales_at_the_ends_of_their_range(L_q, q_scale):
+    lens = [700, 129, 2000]
+    c = _cache_for(lens, 16, 2, seed=63, junk=False)
+    ends = np.array([2.0 ** -60, 2.0 ** 30], np.float32)
+    c.np["v_scale"][:] = ends[np.random.default_rng(1).integers(0, 2, c.np["v_scale"].shape)]
+    c.up()
+    _attend(c, lens, L_q, 8, q_scale=q_scale)
+    for end in ends:                                       # ... and all alike
+        c.np["v_scale"][:] = end
+        c.up()
+        _attend(c, lens, L_q, 8, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("L_q", [1, 6, 7, 70])
+@pytest.mark.parametrize("bad", [2.0 ** -61, 2.0 ** 31, 1.01 * 2.0 ** 30, 0.0, -2.0, math.inf, math.nan])
+def test_value_scales_outside_their_range_are_reported(L_q, bad):
+    lens = [200, 90, 33]
+    c = _cache_for(lens, 16, 2, seed=65, junk=False)
+    good = c.np["v_scale"].copy()
+    for seq, page, head in ((0, 0, 0), (0, 12, 1), (1, 3, 0), (2, 2, 1)):
+        c.np["v_scale"][:] = good
+        c.np["v_scale"][0, c.np["table"][seq, page], head] = bad
+        c.up()
+        _attend(c, lens, L_q, 8, status=api.DAF_ERR_BOUNDS, check=False)
+        # where nobody sees the page it does not count
+        shorter = [min(L, 16 * page) if b == seq else L for b, L in enumerate(lens)]
+        _attend(c, shorter, L_q, 8, check=False)
