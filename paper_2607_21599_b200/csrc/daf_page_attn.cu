@@ -729,6 +729,10 @@ page_decode_kernel(const PageAttnArgs a) {
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 128, kQSub = 64;
 constexpr int kQStages = 3;        // half steps
+// Barriers of their bytes: twice as many, so that each belongs to one of the two pairs of warps that widen half steps in turn.  With one
+// a slot a pair would see every other of its phases only, and where the other pair's bytes were late take its parity for that of its own.
+constexpr int kQFull = 2 * kQStages;
+static_assert(kQFull % 2 == 0 && kQFull % kQStages == 0, "a barrier's half steps all have one slot and one pair");
 // Places (a step of two tiles takes three) that a piece of work costs: rows of Q in, results out.  128 tokens of 28 / 4 heads over 32k
 // keys with 8 or 16: 86.4 us, with 12: 85.0.
 constexpr int kQPad = 12;
@@ -747,7 +751,7 @@ constexpr float kLazy = 6.f;                          // log2: a row's maximum m
 constexpr int kQOffV = 2 * kQTile, kQOffK = kQOffV + 2 * kQSlot, kQOffStage = kQOffK + 2 * kQTile;
 
 struct QuestionSmem {
-    uint64_t st_full[2][kQStages], st_empty[2][kQStages];     // [K, V] the bytes of half a step
+    uint64_t st_full[2][kQFull], st_empty[2][kQStages];       // [K, V] the bytes of half a step, there and taken
     uint64_t k_full[2], k_empty[2];                           // [buffer] a step's K, widened
     uint64_t v_full[4], v_empty[4];                           // [slot] half a step's V, widened
     uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2];   // [group], [half]
@@ -774,7 +778,7 @@ constexpr int kBarStEmpty = (int)(offsetof(QuestionSmem, st_empty) / 8), kBarK =
               kBarS = (int)(offsetof(QuestionSmem, s_full) / 8), kBarP = (int)(offsetof(QuestionSmem, p_full) / 8),
               kBarO = (int)(offsetof(QuestionSmem, o_full) / 8), kBarTurn = (int)(offsetof(QuestionSmem, turn) / 8),
               kBarC = (int)(offsetof(QuestionSmem, c_full) / 8), kBars = kBarC + kQConsts;
-static_assert(offsetof(QuestionSmem, st_full) == 0 && kBarK % kQStages == 0 && kBarK % 2 == 0 && kBarS % 2 == 0 && kBarO % 2 == 0 && kBars <= 64, "what the barriers' numbers rest on");
+static_assert(offsetof(QuestionSmem, st_full) == 0 && kBarStEmpty == 2 * kQFull && kBarStEmpty % kQStages == 0 && kBarK % 2 == 0 && kBarS % 2 == 0 && kBarO % 2 == 0 && kBars <= 64, "what the barriers' numbers rest on");
 constexpr size_t kQuestionSmem = 1024 + kQOffStage + 2 * (size_t)kQStages * kQStage + sizeof(QuestionSmem);
 
 __host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_t N, uint32_t b_mn_major) {
@@ -885,7 +889,8 @@ __device__ __forceinline__ void question_softmax(uint32_t s_addr, const float4* 
 
 // How many phases barrier i completes in a piece of n_t steps.
 __device__ __forceinline__ int bar_uses(int i, int n_t, bool pair) {
-    if (i < kBarK) return (2 * n_t - i % kQStages + kQStages - 1) / kQStages;      // every third half step
+    if (i < kBarStEmpty) return (2 * n_t - i % kQFull + kQFull - 1) / kQFull;      // every sixth half step
+    if (i < kBarK) return (2 * n_t - i % kQStages + kQStages - 1) / kQStages;      // every third
     if (i < kBarV) return (n_t - (i & 1) + 1) >> 1;
     if (i < kBarQ) {
         const int slot = (i - kBarV) & 3;
@@ -1270,13 +1275,14 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                 const int page_bits = 31 - __clz(T), box = min(T, kQSub), pages = kQSub / box;        // copies of half a step
                 const int chunk_page = box < kQSub ? ((lane & 3) * 16) >> page_bits : 0;             // page of a chunk of 16 keys
                 int ids = -1, ids_end = 0;          // page numbers of 32 pages that end in front of ids_end, one a lane
-                for (int t = 0; t < 2 * n_t && ok; ++t) {      // (t counts half steps here)
+                int t = 0;
+                for (; t < 2 * n_t; ++t) {      // (t counts half steps here)
                     const int slot = t % kQStages;
                     if (t >= kQStages) {
                         ok = __all_sync(0xFFFFFFFFu, wait_phase(sm, odd, &sm->st_empty[kv][slot], (uint32_t)((t / kQStages - 1) & 1), abort, 260));
                         if (!ok) break;
                     }
-                    uint64_t* const full = &sm->st_full[kv][slot];
+                    uint64_t* const full = &sm->st_full[kv][t % kQFull];
                     const int key0 = step0 * kQStep + t * kQSub, page0 = key0 >> page_bits;
                     if (page0 + pages > ids_end) {
                         ids_end = page0 + 32;
@@ -1317,8 +1323,11 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     }
                 }
                 if (!ok)       // loads in flight get a bounded chance to land before the CTA retires
-                    for (int i = 0; i < kQStages && lane == 0; ++i)
-                        for (int k = 0; k < 4096 && !mbar_try_wait(&sm->st_full[kv][i], 0) && !mbar_try_wait(&sm->st_full[kv][i], 1); ++k) {}
+                    for (int i = max(0, t - kQStages); i < t; ++i) {
+                        uint64_t* const full = &sm->st_full[kv][i % kQFull];
+                        const uint32_t parity = (uint32_t)((i / kQFull) & 1) ^ ((uint32_t)(odd >> ((smem_u32(full) - smem_u32(sm)) >> 3)) & 1u);
+                        for (int k = 0; k < 4096 && !mbar_try_wait(full, parity); ++k) {}
+                    }
             } else if (warp >= 12) {
                 // --------------------------------------------------------------------------------------------------- widening
                 // Two warps take a half step, the other two the next one: each half step is a chain of waits, reads, conversions, writes and
@@ -1334,7 +1343,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     const int step = t >> 1, slot = kv == 0 ? step & 1 : pair ? t & 1 : t & 3, uses = kv == 0 || !pair ? step >> 1 : step;
                     // one of the two warps polls, the other sleeps at a barrier (twelve polling warps took half of the issue slots)
                     if ((warp & 1) == 0) {
-                        bool there = wait_phase(sm, odd, &sm->st_full[kv][t % kQStages], (uint32_t)((t / kQStages) & 1), abort, 262);
+                        bool there = wait_phase(sm, odd, &sm->st_full[kv][t % kQFull], (uint32_t)((t / kQFull) & 1), abort, 262);
                         if (kv == 1 && there) there = wait_phase(sm, odd, &sm->c_full[t % kQConsts], (uint32_t)((t / kQConsts) & 1), abort, 275);
                         if (there && step == 0 && (kv == 0 || !pair)) {      // the raw rows of Q are out of K's buffers, the second tile is idle
                             there = wait_phase(sm, odd, &sm->q_full[0], 0, abort, 276);

@@ -1035,3 +1035,27 @@ def test_value_scales_outside_their_range_are_reported(L_q, bad):
         # where nobody sees the page it does not count
         shorter = [min(L, 16 * page) if b == seq else L for b, L in enumerate(lens)]
         _attend(c, shorter, L_q, 8, check=False)
+
+
+@pytest.mark.parametrize("n,L_q,Hq,Hkv,T,lo,hi", [(10, 15, 40, 8, 32, 964, 10986), (16, 7, 40, 8, 32, 2049, 3689), (12, 64, 16, 2, 16, 300, 6000),
+                                                  (40, 30, 8, 4, 128, 0, 700), (3, 130, 28, 4, 64, 500, 9000)])
+def test_many_launches_give_the_same_bits(n, L_q, Hq, Hkv, T, lo, hi):
+    """Pieces of work in whatever order their bytes arrive: after a write to the workspace, after other data in L2, back to back."""
+    rng = random.Random(n)
+    c = _cache_for([rng.randint(lo, hi) for _ in range(n)], T, Hkv, seed=66, junk=False)
+    lens = _i32([int((c.np["table"][s] >= 0).sum()) * T - rng.randint(0, T - 1) if c.np["table"][s, 0] >= 0 else 0 for s in range(n)])
+    q = torch.randn(n, L_q, Hq, 128, generator=torch.Generator().manual_seed(7)).to(torch.bfloat16).to(DEV)
+    ws, other = _ws(c, n, L_q, Hq), torch.empty(64 << 20, device=DEV)
+    first = None
+    for i in range(120):
+        if i % 3 == 1:
+            ws[256:].random_(0, 255)
+        if i % 3 == 2 and i < 60:
+            other.fill_(i)
+        out, lse = torch.full_like(q, 7.0), torch.full((n, Hq, L_q), 7.0, device=DEV)
+        api.check(api.daf_page_attn(c.p, 0, n, None, lens, L_q, Hq, 0.0, q, c.t["table"], *c.pool(), out, lse, ws))
+        if first is None:
+            first = out, lse
+            continue
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), (i, (out != first[0]).any(-1).nonzero()[:3].tolist())
+    assert api.daf_poll_status(ws) == api.DAF_OK
