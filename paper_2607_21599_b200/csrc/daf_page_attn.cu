@@ -984,6 +984,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             sm->shares = shares;
             sm->chain = ChainEntry{-1, 0, 0, 0};
         }
+        __syncwarp();          // (lane 0 goes on with what lane 1 found)
     }
     // Three of the five warpgroups need few registers: 256 x 144 + 384 x 64 = 640 x 96
     if (warp < 8) {
