@@ -49,11 +49,11 @@ struct ChainEntry {
 // copies into a ring of its own, whose 16-byte pieces are XOR-ed with the row number so that eight rows of a column lie in
 // different banks), multiplies, keeps the running maximum and sum, and multiplies again.  (Tiled copies were slower here: a warp has
 // to issue them one by one, with everything in uniform registers, and at pages of 16 tokens a step takes four: 1160 clocks a step.)
-//   Measured: one token of 64 sequences of 0.5k to 12k tokens, 32 / 8 heads, 141 us: 5.7 TB/s, 87 % of a copy's rate.  One token of 28 / 4
-// heads over 32k 13.7 us (5.2 at that rate) and over 1k 9.6: two launches and the chain lengths -> table -> bytes -> products -> merge,
-// of which every part runs once (11,000 clocks in this kernel).  One token (7 rows) of 16 sequences of 4k 17.7, two (14) 25.2, three (21)
-// 33.4: each eight rows more cost some 8 us of conversions and products in warps that are too few (two a scheduler) to cover their
-// latencies; with 12 warps of two column blocks 27.0, with 10 of three 48.0 (spills).
+//   Measured: one token of 64 sequences of 0.5k to 12k tokens, 32 / 8 heads, 142 us: 5.7 TB/s, 86 % of a copy's rate.  One token of 28 / 4
+// heads over 32k 13.8 us (5.2 at that rate) and over 1k 9.6: two launches and the chain lengths -> table -> bytes -> products -> merge,
+// of which every part runs once (11,000 clocks in this kernel).  One token (7 rows) of 16 sequences of 4k 17.9, two (14) 25.4, three (21)
+// 33.7: each eight rows more cost some 8 us of conversions and products in warps that are too few (two a scheduler) to cover their
+// latencies; with 12 warps of two column blocks 27.0, with 10 of three 48.0, each in fewer registers.
 //   8-bit values are exact in fp16, and so are the query rows once each is scaled by a power of two to a largest magnitude of
 //   2^14 .. 2^15 (elements 2^-31 of that and below are rounded), so the logits are products of the given numbers with fp32 sums.
 //   P goes into the product as fp16 of p * vs * 2^9 / (row maximum of p * 2^floor(log2 vs)): 11 bits down to 2^-23 of the
@@ -712,20 +712,21 @@ page_decode_kernel(const PageAttnArgs a) {
 // More than 24 rows of a KV head (a question, or a few speculated tokens of a large group) go through the tensor cores in tiles
 // of 128 consecutive rows, in steps of 128 keys.  One CTA per SM, 20 warps:
 //   10, 11  ask for the bytes of K and V (TMA, kQStages half steps ahead);
-//   12-15, 16-19  widen K's, and V's, to fp16, exactly, into the buffers that the products read (128-byte swizzle), half a step at a
-//          time.  Each of these is a chain of waits, reads, conversions and writes, so K and V have warps of their own;
+//   12-15, 16-19  widen K's, and V's, to fp16 into the buffers that the products read (128-byte swizzle), half a step at a time: exactly,
+//          but that V takes along what its scale is beside a power of two, rounded to fp16 (daf_page_write leaves none).  Each of
+//          these is a chain of waits, reads, conversions and writes, so K and V have warps of their own;
 //   8, 9   issue a tile group's products: S = Q K^T, O += P V with P from tensor memory, over S, by halves as they come;
 //   0-3, 4-7  a tile group's softmax, a row per thread, and its epilogue.
 // A block of two tiles shares every widened K and V.  A block of one tile gives its even steps to one group and its odd ones to the
 // other, and the two halves of the result are merged in shared memory.  A group's 256 columns of tensor memory are O and S, 128
 // each.  One S is enough because the groups take turns: while one's products run, the other's softmax does.
-//   Measured: 128 tokens of 28 / 4 heads over 32k keys 85.0 us, 708 TFLOP/s, 43 % of the measured bf16 rate; 4 tokens of 16 sequences of
-// 4k 38.8 (28 rows of a tile's 128), 64 tokens over 6k 29.7.  A step of both tiles takes some 5800 clocks, of which the tensor cores
+//   Measured: 128 tokens of 28 / 4 heads over 32k keys 86.6 us, 696 TFLOP/s, 42 % of the measured bf16 rate; 4 tokens of 16 sequences of
+// 4k 39.1 (28 rows of a tile's 128), 64 tokens over 6k 30.0.  A step of both tiles takes some 5800 clocks, of which the tensor cores
 // are busy for 2050; the rest is each group's chain: exponentials 2000 (the unit needs 1024 of them), maximum 550, P on its way 350,
-// products 1500 to 1800.  Leaving the exponentials or three quarters of Q K^T out of the kernel changed nothing, leaving the widening out
-// a tenth.  A piece of work costs some 15,000 clocks beside its steps.  What was measured on the way, same case: steps of 64 keys
-// with two S a group 114 us; with Q in tensor memory and one S 110; without turns 104 (92 with them then); turns that end before P's last
-// quarter 95 (87 then); 152 / 56 or 168 / 48 registers 87.
+// products 1500 to 1800.  A piece of work costs some 15,000 clocks beside its steps.  What was measured on the way, same case: steps of
+// 64 keys with two S a group 114 us; with Q in tensor memory and one S 110; without turns 104 (92 with them then; what could be left out
+// was measured on that form only: the exponentials or three quarters of Q K^T changed nothing, the widening a tenth); turns that end before
+// P's last quarter 95 (87 then); 152 / 56 or 168 / 48 registers 87 (85 then).
 // Rows of Q are scaled by powers of two and P enters the product as fp16 as in the kernel above.
 constexpr int kQStep = 128, kQSub = 64;
 constexpr int kQStages = 3;        // half steps
@@ -734,7 +735,7 @@ constexpr int kQStages = 3;        // half steps
 constexpr int kQFull = 2 * kQStages;
 static_assert(kQFull % 2 == 0 && kQFull % kQStages == 0, "a barrier's half steps all have one slot and one pair");
 // Places (a step of two tiles takes three) that a piece of work costs: rows of Q in, results out.  128 tokens of 28 / 4 heads over 32k
-// keys with 8 or 16: 86.4 us, with 12: 85.0.
+// keys with 8 or 16: 86.4 us, with 12: 85.0 (86.6 with twice the barriers for bytes).
 constexpr int kQPad = 12;
 constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
@@ -1692,7 +1693,7 @@ int launch_page_attn(const Pool& pool, int n, const int32_t* seqs, const int32_t
     if (e != cudaSuccess) { set_cuda_error(e); return DAF_ERR_CUDA; }
     // Few long segments leave many partials of a row: with four warps a row instead of one, 28 rows of 4 heads over 8k keys (37 partials)
     // take 18.1 us instead of 30.5 with the attention itself, 132 rows of 8 heads over 16k (18) 37.1 instead of 40.5.  Where there are
-    // more rows than warps one is better: 448 rows of 4 heads over 6k, 29.7 us against 31.0.
+    // more rows than warps one is better: 448 rows of 4 heads over 6k, 29.7 us against 31.0.  (The rule lies between these three.)
     const long long heads = (long long)n * pool.Hkv, segments = heads * ((a.rows + kQRows - 1) / kQRows);
     const bool four = ctas > 10 * segments && heads * a.rows <= 10 * ctas;
     e = few ? launch_kernel(page_merge_kernel<8, false>, dim3(ctas, a.rows), dim3(256), 0, stream, a, 8 * blocks, ctas)

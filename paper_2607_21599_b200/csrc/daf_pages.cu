@@ -71,7 +71,7 @@ __device__ __forceinline__ int first_at_least(const int32_t* idx, int a, int b, 
 // (sixteen lanes a row, eight elements each) while the CTA finds their largest magnitude; the rows then leave scaled.  Kept bytes are
 // touched only where the scale grows.  kGiven: positions come from a list, through a table in shared memory of which row a token
 // gets; otherwise the rows are the newest tokens, whose addresses need nothing but the length, and are asked for ahead of the page.
-//   Measured: a context of 16k tokens of 8 heads 21.3 us at 64 tokens a page (4.7 TB/s; a copy of as many bytes would take 15.4) and 26 at
+//   Measured: a context of 16k tokens of 8 heads 21.7 us at 64 tokens a page (4.6 TB/s; a copy of as many bytes would take 15.4) and 26 at
 // 16, where a CTA has 4 KB to fetch; a token of 64 sequences 3.4, a launch and the chain position -> page -> old scale -> bytes; every
 // fifth of 14k tokens 10.7, that chain with two more trips for the list.
 template <int kTokens, bool kGiven>
@@ -250,7 +250,8 @@ __global__ void __launch_bounds__(128) page_read_kernel(const ReadArgs a) {
 // prefix sums over items and over refs, then a grid does what was decided: table, refs and the bytes.  Copies of some 250 MB run at 5.4 to
 // 5.8 TB/s (82 to 88 % of a copy's rate); of few pages the decision is what counts: some 5 us of dependent loads and
 // scans in one CTA.  Its warps look at refs a word of 32 pages at a time, one ballot each, and share all pages evenly: eight answers over
-// a context 12.3 us, compacting 700 pages 7.5; with 512 neighbouring pages a warp whatever their number 13.8 and 11.7.
+// a context 12.5 us, compacting 700 pages 7.4; with 512 neighbouring pages a warp whatever their number 13.8 and 11.7.  Rows that grow by a
+// token: 6.0 us for one or eight, 8.2 for 64, where none needs a page (7.1 and 9.5 where each does).
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanRefs = 16;            // words of 32 pages that a warp looks at per round at most: 16k pages a round
 constexpr int kPlanRound = kPlanThreads * kPlanRefs;
