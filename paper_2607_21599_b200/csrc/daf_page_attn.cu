@@ -663,13 +663,14 @@ page_decode_kernel(const PageAttnArgs a) {
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, d));
             const float mine = partial_weight(ml, mx);
+            const unsigned some = __ballot_sync(0xFFFFFFFFu, ml.y != 0.f);       // pieces with keys; the others' memory holds anything
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             float sum = mine * ml.y;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
             auto add = [&](int i, float4 v) {
                 const float w = __shfl_sync(0xFFFFFFFFu, mine, i);
-                const bool counts = w != 0.f;          // (the others' memory holds anything)
+                const bool counts = (some >> i) & 1u;         // (a weight of 0 still takes a NaN along)
                 acc.x += counts ? w * v.x : 0.f; acc.y += counts ? w * v.y : 0.f;
                 acc.z += counts ? w * v.z : 0.f; acc.w += counts ? w * v.w : 0.f;
             };
@@ -1553,8 +1554,8 @@ __global__ void __launch_bounds__(256) page_merge_kernel(const PageAttnArgs a, i
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.f;
         auto add = [&](float2 x, float4 y) {
+            if (x.y == 0.f) return;                  // no keys (a weight of 0 still takes a NaN along)
             const float w = partial_weight(x, mx);
-            if (w == 0.f) return;
             sum += w * x.y;
             acc.x += w * y.x; acc.y += w * y.y; acc.z += w * y.z; acc.w += w * y.w;
         };

@@ -1059,3 +1059,21 @@ def test_many_launches_give_the_same_bits(n, L_q, Hq, Hkv, T, lo, hi):
             continue
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), (i, (out != first[0]).any(-1).nonzero()[:3].tolist())
     assert api.daf_poll_status(ws) == api.DAF_OK
+
+
+@pytest.mark.parametrize("L_q,Hq", [(1, 2), (3, 8), (1, 24), (13, 2), (25, 8)])
+@pytest.mark.parametrize("n", [1, 40])
+def test_nan_in_a_part_that_hardly_counts(L_q, Hq, n):
+    """Logits hundreds apart: parts of a row that several warps or CTAs worked on get a weight of 0, and a NaN in one has to stay."""
+    lens = [3000] if n == 1 else [100 + 13 * i for i in range(n)]
+    c = _cache_for(lens, 16, 1, seed=67, junk=False)
+    rng = np.random.default_rng(3)
+    for seq, L in enumerate(lens):
+        for j in rng.integers(0, max(1, L - L_q), 2 if n == 1 else 1):
+            x = "k8" if (seq + n) % 3 == 0 else "v8"
+            c.np[x][0, c.np["table"][seq, j // 16], 0, j % 16, rng.integers(0, 128)] = 0x7F
+    c.up()
+    _attend(c, lens, L_q, Hq, scale=0.3, q_scale=3.0)
+    c.np["k8"][0, c.np["table"][0, 5], 0, 3, 1] = 0xFF
+    c.up()
+    _attend(c, lens, L_q, Hq, scale=0.3, q_scale=3.0, seed=1)
