@@ -1273,7 +1273,7 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             if (warp == 10 || warp == 11) {
                 // ---------------------------------------------------------------------------------------- bytes and scales
                 const int kv = warp - 10, seq = sm->at.seq, h = sm->at.h, len = sm->at.len;
-                const bool reports = kv == 0 && h == 0 && sm->at.block == 0;
+                const bool reports = kv == 0 && h == 0;       // (each block: the later ones see more keys)
                 float ks = -1.f, vs = -1.f;         // (K's warp) the scales of the pages in ids
                 const int page_bits = 31 - __clz(T), box = min(T, kQSub), pages = kQSub / box;        // copies of half a step
                 const int chunk_page = box < kQSub ? ((lane & 3) * 16) >> page_bits : 0;             // page of a chunk of 16 keys

@@ -1077,3 +1077,12 @@ def test_nan_in_a_part_that_hardly_counts(L_q, Hq, n):
     c.np["k8"][0, c.np["table"][0, 5], 0, 3, 1] = 0xFF
     c.up()
     _attend(c, lens, L_q, Hq, scale=0.3, q_scale=3.0, seed=1)
+
+
+@pytest.mark.parametrize("T,L,L_q,Hq,page", [(16, 1000, 200, 8, 61), (32, 3, 53, 25, 0), (64, 500, 64, 16, 7), (16, 300, 299, 4, 18)])
+def test_a_missing_page_that_only_later_rows_see_is_reported(T, L, L_q, Hq, page):
+    c = _cache_for([L, 40], T, 1, seed=68, junk=False)
+    for gone in (-1, c.n_pages):
+        c.np["table"][0, page] = gone
+        c.up()
+        _attend(c, [L, 40], L_q, Hq, status=api.DAF_ERR_BOUNDS)
