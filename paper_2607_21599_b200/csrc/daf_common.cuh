@@ -405,6 +405,13 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
     return d;
 }
 
+// (the library is compiled to flush subnormal numbers; rows widened from 8 bits keep theirs)
+__device__ __forceinline__ float mul_rn_keep_subnormals(float a, float b) {
+    float d;
+    asm("mul.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
 __device__ __forceinline__ float fast_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -195,7 +195,8 @@ struct ReadArgs {
 
 __device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi, float s) {
     const float4 x = unpack_e4m3x4(lo), y = unpack_e4m3x4(hi);
-    return make_uint4(pack_bf16(x.x * s, x.y * s), pack_bf16(x.z * s, x.w * s), pack_bf16(y.x * s, y.y * s), pack_bf16(y.z * s, y.w * s));
+    auto two = [s](float a, float b) { return pack_bf16(mul_rn_keep_subnormals(a, s), mul_rn_keep_subnormals(b, s)); };
+    return make_uint4(two(x.x, x.y), two(x.z, x.w), two(y.x, y.y), two(y.z, y.w));
 }
 
 // One CTA takes one page, one head, K or V at a time: T * 8 chunks of 16 bytes, all of a thread's requested ahead of the first

@@ -910,11 +910,6 @@ int launch_check_indices(const int32_t* idx, int k, int L_d, DeviceStatus* statu
 // Expands the document rows of an offline cache kept as 8-bit floating point (1 sign, 4 exponent, 3 mantissa
 // bits, bias 7, no infinities) into the bf16 hybrid-cache buffer: element = bf16(scale[head] * value), the product in
 // fp32, both roundings to nearest-even.  A streaming pass (1 byte read, 2 written per element).
-__device__ __forceinline__ float mul_rn_keep_subnormals(float a, float b) {
-    float d;
-    asm("mul.rn.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
 __device__ __forceinline__ uint4 expand8(uint2 bytes, float scale) {
     const __nv_fp8x2_storage_t* pr = reinterpret_cast<const __nv_fp8x2_storage_t*>(&bytes);
     uint32_t w[4];

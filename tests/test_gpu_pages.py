@@ -1086,3 +1086,25 @@ def test_a_missing_page_that_only_later_rows_see_is_reported(T, L, L_q, Hq, page
         c.np["table"][0, page] = gone
         c.up()
         _attend(c, [L, 40], L_q, Hq, status=api.DAF_ERR_BOUNDS)
+
+
+@pytest.mark.parametrize("T", [16, 128])
+def test_read_of_scales_at_the_ends_of_the_range(T):
+    """Products below 2^-126 among them: rounded to bf16's subnormal numbers, as daf_expand_fp8_cache does."""
+    n = 2560 // T
+    c = Cache(n, T, 1, 1, n, seed=T, junk=False)
+    c.np["k8"][:] = (np.arange(n * T * 128) * 37 % 256).astype(np.uint8).reshape(c.np["k8"].shape)
+    c.np["v8"][:] = c.np["k8"][:, ::-1]
+    for x, lo in (("k", -126), ("v", -121)):
+        c.np[x + "_scale"][:] = (2.0 ** (lo + np.arange(n) % 9)).astype(np.float32).reshape(c.np[x + "_scale"].shape)
+    c.np["v_scale"][0, ::4] *= np.float32(1.37)
+    c.np["k_scale"][0, 5] = 2.0 ** 119
+    c.give(0, n * T)
+    k = torch.zeros(n * T, 1, 128, dtype=torch.bfloat16, device=DEV)
+    v, ws = torch.zeros_like(k), _ws(c)
+    api.check(api.daf_page_read(c.p, 0, 1, None, None, _i32([0, n * T]), n * T, c.t["table"], *c.pool(), k, v, ws))
+    assert api.daf_poll_status(ws) == api.DAF_OK
+    for x, got in (("k", k), ("v", v)):
+        want = O.read(c.np[x + "8"], c.np[x + "_scale"], 0, 0, 0, n * T, c.np["table"])
+        assert np.array_equal(got.float().cpu().numpy(), want, equal_nan=True), x
+        assert ((want != 0) & (np.abs(want) < 2.0 ** -126)).any()
