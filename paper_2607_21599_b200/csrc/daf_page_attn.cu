@@ -113,6 +113,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Two bf16 values times a power of two as fp16.  (Subnormal ones too: with K's scale large enough they count.)
+__device__ __forceinline__ uint32_t scaled_f16(uint32_t w, float up) {
+    return pack_f16(mul_rn_keep_subnormals(__uint_as_float(w << 16), up), mul_rn_keep_subnormals(__uint_as_float(w & 0xFFFF0000u), up));
+}
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {            // 0xFF where a byte is NaN (0x7f, 0xff)
     return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
 }
@@ -417,7 +421,7 @@ page_decode_kernel(const PageAttnArgs a) {
             for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    qf[n][kk][j] = pack_f16(__uint_as_float(qf[n][kk][j] << 16) * up, __uint_as_float(qf[n][kk][j] & 0xFFFF0000u) * up);
+                    qf[n][kk][j] = scaled_f16(qf[n][kk][j], up);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int mine = 8 * n + 2 * t + j;
@@ -721,7 +725,7 @@ page_decode_kernel(const PageAttnArgs a) {
 // A block of two tiles shares every widened K and V.  A block of one tile gives its even steps to one group and its odd ones to the
 // other, and the two halves of the result are merged in shared memory.  A group's 256 columns of tensor memory are O and S, 128
 // each.  One S is enough because the groups take turns: while one's products run, the other's softmax does.
-//   Measured: 128 tokens of 28 / 4 heads over 32k keys 86.6 us, 696 TFLOP/s, 42 % of the measured bf16 rate; 4 tokens of 16 sequences of
+//   Measured: 128 tokens of 28 / 4 heads over 32k keys 85 to 87 us, 700 TFLOP/s, 42 % of the measured bf16 rate; 4 tokens of 16 sequences of
 // 4k 39.1 (28 rows of a tile's 128), 64 tokens over 6k 30.0.  A step of both tiles takes some 5800 clocks, of which the tensor cores
 // are busy for 2050; the rest is each group's chain: exponentials 2000 (the unit needs 1024 of them), maximum 550, P on its way 350,
 // products 1500 to 1800.  A piece of work costs some 15,000 clocks beside its steps.  What was measured on the way, same case: steps of
@@ -736,7 +740,7 @@ constexpr int kQStages = 3;        // half steps
 constexpr int kQFull = 2 * kQStages;
 static_assert(kQFull % 2 == 0 && kQFull % kQStages == 0, "a barrier's half steps all have one slot and one pair");
 // Places (a step of two tiles takes three) that a piece of work costs: rows of Q in, results out.  128 tokens of 28 / 4 heads over 32k
-// keys with 8 or 16: 86.4 us, with 12: 85.0 (86.6 with twice the barriers for bytes).
+// keys with 8 or 16: 86.4 us, with 12: 85.0 (before the bytes had twice as many barriers).
 constexpr int kQPad = 12;
 constexpr int kQConsts = 16;       // half steps whose constants are kept: written up to 10 ahead of their last reader
 constexpr int kQRows = 256;
@@ -1085,10 +1089,10 @@ page_question_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
                     for (int i = 0; i < 16; ++i) {
                         const uint4 w = mine[i ^ (rt & 15)];
                         uint4 y;
-                        y.x = pack_f16(__uint_as_float(w.x << 16) * up, __uint_as_float(w.x & 0xFFFF0000u) * up);
-                        y.y = pack_f16(__uint_as_float(w.y << 16) * up, __uint_as_float(w.y & 0xFFFF0000u) * up);
-                        y.z = pack_f16(__uint_as_float(w.z << 16) * up, __uint_as_float(w.z & 0xFFFF0000u) * up);
-                        y.w = pack_f16(__uint_as_float(w.w << 16) * up, __uint_as_float(w.w & 0xFFFF0000u) * up);
+                        y.x = scaled_f16(w.x, up);
+                        y.y = scaled_f16(w.y, up);
+                        y.z = scaled_f16(w.z, up);
+                        y.w = scaled_f16(w.w, up);
                         *reinterpret_cast<uint4*>(dst + (i >> 3) * kQHalf + (((i & 7) ^ (rt & 7)) << 4)) = y;
                     }
                     fence_proxy_async();

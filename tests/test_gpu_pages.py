@@ -1108,3 +1108,14 @@ def test_read_of_scales_at_the_ends_of_the_range(T):
         want = O.read(c.np[x + "8"], c.np[x + "_scale"], 0, 0, 0, n * T, c.np["table"])
         assert np.array_equal(got.float().cpu().numpy(), want, equal_nan=True), x
         assert ((want != 0) & (np.abs(want) < 2.0 ** -126)).any()
+
+
+@pytest.mark.parametrize("L_q", [1, 6, 7, 70])
+@pytest.mark.parametrize("k_exp,q_exp", [(-126, 0), (-126, 100), (90, -92), (119, -121), (-60, 60)])
+def test_key_scales_at_the_ends_of_their_range(L_q, k_exp, q_exp):
+    lens = [700, 4, 90]
+    c = _cache_for(lens, 32, 2, seed=69, junk=False)
+    c.np["k_scale"][:] = 2.0 ** k_exp
+    c.np["k_scale"][0, ::3] *= np.float32(1.37)
+    c.up()
+    _attend(c, lens, L_q, 8, q_scale=2.0 ** q_exp)
